@@ -424,6 +424,78 @@ chn_status chn_embed_fwd(const chn_array *table, const chn_array *ids, const chn
 chn_status chn_embed_bwd(const chn_array *ids, const chn_array *dout, const chn_array *dtable,
                          int accumulate, chn_stream stream);
 
+/* ---- dropout -------------------------------------------------------------------------------------------
+ * y = residual + keep * x / (1 - ratio)      (residual NULL: without it)
+ * x, y, residual: F32 or BF16, one shape, any strides as in chn_elementwise_broadcast (up to CHN_MAX_NDIM dimensions, views,
+ * inputs of stride 0); residual has y's dtype.  ratio in [0, 1).  A dropped element is 0 (the residual's value) whatever x was.
+ * The mask comes from a counter-based generator and is never stored: with the array as rows of its last axis, element (row, col)
+ * is kept where word col % 4 of Philox-4x32 with seven rounds (Salmon et al., "Parallel random numbers: as easy as 1, 2, 3"),
+ * key = seed, counter = (col / 4, row, offset, site), is at least round(ratio * 2^32).  `rng`: I64 (2,) in DEVICE memory, seed
+ * (64 bits) and offset (its low 32 bits), read when the work runs: a captured graph draws new masks when rng has been
+ * advanced between replays.  `site` (0 .. 2^32 - 1) tells the places of a step apart that share one rng; two calls with the
+ * same seed, offset and site draw the same mask, and so the gradient of x is the same call on the gradient of y.  The
+ * last axis of up to 2^34 elements, up to 2^32 - 1 rows (CHN_ERR_SHAPE).  ratio 0 copies (adds) and needs no rng.
+ * Each of scale, product, sum and the store rounds once. */
+chn_status chn_dropout(const chn_array *x, const chn_array *residual, double ratio, const chn_array *rng, int64_t site,
+                       const chn_array *y, chn_stream stream);
+/* rng[1] += steps, on the stream: what a training step that draws masks begins or ends with. */
+chn_status chn_rng_advance(const chn_array *rng, int64_t steps, chn_stream stream);
+
+/* ---- layer normalisation -----------------------------------------------------------------------------------
+ * Every row of x (N,C), F32 or BF16, row-major with unit inner stride and any pitch:
+ *   mean = sum x / C      rstd = 1 / sqrt(sum (x - mean)^2 / C + eps)      y = (x - mean) * rstd * gamma + beta
+ * gamma, beta: (C,) F32 or NULL (1 and 0).  y: F32 or BF16.  mean, rstd: (N,) F32, for the backward pass, or NULL.
+ * Statistics and sums are fp32 in a fixed order (bit-reproducible).  eps finite and not negative.  Rows without
+ * elements (N > 0, C = 0) are CHN_ERR_SHAPE.
+ * Backward, from x and the retained statistics, with h = (x - mean) rstd and g = dy gamma:
+ *   dx = rstd (g - sum g / C - h sum(g h) / C)     dgamma = sum over rows of dy h     dbeta = sum over rows of dy
+ * dy: F32 or BF16; dx: x's dtype; dgamma, dbeta: (C,) F32 or NULL.  Workspace, where dgamma or dbeta is wanted:
+ * chn_layer_norm_bwd_workspace_bytes(x), 256-byte aligned, the library's until the work on `stream` is done.
+ * An output may be the very array of an input (y over x, dx over dy or x). */
+chn_status chn_layer_norm_fwd(const chn_array *x, const chn_array *gamma, const chn_array *beta, double eps, const chn_array *y,
+                              const chn_array *mean, const chn_array *rstd, chn_stream stream);
+size_t chn_layer_norm_bwd_workspace_bytes(const chn_array *x);
+chn_status chn_layer_norm_bwd(const chn_array *dy, const chn_array *x, const chn_array *mean, const chn_array *rstd,
+                              const chn_array *gamma, const chn_array *dx, const chn_array *dgamma, const chn_array *dbeta,
+                              void *ws, size_t ws_bytes, chn_stream stream);
+
+/* What a residual block does between two layers, in one pass over the rows:
+ *   sum = residual + dropout(x)      y = layer_norm(sum), the sum as it is stored
+ * with chn_dropout's mask and roundings and chn_layer_norm_fwd's statistics: the results of the two calls, where sum has the type
+ * of residual (the stream's, F32 or BF16) and y that of x (the layer's, F32 or BF16).
+ * Backward, from dy (the layer's type) and the gradient dsum that reaches the sum from further on (the stream's, or NULL):
+ *   t = layer_norm's dx + dsum      dresidual = t (stream's type, or NULL)      dx = dropout(t) with the forward's mask
+ * (layer's type, or NULL; both from the fp32 t); dgamma, dbeta and the workspace (chn_layer_norm_bwd_workspace_bytes(sum)) as above.
+ * sum may be the array of residual, dresidual that of dsum, y that of x, dx that of dy. */
+chn_status chn_residual_norm_fwd(const chn_array *x, const chn_array *residual, double ratio, const chn_array *rng, int64_t site,
+                                 const chn_array *gamma, const chn_array *beta, double eps, const chn_array *sum,
+                                 const chn_array *y, const chn_array *mean, const chn_array *rstd, chn_stream stream);
+chn_status chn_residual_norm_bwd(const chn_array *dy, const chn_array *dsum, const chn_array *sum, const chn_array *mean,
+                                 const chn_array *rstd, const chn_array *gamma, double ratio, const chn_array *rng, int64_t site,
+                                 const chn_array *dresidual, const chn_array *dx, const chn_array *dgamma, const chn_array *dbeta,
+                                 void *ws, size_t ws_bytes, chn_stream stream);
+
+/* ---- sampling ------------------------------------------------------------------------------------------------
+ * One token for each row of logits (N,V), F32 or BF16, row-major with any pitch (what a language model answers with; chn_argmax_axis
+ * takes the best).  u (N,) F32: a number in [0, 1) for each row.  temperature, top_p, min_p (N,) F32 and top_k (N,) I32 or
+ * I64: parameters by row (stride 0: one for all rows), each NULL where it is not used.  out (N,) I32 or I64.  In a row:
+ *   - tokens whose logit is -inf or NaN are never drawn; a row that has no others yields -1;
+ *   - temperature t > 0: w_i = exp((z_i - max z) / t) (of an infinite maximum: 1 for the tokens that have it, 0 for the others);
+ *     any other temperature (0): the first token with the largest logit, whatever the filters say; NULL: 1;
+ *   - top_k k > 0: only the k largest logits, among equals the first by index; k <= 0: all;
+ *   - top_p p < 1: of what is left, in descending order (equals by index), every token before which the weights sum to less than
+ *     p times the sum of what is left, and always the first one; p >= 1 or NaN: all;
+ *   - min_p: of what is left only tokens with w_i >= min(min_p, 1); 0, NaN: all;
+ *   - the token: the first, in the order of indices, whose running sum of kept weights exceeds u times their sum.
+ * Weights are summed as whole multiples of 2^-46 (of 2^-(63 - log2 V), V rounded up to a power of two, beyond 2^17 tokens), the exponential
+ * in 64 bits: bit-reproducible, and no order of summation shows.  u below 0 or NaN counts as 0, from 1 on the last kept token is drawn.  V up to
+ * 2^30; V = 0 with N > 0 is CHN_ERR_SHAPE.  Workspace: optional, chn_sample_workspace_bytes(logits), 256-byte aligned, the library's
+ * until the work on `stream` is done; it lets several workgroups share a row.  Without it the same tokens, possibly later. */
+size_t chn_sample_workspace_bytes(const chn_array *logits);
+chn_status chn_sample(const chn_array *logits, const chn_array *u, const chn_array *temperature, const chn_array *top_k,
+                      const chn_array *top_p, const chn_array *min_p, const chn_array *out, void *ws, size_t ws_bytes,
+                      chn_stream stream);
+
 /* ---- user-defined kernels ----------------------------------------------------------------------------
  * Section "Custom CUDA Kernels" and the figure "Example of a user-defined kernel": a kernel is
  * declared by a list of input parameters, a list of output parameters ("<type> <name>", comma

@@ -31,6 +31,8 @@ EXPORTS = ["chn_elementwise_broadcast", "chn_reduce_axis_workspace_bytes", "chn_
            "chn_lstm_seq_bwd_supported", "chn_lstm_seq_bwd_in_xcd", "chn_lstm_seq_bwd_workspace_bytes", "chn_lstm_seq_bwd", "chn_lstm_seq_spin_limit", "chn_lstm_seq_meeting",
            "chn_softmax_ce_workspace_bytes", "chn_softmax_ce_fwd", "chn_softmax_ce_bwd", "chn_softmax_ce_bwd2", "chn_softmax_ce_fwd_bwd",
            "chn_sgd_update", "chn_sgd_update_multi", "chn_adam_update_multi", "chn_embed_fwd", "chn_embed_bwd",
+           "chn_dropout", "chn_rng_advance", "chn_layer_norm_fwd", "chn_layer_norm_bwd_workspace_bytes", "chn_layer_norm_bwd",
+           "chn_residual_norm_fwd", "chn_residual_norm_bwd", "chn_sample_workspace_bytes", "chn_sample",
            "chn_status_string", "chn_last_error", "chn_version", "chn_elementwise_plan", "chn_gemm_plan", "chn_gemm_plan_kernel", "chn_gemm_plan_override",
            "chn_user_kernel_config", "chn_user_kernel_stats", "chn_user_kernel_destroy",
            "chn_elementwise_kernel_create", "chn_elementwise_kernel_prepare", "chn_elementwise_kernel_launch",
@@ -123,6 +125,17 @@ def lib():
     L.chn_adam_update_multi.argtypes = [C.c_int, APP, APP, APP, APP, C.c_double, C.c_double, C.c_double, C.c_double, C.c_int64, APP, st]
     L.chn_embed_fwd.argtypes = [AP, AP, AP, st]
     L.chn_embed_bwd.argtypes = [AP, AP, AP, C.c_int, st]
+    L.chn_dropout.argtypes = [AP, AP, C.c_double, AP, C.c_int64, AP, st]
+    L.chn_rng_advance.argtypes = [AP, C.c_int64, st]
+    L.chn_layer_norm_fwd.argtypes = [AP, AP, AP, C.c_double, AP, AP, AP, st]
+    L.chn_layer_norm_bwd_workspace_bytes.argtypes = [AP]
+    L.chn_layer_norm_bwd_workspace_bytes.restype = C.c_size_t
+    L.chn_layer_norm_bwd.argtypes = [AP] * 8 + [vp, C.c_size_t, st]
+    L.chn_residual_norm_fwd.argtypes = [AP, AP, C.c_double, AP, C.c_int64, AP, AP, C.c_double, AP, AP, AP, AP, st]
+    L.chn_residual_norm_bwd.argtypes = [AP] * 6 + [C.c_double, AP, C.c_int64, AP, AP, AP, AP, vp, C.c_size_t, st]
+    L.chn_sample_workspace_bytes.argtypes = [AP]
+    L.chn_sample_workspace_bytes.restype = C.c_size_t
+    L.chn_sample.argtypes = [AP] * 7 + [vp, C.c_size_t, st]
     L.chn_status_string.argtypes = [C.c_int32]
     L.chn_status_string.restype = C.c_char_p
     L.chn_last_error.argtypes = []
@@ -173,8 +186,21 @@ def desc(t):
     a.shape[:n] = t.shape
     a.strides[:n] = [s * isz for s in t.stride()]
     a.dtype = _DTYPES[t.dtype]
+    a.device = t.get_device()
     t._chn_desc = a
     return a
+
+
+def _here(*arrays):
+    """Descriptors of the arrays, which have to lie on the current device, whose stream the call goes to."""
+    current = _raw_device() if _raw_device is not None else torch.cuda.current_device()
+    out = []
+    for t in arrays:
+        d = desc(t)
+        if d is not None and getattr(d, "device", current) != current:
+            raise ValueError("an array lies on %s, the current device is cuda:%d" % ("the host" if d.device < 0 else "cuda:%d" % d.device, current))
+        out.append(None if d is None else C.byref(d))
+    return out
 
 
 def raw_desc(ptr, shape, strides_bytes, dtype):
@@ -539,6 +565,62 @@ def embed_bwd(ids, dout, dtable, accumulate=False, stream=None):
     _check(lib().chn_embed_bwd(_ref(desc(ids)), _ref(desc(dout)), _ref(desc(dtable)), int(accumulate),
                                _stream() if stream is None else stream))
     return dtable
+
+
+def dropout(x, y, ratio, rng=None, site=0, residual=None, stream=None):
+    """y = (residual +) dropout(x); rng: int64 tensor (seed, offset).  The gradient of x is the same call on the gradient of y."""
+    dx, dr, dg, dy = _here(x, residual, rng, y)
+    _check(lib().chn_dropout(dx, dr, float(ratio), dg, int(site), dy, _stream() if stream is None else stream))
+    return y
+
+
+def rng_advance(rng, steps=1, stream=None):
+    """rng[1] += steps on the stream: later draws (a replayed graph's too) use other masks."""
+    _check(lib().chn_rng_advance(_here(rng)[0], int(steps), _stream() if stream is None else stream))
+    return rng
+
+
+def layer_norm_fwd(x, y, gamma=None, beta=None, eps=1e-5, mean=None, rstd=None, stream=None):
+    dx, dg, db, dy, dm, dr = _here(x, gamma, beta, y, mean, rstd)
+    _check(lib().chn_layer_norm_fwd(dx, dg, db, float(eps), dy, dm, dr, _stream() if stream is None else stream))
+    return y
+
+
+def layer_norm_bwd_workspace_bytes(x):
+    return lib().chn_layer_norm_bwd_workspace_bytes(_ref(desc(x)))
+
+
+def layer_norm_bwd(dy, x, mean, rstd, dx, gamma=None, dgamma=None, dbeta=None, ws=None, stream=None):
+    p, n = _ws(ws)
+    _check(lib().chn_layer_norm_bwd(*_here(dy, x, mean, rstd, gamma, dx, dgamma, dbeta), p, n, _stream() if stream is None else stream))
+    return dx
+
+
+def residual_norm_fwd(x, residual, s, y, gamma=None, beta=None, eps=1e-5, mean=None, rstd=None, ratio=0.0, rng=None, site=0, stream=None):
+    """s = residual + dropout(x), y = layer_norm(s)."""
+    dx, dres, ds, dy, dg, db, dm, dr, drng = _here(x, residual, s, y, gamma, beta, mean, rstd, rng)
+    _check(lib().chn_residual_norm_fwd(dx, dres, float(ratio), drng, int(site), dg, db, float(eps), ds, dy, dm, dr,
+                                       _stream() if stream is None else stream))
+    return y
+
+
+def residual_norm_bwd(dy, ds, s, mean, rstd, dresidual, dx, gamma=None, dgamma=None, dbeta=None, ratio=0.0, rng=None, site=0, ws=None, stream=None):
+    """dresidual and dx from the gradients dy of y and ds of s (or None)."""
+    p, n = _ws(ws)
+    a = _here(dy, ds, s, mean, rstd, gamma, rng, dresidual, dx, dgamma, dbeta)
+    _check(lib().chn_residual_norm_bwd(*a[:6], float(ratio), a[6], int(site), *a[7:], p, n, _stream() if stream is None else stream))
+    return dx
+
+
+def sample_workspace_bytes(logits):
+    return lib().chn_sample_workspace_bytes(_ref(desc(logits)))
+
+
+def sample(logits, u, out, temperature=None, top_k=None, top_p=None, min_p=None, ws=None, stream=None):
+    """out[n]: a token of row n, drawn by u[n]; parameters are tensors of one value for each row (stride 0: one for all), None: not used."""
+    p, n = _ws(ws)
+    _check(lib().chn_sample(*_here(logits, u, temperature, top_k, top_p, min_p, out), p, n, _stream() if stream is None else stream))
+    return out
 
 
 # ---- user-defined kernels ---------------------------------------------------------------------------------
