@@ -170,6 +170,12 @@ __device__ __forceinline__ void store16_any(T *p, const Vec16<T> &x) {
   __builtin_memcpy(&v, &x.raw, 16);
   *reinterpret_cast<chn_u32x4_any *>(p) = v;
 }
+template <typename T>
+__device__ __forceinline__ void store16_any_nt(T *p, const Vec16<T> &x) {
+  chn_u32x4 v;
+  __builtin_memcpy(&v, &x.raw, 16);
+  __builtin_nontemporal_store(v, reinterpret_cast<chn_u32x4_any *>(p));
+}
 // The first n (0 .. whole vector) elements only; the others read as zero / stay untouched.  The elements are moved as they
 // are.  In two-byte types a partial load takes the last one again in place of those beyond n, so that its eight loads are in
 // flight together (behind conditions, each waits for the word it shares: 1392 x 7 transposed 7.4 us, 5.2 like this); the

@@ -8,7 +8,13 @@
 //
 // All sums and statistics are fp32; the mean is corrected by the mean of what is left after its subtraction, so that rows whose mean
 // is far larger than their spread keep their digits.
+//
+// Bound by memory: every element is read once and written once.  A row is held in the registers of 16, 64, 256 or 1024 lanes between the
+// passes that its statistics need (rows.h); only rows that no block can hold are read again.
 #include "philox.h"
+#include "rows.h"
+
+#include <type_traits>
 
 namespace chn {
 namespace {
@@ -22,57 +28,217 @@ struct NormArgs {
   DropArgs drop;
 };
 
-__device__ __forceinline__ float block_sum(float v, float *smem) {
-  v = wave_sum(v);
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) smem[threadIdx.x >> 6] = v;
-  __syncthreads();
-  return smem[0] + smem[1] + smem[2] + smem[3];
+// The word of one column, for the elements behind the last whole unit.
+__device__ __forceinline__ uint32_t word_of(const DropState &d, uint32_t c, uint32_t row) {
+  const Philox4 w = d.words(c >> 2, row);
+  return (c & 2) ? ((c & 1) ? w.w[3] : w.w[2]) : ((c & 1) ? w.w[1] : w.w[0]);
 }
 
-// TL: the layer's type (x and y); TS: the stream's (residual and s); RES: s = residual + dropout(x) is formed and stored first
-template <typename TX, typename TY, typename TS, bool RES>
-__global__ __launch_bounds__(256) void norm_fwd_kernel(const TX *x, const TS *residual, TS *s, TY *y, NormArgs a) {
-  __shared__ float smem[4];
-  const DropState d(a.drop);
-  const float inv = 1.0f / (float)a.C;
-  for (int64_t row = blockIdx.x; row < a.N; row += gridDim.x) {
-    float sum = 0.0f;
-    if constexpr (RES) {
-      for (int64_t c0 = threadIdx.x * 4; c0 < a.C; c0 += 1024) {
-        Philox4 w{{~0u, ~0u, ~0u, ~0u}};
-        if (a.drop.rng) w = d.words((uint32_t)(c0 >> 2), (uint32_t)row);
-        for (int j = 0; j < 4 && c0 + j < a.C; ++j) {
-          const float v = add_rounded(Elem<TS>::load(residual + row * a.pr + c0 + j), d.apply(Elem<TX>::load(x + row * a.px + c0 + j), w.w[j]));
-          Elem<TS>::store(s + row * a.ps + c0 + j, v);
-        }
-      }
-    }
-    const auto at = [&](int64_t c) -> float {
-      if constexpr (RES) return Elem<TS>::load(s + row * a.ps + c);
-      else return Elem<TX>::load(x + row * a.px + c);
-    };
-    // (a thread reads the elements that it stored itself)
-    const auto each = [&](auto f) {
-      for (int64_t c0 = threadIdx.x * 4; c0 < a.C; c0 += 1024)
-        for (int j = 0; j < 4 && c0 + j < a.C; ++j) f(c0 + j);
-    };
-    each([&](int64_t c) { sum += at(c); });
-    const float m0 = block_sum(sum, smem) * inv;
-    float dev = 0.0f, sq = 0.0f;
-    each([&](int64_t c) { const float t = at(c) - m0; dev += t; sq += t * t; });
-    const float m1 = block_sum(dev, smem) * inv;
-    const float var = fmaxf(block_sum(sq, smem) * inv - m1 * m1, 0.0f);
-    const float rstd = 1.0f / sqrtf(var + a.eps);
-    if (threadIdx.x == 0) {
-      if (a.mean) a.mean[row] = m0 + m1;
-      if (a.rstd) a.rstd[row] = rstd;
-    }
-    each([&](int64_t c) {
-      const float h = ((at(c) - m0) - m1) * rstd;
-      Elem<TY>::store(y + row * a.py + c, h * (a.gamma ? a.gamma[c] : 1.0f) + (a.beta ? a.beta[c] : 0.0f));
-    });
+// v[0 .. E) dropped out, columns from c0 (a multiple of four) on
+template <int E>
+__device__ __forceinline__ void drop_unit(const DropState &d, uint32_t c0, uint32_t row, float (&v)[E]) {
+#pragma unroll
+  for (int b = 0; b < E / 4; ++b) {
+    const Philox4 w = d.words((c0 >> 2) + b, row);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[b * 4 + j] = d.apply(v[b * 4 + j], w.w[j]);
   }
+}
+
+// One row by G lanes of KE elements each; groups of up to 256 lanes share a block of 256.  (Kernels that walk over rows with gamma and beta
+// in registers are slower: 8192 x 4096 bf16 24.9 us with 2048 blocks, 22.1 with a block for each row.)  Results are stored past the
+// caches' usual order of replacement, since nothing of them is read here again: 4480 x 650 fp32 6.1 -> 5.6 us, 1024 x 1000 with residual 5.3 -> 5.0.
+template <typename TX, typename TY, typename TS, bool RES, int G, int KE>
+__global__ __launch_bounds__(G > 256 ? G : 256) void norm_fwd_rows_kernel(const TX *x, const TS *residual, TS *s, TY *y, NormArgs a) {
+  constexpr int E = unit_elements<TX, TY, TS>(), K = KE / E, GROUPS = (G > 256 ? G : 256) / G;
+  __shared__ float2 smem[G > 64 ? 2 * G / 64 : 1];
+  const int C = (int)a.C, whole = C / E, left = C - whole * E;
+  const float inv = 1.0f / (float)C;
+  const int g = threadIdx.x % G;
+  int64_t row = (int64_t)blockIdx.x * GROUPS;
+  if constexpr (G == 64) row += __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+  else if constexpr (G < 64) row += threadIdx.x / G;
+  if (row >= a.N) return;                                // (groups that share a block meet at no barrier)
+  const int cl = whole * E + g;                          // (l: the element behind the last whole unit, in the first few lanes)
+  const TX *xr = x + row * a.px;
+  TY *yr = y + row * a.py;
+  float v[K][E], vl = 0.0f;
+  Unit<TX, E> xu[K];
+#pragma unroll
+  for (int k = 0; k < K; ++k) {
+    xu[k].zero();
+    if (g + k * G < whole) xu[k].load(xr + (g + k * G) * E);
+  }
+  if (g < left) vl = Elem<TX>::load(xr + cl);
+  if constexpr (RES) {
+    const TS *rr = residual + row * a.pr;
+    TS *sr = s + row * a.ps;
+    Unit<TS, E> ru[K];
+    float rl = 0.0f;
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      ru[k].zero();
+      if (g + k * G < whole) ru[k].load(rr + (g + k * G) * E);
+    }
+    if (g < left) rl = Elem<TS>::load(rr + cl);
+    const DropState d(a.drop);
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      const uint32_t c0 = (uint32_t)(g + k * G) * E;
+#pragma unroll
+      for (int i = 0; i < E; ++i) v[k][i] = xu[k].get(i);
+      if (a.drop.rng) drop_unit<E>(d, c0, (uint32_t)row, v[k]);
+#pragma unroll
+      for (int i = 0; i < E; ++i) {
+        ru[k].set(i, add_rounded(ru[k].get(i), v[k][i]));
+        v[k][i] = ru[k].get(i);
+      }
+      if (g + k * G < whole) ru[k].store_nt(sr + c0);
+    }
+    if (g < left) {
+      if (a.drop.rng) vl = d.apply(vl, word_of(d, (uint32_t)cl, (uint32_t)row));
+      vl = as_stored<TS>(add_rounded(rl, vl));
+      Elem<TS>::store(sr + cl, vl);
+    }
+  } else {
+#pragma unroll
+    for (int k = 0; k < K; ++k)
+#pragma unroll
+      for (int i = 0; i < E; ++i) v[k][i] = xu[k].get(i);
+  }
+  float sum = vl;                                        // (lanes without elements hold zeros)
+#pragma unroll
+  for (int k = 0; k < K; ++k)
+#pragma unroll
+    for (int i = 0; i < E; ++i) sum += v[k][i];
+  const float m0 = group_sum<G>(make_float2(sum, 0.0f), smem, 0).x * inv;
+  float dev = 0.0f, sq = 0.0f;
+#pragma unroll
+  for (int k = 0; k < K; ++k) {
+    const bool there = g + k * G < whole;
+#pragma unroll
+    for (int i = 0; i < E; ++i) {
+      v[k][i] = there ? v[k][i] - m0 : 0.0f;
+      dev += v[k][i];
+      sq = fmaf(v[k][i], v[k][i], sq);
+    }
+  }
+  vl = g < left ? vl - m0 : 0.0f;
+  dev += vl;
+  sq = fmaf(vl, vl, sq);
+  const float2 t = group_sum<G>(make_float2(dev, sq), smem, 1);
+  const float m1 = t.x * inv;
+  const float rstd = 1.0f / sqrtf(fmaxf(t.y * inv - m1 * m1, 0.0f) + a.eps);
+  if (g == 0) {
+    if (a.mean) a.mean[row] = m0 + m1;
+    if (a.rstd) a.rstd[row] = rstd;
+  }
+#pragma unroll
+  for (int k = 0; k < K; ++k) {
+    const int c0 = (g + k * G) * E;
+    if (g + k * G < whole) {
+      Unit<float, E> gm, bt;
+      if (a.gamma) gm.load(a.gamma + c0);
+      if (a.beta) bt.load(a.beta + c0);
+      Unit<TY, E> yu;
+#pragma unroll
+      for (int i = 0; i < E; ++i) yu.set(i, fmaf((v[k][i] - m1) * rstd, a.gamma ? gm.get(i) : 1.0f, a.beta ? bt.get(i) : 0.0f));
+      yu.store_nt(yr + c0);
+    }
+  }
+  if (g < left) Elem<TY>::store(yr + cl, fmaf((vl - m1) * rstd, a.gamma ? a.gamma[cl] : 1.0f, a.beta ? a.beta[cl] : 0.0f));
+}
+
+// Rows longer than a block holds: three passes over the row, a block of 1024 each.  A thread reads the elements that it stored itself.
+template <typename TX, typename TY, typename TS, bool RES>
+__global__ __launch_bounds__(1024) void norm_fwd_wide_kernel(const TX *x, const TS *residual, TS *s, TY *y, NormArgs a) {
+  constexpr int E = unit_elements<TX, TY, TS>();
+  __shared__ float2 smem[32];
+  const float inv = 1.0f / (float)a.C;
+  const int64_t row = blockIdx.x, whole = a.C / E;
+  const TX *xr = x + row * a.px;
+  TY *yr = y + row * a.py;
+  TS *sr = RES ? s + row * a.ps : nullptr;
+  const int64_t cl = whole * E + threadIdx.x;
+  const bool last = cl < a.C;
+  const auto at = [&](int64_t u, float (&v)[E]) {
+    if constexpr (RES) {
+      Unit<TS, E> t;
+      t.load(sr + u * E);
+#pragma unroll
+      for (int i = 0; i < E; ++i) v[i] = t.get(i);
+    } else {
+      Unit<TX, E> t;
+      t.load(xr + u * E);
+#pragma unroll
+      for (int i = 0; i < E; ++i) v[i] = t.get(i);
+    }
+  };
+  float sum = 0.0f, vl = last ? Elem<TX>::load(xr + cl) : 0.0f;
+  if constexpr (RES) {
+    const DropState d(a.drop);
+    const TS *rr = residual + row * a.pr;
+    for (int64_t u = threadIdx.x; u < whole; u += 1024) {
+      Unit<TX, E> xu;
+      Unit<TS, E> ru;
+      xu.load(xr + u * E);
+      ru.load(rr + u * E);
+      float v[E];
+#pragma unroll
+      for (int i = 0; i < E; ++i) v[i] = xu.get(i);
+      if (a.drop.rng) drop_unit<E>(d, (uint32_t)u * E, (uint32_t)row, v);
+#pragma unroll
+      for (int i = 0; i < E; ++i) {
+        ru.set(i, add_rounded(ru.get(i), v[i]));
+        sum += ru.get(i);
+      }
+      ru.store(sr + u * E);
+    }
+    if (last) {
+      if (a.drop.rng) vl = d.apply(vl, word_of(d, (uint32_t)cl, (uint32_t)row));
+      vl = as_stored<TS>(add_rounded(Elem<TS>::load(rr + cl), vl));
+      Elem<TS>::store(sr + cl, vl);
+    }
+  } else {
+    for (int64_t u = threadIdx.x; u < whole; u += 1024) {
+      float v[E];
+      at(u, v);
+#pragma unroll
+      for (int i = 0; i < E; ++i) sum += v[i];
+    }
+  }
+  const float m0 = group_sum<1024>(make_float2(sum + vl, 0.0f), smem, 0).x * inv;
+  if (last) vl -= m0;
+  float dev = vl, sq = vl * vl;
+  for (int64_t u = threadIdx.x; u < whole; u += 1024) {
+    float v[E];
+    at(u, v);
+#pragma unroll
+    for (int i = 0; i < E; ++i) {
+      const float t = v[i] - m0;
+      dev += t;
+      sq = fmaf(t, t, sq);
+    }
+  }
+  const float2 t = group_sum<1024>(make_float2(dev, sq), smem, 1);
+  const float m1 = t.x * inv;
+  const float rstd = 1.0f / sqrtf(fmaxf(t.y * inv - m1 * m1, 0.0f) + a.eps);
+  if (threadIdx.x == 0) {
+    if (a.mean) a.mean[row] = m0 + m1;
+    if (a.rstd) a.rstd[row] = rstd;
+  }
+  for (int64_t u = threadIdx.x; u < whole; u += 1024) {
+    float v[E];
+    at(u, v);
+    Unit<float, E> gm, bt;
+    if (a.gamma) gm.load(a.gamma + u * E);
+    if (a.beta) bt.load(a.beta + u * E);
+    Unit<TY, E> yu;
+#pragma unroll
+    for (int i = 0; i < E; ++i) yu.set(i, fmaf(((v[i] - m0) - m1) * rstd, a.gamma ? gm.get(i) : 1.0f, a.beta ? bt.get(i) : 0.0f));
+    yu.store(yr + u * E);
+  }
+  if (last) Elem<TY>::store(yr + cl, fmaf((vl - m1) * rstd, a.gamma ? a.gamma[cl] : 1.0f, a.beta ? a.beta[cl] : 0.0f));
 }
 
 struct NormBwdArgs {
@@ -80,67 +246,375 @@ struct NormBwdArgs {
   int64_t pdy, ps, pds, pdr, pdx;
   const float *gamma, *mean, *rstd;
   float *partial;                    // [strips][2][C] or NULL
-  int64_t strips;
+  int64_t strips;                    // wide rows: as many, of neighbouring rows
+  float2 *sums;                      // wide rows: [N][segments] sums of g and g h
+  int segments;
   DropArgs drop;
 };
 
-// Column sums of dy h and dy over a strip of rows: strip k takes rows k, k + strips, ...
+// One pass: a group of G lanes walks over rows, KE columns a lane, adding dy h and dy of its columns up in registers; at the end the groups
+// of a block join theirs and the block leaves one strip of partial sums.  The rows after this one are on their way while a row is worked on.
+template <typename TX, typename TY, typename TS, bool RES, int G, int KE, int THREADS>
+__global__ __launch_bounds__(THREADS) void norm_bwd_rows_kernel(const TY *dy, const TS *s, const TS *ds, TS *dres, TX *dx, NormBwdArgs a) {
+  constexpr int E = unit_elements<TX, TY, TS>(), K = KE / E, GROUPS = THREADS / G;
+  constexpr int PARTS = G < 64 ? THREADS / 64 : GROUPS;   // sets of column sums that a block joins
+  constexpr int SPAN = G * KE;
+  __shared__ float2 smem[G > 64 ? 2 * THREADS / 64 : 1];
+  __shared__ float joined[PARTS > 1 ? PARTS * 2 * SPAN : 1];
+  const DropState d(a.drop);
+  const int C = (int)a.C, whole = C / E, left = C - whole * E;
+  const float inv = 1.0f / (float)C;
+  const int g = threadIdx.x % G;
+  const int64_t stride = (int64_t)gridDim.x * GROUPS;
+  int64_t row = (int64_t)blockIdx.x * GROUPS;
+  if constexpr (G >= 64) row += __builtin_amdgcn_readfirstlane(threadIdx.x / G);
+  else row += threadIdx.x / G;
+  const int cl = whole * E + g;
+  // gamma: in registers where a wave has the row, in LDS where a block has it (the registers are worth more there)
+  constexpr bool SHARED = G > 64;
+  __shared__ __align__(16) float gs[SHARED ? G * KE + 8 : 1];
+  float gm[SHARED ? 1 : K][E], gml = 1.0f;
+  float ag[K][E] = {}, ab[K][E] = {}, agl = 0.0f, abl = 0.0f;
+  if constexpr (SHARED) {
+    for (int c = threadIdx.x; c < C; c += THREADS) gs[c] = a.gamma ? a.gamma[c] : 1.0f;
+    __syncthreads();
+    if (g < left) gml = gs[cl];
+  } else {
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      const int u = g + k * G;
+      Unit<float, E> gu;
+#pragma unroll
+      for (int i = 0; i < E; ++i) gu.set(i, 1.0f);
+      if (u < whole && a.gamma) gu.load(a.gamma + u * E);
+#pragma unroll
+      for (int i = 0; i < E; ++i) gm[k][i] = gu.get(i);
+    }
+    if (g < left && a.gamma) gml = a.gamma[cl];
+  }
+  Unit<TY, E> yu[K];
+  Unit<TS, E> su[K], eu[K];
+  float yl = 0.0f, sl = 0.0f, el = 0.0f, mean = 0.0f, rstd = 0.0f;
+#pragma unroll
+  for (int k = 0; k < K; ++k) {
+    yu[k].zero();
+    su[k].zero();
+    eu[k].zero();
+  }
+  const auto fetch = [&](int64_t r) __attribute__((always_inline)) {
+    if (r >= a.N) return;
+    const TY *yr = dy + r * a.pdy;
+    const TS *sr = s + r * a.ps;
+#pragma unroll
+    for (int k = 0; k < K; ++k)
+      if (g + k * G < whole) {
+        yu[k].load(yr + (g + k * G) * E);
+        su[k].load(sr + (g + k * G) * E);
+      }
+    if (g < left) {
+      yl = Elem<TY>::load(yr + cl);
+      sl = Elem<TS>::load(sr + cl);
+    }
+    if constexpr (RES) {
+      if (ds) {
+        const TS *er = ds + r * a.pds;
+#pragma unroll
+        for (int k = 0; k < K; ++k)
+          if (g + k * G < whole) eu[k].load(er + (g + k * G) * E);
+        if (g < left) el = Elem<TS>::load(er + cl);
+      }
+    }
+    mean = a.mean[r];
+    rstd = a.rstd[r];
+  };
+  int turn = 0;
+  fetch(row);
+  // (the waves of a block that meet at barriers make the same number of turns)
+  for (int64_t first = G > 64 ? (int64_t)blockIdx.x * GROUPS : row; first < a.N; first += stride, row += stride) {
+    const bool there_row = row < a.N;
+    float h[K][E], gv[K][E], ev[K][E];
+    float hl = 0.0f, gl = 0.0f, evl = 0.0f;
+    const float rs = rstd, me = mean;
+    float sg = 0.0f, sgh = 0.0f;
+    if (G <= 64 || there_row) {
+#pragma unroll
+      for (int k = 0; k < K; ++k) {
+        const bool there = g + k * G < whole;
+        float gk[E];
+        if constexpr (SHARED) {
+#pragma unroll
+          for (int i = 0; i < E; i += 4) *reinterpret_cast<float4 *>(gk + i) = *reinterpret_cast<const float4 *>(gs + (g + k * G) * E + i);
+        }
+#pragma unroll
+        for (int i = 0; i < E; ++i) {
+          const float v = yu[k].get(i);
+          h[k][i] = there ? (su[k].get(i) - me) * rs : 0.0f;
+          gv[k][i] = there ? v * (SHARED ? gk[i] : gm[SHARED ? 0 : k][i]) : 0.0f;
+          ag[k][i] = fmaf(v, h[k][i], ag[k][i]);
+          ab[k][i] += v;
+          sg += gv[k][i];
+          sgh = fmaf(gv[k][i], h[k][i], sgh);
+          if constexpr (RES) ev[k][i] = eu[k].get(i);
+        }
+      }
+      hl = g < left ? (sl - me) * rs : 0.0f;
+      gl = yl * gml;
+      evl = el;
+      agl = fmaf(yl, hl, agl);
+      abl += yl;
+      sg += gl;
+      sgh = fmaf(gl, hl, sgh);
+    }
+    fetch(row + stride);
+    const float2 t = group_sum<G>(make_float2(sg, sgh), smem + (G > 64 ? threadIdx.x / G * (2 * G / 64) : 0), turn);
+    turn ^= 1;
+    if (G > 64 && !there_row) break;                      // (the last turn)
+    const float c1 = t.x * inv, c2 = t.y * inv;
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      const uint32_t c0 = (uint32_t)(g + k * G) * E;
+      float o[E];
+#pragma unroll
+      for (int i = 0; i < E; ++i) {
+        o[i] = rs * (gv[k][i] - c1 - h[k][i] * c2);
+        if constexpr (RES) {
+          if (ds) o[i] += ev[k][i];
+        }
+      }
+      if constexpr (RES) {
+        if (dres) {
+          Unit<TS, E> out;
+#pragma unroll
+          for (int i = 0; i < E; ++i) out.set(i, o[i]);
+          if (g + k * G < whole) out.store_nt(dres + row * a.pdr + c0);
+        }
+        if (dx && a.drop.rng) drop_unit<E>(d, c0, (uint32_t)row, o);
+      }
+      if (!RES || dx) {
+        Unit<TX, E> out;
+#pragma unroll
+        for (int i = 0; i < E; ++i) out.set(i, o[i]);
+        if (g + k * G < whole) out.store_nt(dx + row * a.pdx + c0);
+      }
+    }
+    if (g < left) {
+      float o = rs * (gl - c1 - hl * c2);
+      if constexpr (RES) {
+        if (ds) o += evl;
+        if (dres) Elem<TS>::store(dres + row * a.pdr + cl, o);
+        if (dx && a.drop.rng) o = d.apply(o, word_of(d, (uint32_t)cl, (uint32_t)row));
+      }
+      if (!RES || dx) Elem<TX>::store(dx + row * a.pdx + cl, o);
+    }
+  }
+  if (!a.partial) return;
+  float *pg = a.partial + (int64_t)blockIdx.x * 2 * C, *pb = pg + C;
+  if constexpr (GROUPS == 1) {
+#pragma unroll
+    for (int k = 0; k < K; ++k)
+      if (g + k * G < whole) {
+        Unit<float, E> out;
+#pragma unroll
+        for (int i = 0; i < E; ++i) out.set(i, ag[k][i]);
+        out.store(pg + (g + k * G) * E);
+#pragma unroll
+        for (int i = 0; i < E; ++i) out.set(i, ab[k][i]);
+        out.store(pb + (g + k * G) * E);
+      }
+    if (g < left) {
+      pg[cl] = agl;
+      pb[cl] = abl;
+    }
+  } else {
+    // groups of 16 first join within their wave, in the order of the rows of lanes
+    const auto join16 = [&](float v) -> float {
+      if constexpr (G == 16) {
+        const int l = threadIdx.x & 15;
+        return (__shfl(v, l, 64) + __shfl(v, l + 16, 64)) + (__shfl(v, l + 32, 64) + __shfl(v, l + 48, 64));
+      }
+      return v;
+    };
+    const int part = threadIdx.x / (G < 64 ? 64 : G);
+    const bool writes = G >= 64 || (threadIdx.x & 63) < G;
+    float *mg = joined + part * SPAN, *mb = joined + (PARTS + part) * SPAN;
+#pragma unroll
+    for (int k = 0; k < K; ++k)
+#pragma unroll
+      for (int i = 0; i < E; ++i) {
+        const float vg = join16(ag[k][i]), vb = join16(ab[k][i]);
+        if (writes) {
+          mg[(g + k * G) * E + i] = vg;
+          mb[(g + k * G) * E + i] = vb;
+        }
+      }
+    const float vg = join16(agl), vb = join16(abl);
+    const auto add_up = [&](int c, int at) {
+      float sg = joined[at], sb = joined[PARTS * SPAN + at];
+#pragma unroll
+      for (int p = 1; p < PARTS; ++p) {
+        sg += joined[p * SPAN + at];
+        sb += joined[(PARTS + p) * SPAN + at];
+      }
+      pg[c] = sg;
+      pb[c] = sb;
+    };
+    __syncthreads();
+    for (int c = threadIdx.x; c < whole * E; c += THREADS) add_up(c, c);
+    if (left > 0) {
+      __syncthreads();
+      if (writes && g < left) {
+        mg[g] = vg;
+        mb[g] = vb;
+      }
+      __syncthreads();
+      if ((int)threadIdx.x < left) add_up(whole * E + (int)threadIdx.x, (int)threadIdx.x);
+    }
+  }
+}
+
+
+// Rows longer than a block holds with their column sums, in two launches.  First the rows' sums of g and g h: a block has a segment of a
+// row, so that few rows still fill the chip.
 template <typename TY, typename TS>
-__global__ __launch_bounds__(256) void norm_partial_kernel(const TY *dy, const TS *s, NormBwdArgs a) {
-  const int64_t c = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (c >= a.C) return;
-  float sg = 0.0f, sb = 0.0f;
-  for (int64_t row = blockIdx.y; row < a.N; row += a.strips) {
-    const float g = Elem<TY>::load(dy + row * a.pdy + c);
-    sg += g * ((Elem<TS>::load(s + row * a.ps + c) - a.mean[row]) * a.rstd[row]);
-    sb += g;
+__global__ __launch_bounds__(256) void norm_bwd_sums_kernel(const TY *dy, const TS *s, NormBwdArgs a) {
+  constexpr int E = unit_elements<TY, TS>();
+  __shared__ float2 smem[8];
+  const int64_t row = blockIdx.x, units = (a.C + E - 1) / E, per = (units + a.segments - 1) / a.segments;
+  const int64_t u0 = blockIdx.y * per, u1 = u0 + per < units ? u0 + per : units;
+  const TY *yr = dy + row * a.pdy;
+  const TS *sr = s + row * a.ps;
+  const float mean = a.mean[row], rstd = a.rstd[row];
+  float sg = 0.0f, sgh = 0.0f;
+  for (int64_t u = u0 + threadIdx.x; u < u1; u += 256) {
+    const int64_t c0 = u * E;
+    if (c0 + E <= a.C) {
+      Unit<TY, E> yu;
+      Unit<TS, E> su;
+      Unit<float, E> gm;
+      yu.load(yr + c0);
+      su.load(sr + c0);
+      if (a.gamma) gm.load(a.gamma + c0);
+#pragma unroll
+      for (int i = 0; i < E; ++i) {
+        const float g = a.gamma ? yu.get(i) * gm.get(i) : yu.get(i);
+        sg += g;
+        sgh = fmaf(g, (su.get(i) - mean) * rstd, sgh);
+      }
+    } else {
+      for (int64_t c = c0; c < a.C; ++c) {
+        const float g = Elem<TY>::load(yr + c) * (a.gamma ? a.gamma[c] : 1.0f);
+        sg += g;
+        sgh = fmaf(g, (Elem<TS>::load(sr + c) - mean) * rstd, sgh);
+      }
+    }
   }
-  a.partial[(blockIdx.y * 2) * a.C + c] = sg;
-  a.partial[(blockIdx.y * 2 + 1) * a.C + c] = sb;
+  const float2 t = group_sum<256>(make_float2(sg, sgh), smem, 0);
+  if (threadIdx.x == 0) a.sums[row * a.segments + blockIdx.y] = t;
 }
 
-// The strips' sums added in their order.
-__global__ __launch_bounds__(256) void norm_fold_kernel(const float *partial, int64_t strips, int64_t C, float *dgamma, float *dbeta) {
-  const int64_t c = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (c >= C) return;
-  float sg = 0.0f, sb = 0.0f;
-  for (int64_t k = 0; k < strips; ++k) {
-    sg += partial[(k * 2) * C + c];
-    sb += partial[(k * 2 + 1) * C + c];
-  }
-  if (dgamma) dgamma[c] = sg;
-  if (dbeta) dbeta[c] = sb;
-}
-
+// Then the gradients: a thread has E columns and walks over the neighbouring rows of a strip, so that the column sums need no exchange.
 template <typename TX, typename TY, typename TS, bool RES>
-__global__ __launch_bounds__(256) void norm_bwd_kernel(const TY *dy, const TS *s, const TS *ds, TS *dres, TX *dx, NormBwdArgs a) {
-  __shared__ float smem[4];
+__global__ __launch_bounds__(256) void norm_bwd_wide_kernel(const TY *dy, const TS *s, const TS *ds, TS *dres, TX *dx, NormBwdArgs a) {
+  constexpr int E = unit_elements<TX, TY, TS>();
+  const int64_t c0 = ((int64_t)blockIdx.x * 256 + threadIdx.x) * E;
+  if (c0 >= a.C) return;
   const DropState d(a.drop);
   const float inv = 1.0f / (float)a.C;
-  for (int64_t row = blockIdx.x; row < a.N; row += gridDim.x) {
+  const int n = a.C - c0 < E ? (int)(a.C - c0) : E;     // columns of this thread
+  const bool all = n == E;
+  float gm[E], ag[E] = {}, ab[E] = {};
+#pragma unroll
+  for (int i = 0; i < E; ++i) gm[i] = a.gamma && i < n ? a.gamma[c0 + i] : 1.0f;
+  const int64_t per = (a.N + a.strips - 1) / a.strips, r0 = blockIdx.y * per, r1 = r0 + per < a.N ? r0 + per : a.N;
+  for (int64_t row = r0; row < r1; ++row) {
     const float mean = a.mean[row], rstd = a.rstd[row];
     float sg = 0.0f, sgh = 0.0f;
-    for (int64_t c = threadIdx.x; c < a.C; c += 256) {
-      const float g = Elem<TY>::load(dy + row * a.pdy + c) * (a.gamma ? a.gamma[c] : 1.0f);
-      sg += g;
-      sgh += g * ((Elem<TS>::load(s + row * a.ps + c) - mean) * rstd);
+    for (int k = 0; k < a.segments; ++k) {
+      const float2 t = a.sums[row * a.segments + k];
+      sg += t.x;
+      sgh += t.y;
     }
-    const float c1 = block_sum(sg, smem) * inv, c2 = block_sum(sgh, smem) * inv;
-    for (int64_t c0 = threadIdx.x * 4; c0 < a.C; c0 += 1024) {
-      Philox4 w{{~0u, ~0u, ~0u, ~0u}};
-      if (RES && a.drop.rng && dx) w = d.words((uint32_t)(c0 >> 2), (uint32_t)row);
-      for (int j = 0; j < 4 && c0 + j < a.C; ++j) {
-        const int64_t c = c0 + j;
-        const float g = Elem<TY>::load(dy + row * a.pdy + c) * (a.gamma ? a.gamma[c] : 1.0f);
-        const float h = (Elem<TS>::load(s + row * a.ps + c) - mean) * rstd;
-        float v = rstd * (g - c1 - h * c2);
-        if constexpr (RES) {
-          if (ds) v += Elem<TS>::load(ds + row * a.pds + c);
-          if (dres) Elem<TS>::store(dres + row * a.pdr + c, v);
-          if (dx) Elem<TX>::store(dx + row * a.pdx + c, d.apply(v, w.w[j]));
-        } else {
-          Elem<TX>::store(dx + row * a.pdx + c, v);
+    const float c1 = sg * inv, c2 = sgh * inv;
+    const TY *yr = dy + row * a.pdy + c0;
+    const TS *sr = s + row * a.ps + c0, *er = RES && ds ? ds + row * a.pds + c0 : nullptr;
+    Unit<TY, E> yu;
+    Unit<TS, E> su, eu;
+    eu.zero();
+    if (all) {
+      yu.load(yr);
+      su.load(sr);
+      if (RES && ds) eu.load(er);
+    } else {
+      yu.zero();
+      su.zero();
+#pragma unroll
+      for (int i = 0; i < E; ++i)
+        if (i < n) {
+          yu.set(i, Elem<TY>::load(yr + i));
+          su.set(i, Elem<TS>::load(sr + i));
+          if (RES && ds) eu.set(i, Elem<TS>::load(er + i));
         }
+    }
+    float o[E];
+#pragma unroll
+    for (int i = 0; i < E; ++i) {
+      const float v = yu.get(i), h = (su.get(i) - mean) * rstd;
+      ag[i] = fmaf(v, h, ag[i]);
+      ab[i] += v;
+      o[i] = rstd * (v * gm[i] - c1 - h * c2);
+      if (RES && ds) o[i] += eu.get(i);
+    }
+    const auto put = [&](auto *p) __attribute__((always_inline)) {
+      using T = std::remove_pointer_t<decltype(p)>;
+      if (all) {
+        Unit<T, E> out;
+#pragma unroll
+        for (int i = 0; i < E; ++i) out.set(i, o[i]);
+        out.store_nt(p);
+      } else {
+#pragma unroll
+        for (int i = 0; i < E; ++i)
+          if (i < n) Elem<T>::store(p + i, o[i]);
+      }
+    };
+    if constexpr (RES) {
+      if (dres) put(dres + row * a.pdr + c0);
+      if (dx && a.drop.rng) drop_unit<E>(d, (uint32_t)c0, (uint32_t)row, o);
+    }
+    if (!RES || dx) put(dx + row * a.pdx + c0);
+  }
+  if (!a.partial) return;
+#pragma unroll
+  for (int i = 0; i < E; ++i)
+    if (i < n) {
+      a.partial[blockIdx.y * 2 * a.C + c0 + i] = ag[i];
+      a.partial[(blockIdx.y * 2 + 1) * a.C + c0 + i] = ab[i];
+    }
+}
+
+// The strips' sums, 2 C columns of them: a block has sixteen columns and 64 threads for each, every 64th strip a thread; the threads' sums are added
+// in their order by halves.
+__global__ __launch_bounds__(1024) void norm_fold_kernel(const float *partial, int strips, int64_t C, float *dgamma, float *dbeta) {
+  __shared__ float part[64][17];
+  const int col = threadIdx.x & 15, slice = threadIdx.x >> 4;
+  const int64_t c = (int64_t)blockIdx.x * 16 + col;
+  float v = 0.0f;
+  if (c < 2 * C) {
+#pragma unroll 4
+    for (int k = slice; k < strips; k += 64) v += partial[k * 2 * C + c];
+  }
+  part[slice][col] = v;
+  __syncthreads();
+  // thread (column, slice) of one wave: sixteen lanes' worth of slices at a time
+  if (threadIdx.x < 256) {
+    const int cc = threadIdx.x >> 4, k = threadIdx.x & 15;
+    const float t = sum16((part[k][cc] + part[k + 16][cc]) + (part[k + 32][cc] + part[k + 48][cc]));
+    const int64_t o = (int64_t)blockIdx.x * 16 + cc;
+    if (k == 0 && o < 2 * C) {
+      if (o < C) {
+        if (dgamma) dgamma[o] = t;
+      } else if (dbeta) {
+        dbeta[o - C] = t;
       }
     }
   }
@@ -164,11 +638,28 @@ chn_status check_matrix(const chn_array *m, const char *name, bool is_output, in
   *N = n;
   *C = c;
   if (n > 0 && c == 0) return fail(CHN_ERR_SHAPE, "norm: %s has rows without elements", name);
+  if (n > 0x7fffffffLL || c > 0x7fffffffLL) return fail(CHN_ERR_SHAPE, "norm: %s has more than 2^31 - 1 rows or columns", name);
   return CHN_OK;
 }
 
 const float *floats(const chn_array *v) { return v ? static_cast<const float *>(v->data) : nullptr; }
 float *floats_out(const chn_array *v) { return v ? static_cast<float *>(v->data) : nullptr; }
+
+template <typename TX, typename TY, typename TS, bool RES>
+void launch_fwd(const TX *x, const TS *residual, TS *s, TY *y, const NormArgs &a, hipStream_t st) {
+  constexpr int E = unit_elements<TX, TY, TS>();
+  const int64_t held = a.C / E * E;                      // (the elements behind the last whole unit come on top)
+#define CHN_ROWS(G, KE)                                                                                                             \
+  hipLaunchKernelGGL((norm_fwd_rows_kernel<TX, TY, TS, RES, G, KE>), dim3((unsigned)((a.N + (G < 256 ? 256 / G : 1) - 1) / (G < 256 ? 256 / G : 1))), \
+                     dim3(G > 256 ? G : 256), 0, st, x, residual, s, y, a)
+  if (held <= 16 * 16) CHN_ROWS(16, 16);
+  else if (held <= 64 * 16) CHN_ROWS(64, 16);
+  else if (held <= 256 * 16) CHN_ROWS(256, 16);
+  else if (held <= 1024 * 16) CHN_ROWS(1024, 16);
+  else if (held <= 1024 * 32) CHN_ROWS(1024, 32);
+  else hipLaunchKernelGGL((norm_fwd_wide_kernel<TX, TY, TS, RES>), dim3((unsigned)a.N), dim3(1024), 0, st, x, residual, s, y, a);
+#undef CHN_ROWS
+}
 
 chn_status norm_fwd(const chn_array *x, const chn_array *residual, double ratio, const chn_array *rng, int64_t site, const chn_array *gamma,
                     const chn_array *beta, double eps, const chn_array *s, const chn_array *y, const chn_array *mean, const chn_array *rstd,
@@ -195,12 +686,10 @@ chn_status norm_fwd(const chn_array *x, const chn_array *residual, double ratio,
   a.beta = floats(beta);
   a.mean = floats_out(mean);
   a.rstd = floats_out(rstd);
-  const dim3 grid((unsigned)(a.N < (1 << 20) ? a.N : (1 << 20)));
   const bool x32 = x->dtype == CHN_F32, y32 = y->dtype == CHN_F32;
-#define CHN_GO(TX, TY, TS, RES)                                                                                                        \
-  hipLaunchKernelGGL((norm_fwd_kernel<TX, TY, TS, RES>), grid, dim3(256), 0, st, static_cast<const TX *>(x->data),                      \
-                     residual ? static_cast<const TS *>(residual->data) : nullptr, s ? static_cast<TS *>(s->data) : nullptr,            \
-                     static_cast<TY *>(y->data), a)
+#define CHN_GO(TX, TY, TS, RES)                                                                                                      \
+  launch_fwd<TX, TY, TS, RES>(static_cast<const TX *>(x->data), residual ? static_cast<const TS *>(residual->data) : nullptr,          \
+                              s ? static_cast<TS *>(s->data) : nullptr, static_cast<TY *>(y->data), a, st)
   if (res) {
     const bool s32 = s->dtype == CHN_F32;
     if (x32 && s32) CHN_GO(float, float, float, true);
@@ -217,7 +706,47 @@ chn_status norm_fwd(const chn_array *x, const chn_array *residual, double ratio,
   return check_launch(what);
 }
 
-int64_t strips_of(int64_t N) { return N < 64 ? (N > 0 ? N : 1) : 64; }
+// What the backward pass leaves in its workspace: strips of column sums, and for rows longer than a block holds the rows' sums behind them.
+constexpr int64_t kHeld = 512 * 16;                      // elements of a row that a block holds
+constexpr int64_t kStrips = 256;                         // one for each compute unit
+int64_t strips_of(int64_t N, int64_t C) {
+  if (C <= kHeld) return N < kStrips ? (N > 0 ? N : 1) : kStrips;
+  // wide rows: at least four rows to a strip, so that their sums stay a fraction of what is read
+  const int64_t n = (N + 3) / 4;
+  return n < 64 ? (n > 0 ? n : 1) : 64;
+}
+int segments_of(int64_t N, int64_t C) {
+  if (C <= kHeld) return 0;
+  const int64_t want = N > 0 ? (1024 + N - 1) / N : 1, most = (C + 4095) / 4096;
+  return (int)(want < most ? want : most);
+}
+size_t bwd_sums_bytes(int64_t N, int64_t C) { return ((size_t)(N * segments_of(N, C)) * sizeof(float2) + 255) / 256 * 256; }
+size_t bwd_workspace(int64_t N, int64_t C) { return bwd_sums_bytes(N, C) + (size_t)(strips_of(N, C) * 2 * C) * sizeof(float); }
+
+template <typename TX, typename TY, typename TS, bool RES, int G, int KE, int THREADS>
+int64_t launch_bwd_rows(const TY *dy, const TS *s, const TS *ds, TS *dres, TX *dx, const NormBwdArgs &a, hipStream_t st) {
+  const int64_t blocks = (a.N + THREADS / G - 1) / (THREADS / G), n = blocks < kStrips ? (blocks > 0 ? blocks : 1) : kStrips;
+  hipLaunchKernelGGL((norm_bwd_rows_kernel<TX, TY, TS, RES, G, KE, THREADS>), dim3((unsigned)n), dim3(THREADS), 0, st, dy, s, ds, dres, dx, a);
+  return n;
+}
+
+// Returns the number of strips it leaves.
+template <typename TX, typename TY, typename TS, bool RES>
+int64_t launch_bwd(const TY *dy, const TS *s, const TS *ds, TS *dres, TX *dx, NormBwdArgs &a, hipStream_t st) {
+  constexpr int E = unit_elements<TX, TY, TS>();
+#define CHN_ROWS(G, KE, THREADS) return launch_bwd_rows<TX, TY, TS, RES, G, KE, THREADS>(dy, s, ds, dres, dx, a, st)
+  if (a.C <= 16 * 16) CHN_ROWS(16, 16, 512);
+  if (a.C <= 64 * 16) CHN_ROWS(64, 16, 512);
+  if (a.C <= 256 * 8) CHN_ROWS(256, 8, 1024);
+  if (a.C <= 512 * 8) CHN_ROWS(512, 8, 1024);
+  if (a.C <= kHeld) CHN_ROWS(512, 16, 512);
+#undef CHN_ROWS
+  if (a.N > 0)
+    hipLaunchKernelGGL((norm_bwd_sums_kernel<TY, TS>), dim3((unsigned)a.N, (unsigned)a.segments), dim3(256), 0, st, dy, s, a);
+  hipLaunchKernelGGL((norm_bwd_wide_kernel<TX, TY, TS, RES>), dim3((unsigned)((a.C + 256 * E - 1) / (256 * E)), (unsigned)a.strips), dim3(256), 0, st,
+                     dy, s, ds, dres, dx, a);
+  return a.strips;
+}
 
 chn_status norm_bwd(const chn_array *dy, const chn_array *ds, const chn_array *s, const chn_array *mean, const chn_array *rstd, const chn_array *gamma,
                     double ratio, const chn_array *rng, int64_t site, const chn_array *dres, const chn_array *dx, const chn_array *dgamma,
@@ -247,31 +776,20 @@ chn_status norm_bwd(const chn_array *dy, const chn_array *ds, const chn_array *s
   a.gamma = floats(gamma);
   a.mean = floats(mean);
   a.rstd = floats(rstd);
-  a.strips = strips_of(a.N);
-  if (dgamma || dbeta) {
-    CHN_TRY(check_ws(ws, ws_bytes, (size_t)(a.strips * 2 * a.C * 4), what));
-    a.partial = static_cast<float *>(ws);
-  }
+  a.strips = strips_of(a.N, a.C);
+  a.segments = segments_of(a.N, a.C);
+  const bool sums = dgamma || dbeta;
+  if (!sums && (a.N == 0 || (!dx && !dres))) return CHN_OK;
+  const size_t rows_bytes = bwd_sums_bytes(a.N, a.C);
+  CHN_TRY(check_ws(ws, ws_bytes, sums ? bwd_workspace(a.N, a.C) : rows_bytes, what));
+  a.sums = static_cast<float2 *>(ws);
+  if (sums) a.partial = reinterpret_cast<float *>(static_cast<char *>(ws) + rows_bytes);
   const bool y32 = dy->dtype == CHN_F32, s32 = s->dtype == CHN_F32;
-  const unsigned cb = (unsigned)((a.C + 255) / 256);
-  if (a.partial) {
-    const dim3 grid(cb, (unsigned)a.strips);
-#define CHN_GO(TY, TS) \
-  hipLaunchKernelGGL((norm_partial_kernel<TY, TS>), grid, dim3(256), 0, st, static_cast<const TY *>(dy->data), static_cast<const TS *>(s->data), a)
-    if (y32 && s32) CHN_GO(float, float);
-    else if (y32) CHN_GO(float, bf16_raw);
-    else if (s32) CHN_GO(bf16_raw, float);
-    else CHN_GO(bf16_raw, bf16_raw);
-#undef CHN_GO
-    hipLaunchKernelGGL(norm_fold_kernel, dim3(cb), dim3(256), 0, st, a.partial, a.strips, a.C, floats_out(dgamma), floats_out(dbeta));
-    CHN_TRY(check_launch(what));
-  }
-  if (a.N == 0 || (!dx && !dres)) return CHN_OK;
-  const dim3 grid((unsigned)(a.N < (1 << 20) ? a.N : (1 << 20)));
-#define CHN_GO(TX, TY, TS, RES)                                                                                                      \
-  hipLaunchKernelGGL((norm_bwd_kernel<TX, TY, TS, RES>), grid, dim3(256), 0, st, static_cast<const TY *>(dy->data),                   \
-                     static_cast<const TS *>(s->data), ds ? static_cast<const TS *>(ds->data) : nullptr,                              \
-                     dres ? static_cast<TS *>(dres->data) : nullptr, dx ? static_cast<TX *>(dx->data) : nullptr, a)
+  int64_t strips = 0;
+#define CHN_GO(TX, TY, TS, RES)                                                                                                     \
+  strips = launch_bwd<TX, TY, TS, RES>(static_cast<const TY *>(dy->data), static_cast<const TS *>(s->data),                          \
+                                       ds ? static_cast<const TS *>(ds->data) : nullptr, dres ? static_cast<TS *>(dres->data) : nullptr, \
+                                       dx ? static_cast<TX *>(dx->data) : nullptr, a, st)
   if (res) {
     if (y32 && s32) CHN_GO(float, float, float, true);
     else if (y32) CHN_GO(float, float, bf16_raw, true);
@@ -284,6 +802,9 @@ chn_status norm_bwd(const chn_array *dy, const chn_array *ds, const chn_array *s
     else CHN_GO(bf16_raw, bf16_raw, bf16_raw, false);
   }
 #undef CHN_GO
+  CHN_TRY(check_launch(what));
+  if (a.partial)
+    hipLaunchKernelGGL(norm_fold_kernel, dim3((unsigned)((2 * a.C + 15) / 16)), dim3(1024), 0, st, a.partial, (int)strips, a.C, floats_out(dgamma), floats_out(dbeta));
   return check_launch(what);
 }
 
@@ -299,7 +820,7 @@ chn_status chn_layer_norm_fwd(const chn_array *x, const chn_array *gamma, const 
 
 size_t chn_layer_norm_bwd_workspace_bytes(const chn_array *x) {
   if (!x || x->ndim != 2 || x->shape[0] < 0 || x->shape[1] < 0) return 0;
-  return (size_t)(chn::strips_of(x->shape[0]) * 2 * x->shape[1] * 4);
+  return chn::bwd_workspace(x->shape[0], x->shape[1]);
 }
 
 chn_status chn_layer_norm_bwd(const chn_array *dy, const chn_array *x, const chn_array *mean, const chn_array *rstd, const chn_array *gamma,

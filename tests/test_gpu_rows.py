@@ -111,9 +111,9 @@ def check_norm(x, tx, ty, gamma, beta, eps=1e-5, pad=0, shift=0, dy=None):
     close(values(dg), wdg, bdg + U * np.abs(wdg), "dgamma")
     close(values(db), wdb, bdb + U * np.abs(wdb), "dbeta")
     assert untouched(dx, pad, shift)
-    # without the weights' gradients: the same dx, no workspace
+    # without the weights' gradients: the same dx, and a workspace for long rows only
     dx2 = matrix(x * 0, tx, pad, shift)
-    B.layer_norm_bwd(dyd, xd, mean, rstd, dx2, opt(gamma))
+    B.layer_norm_bwd(dyd, xd, mean, rstd, dx2, opt(gamma), ws=workspace(xd) if c > 8192 else None)
     assert torch.equal(dx2, dx)
 
 
@@ -210,8 +210,9 @@ def check_residual(shape, tl, ts, ratio, pad=0, shift=0, with_ds=True):
     assert all(untouched(m, pad, shift) for m in (s, y, dres, dx))
     # either gradient by itself
     only, other = new(ts), new(tl)
-    B.residual_norm_bwd(dyd, dsd, s, mean, rstd, only, None, g, **drop)
-    B.residual_norm_bwd(dyd, dsd, s, mean, rstd, None, other, g, **drop)
+    long = workspace(s) if c > 8192 else None
+    B.residual_norm_bwd(dyd, dsd, s, mean, rstd, only, None, g, ws=long, **drop)
+    B.residual_norm_bwd(dyd, dsd, s, mean, rstd, None, other, g, ws=long, **drop)
     assert torch.equal(only, dres) and torch.equal(other, dx)
     # over their inputs
     B.residual_norm_fwd(xd, rd, rd, xd, g, b, 1e-5, None, None, **drop)
