@@ -5,6 +5,11 @@
 //
 // The leading dimensions of the arrays are merged where all of them allow it; what is left are rows with a list of strides.
 #include "philox.h"
+#include "rows.h"
+
+#ifndef CHN_DROP_U
+#define CHN_DROP_U 2
+#endif
 
 namespace chn {
 namespace {
@@ -18,6 +23,63 @@ struct DropShape {
   int64_t sx[kMaxLead], sr[kMaxLead], sy[kMaxLead];   // elements
   int64_t cx, cr, cy;                // strides along the last axis
 };
+
+// Rows of unit stride: a thread takes units of E neighbouring columns, U of them at a time so that their loads are in flight together, at
+// whatever element address they have; the last unit of a row that is not whole goes element by element.  `upr`: units of a row.
+template <typename TX, typename TY, bool RES, int U>
+__global__ __launch_bounds__(256) void dropout_rows_kernel(const TX *x, const TY *residual, TY *y, int64_t rows, int64_t cols, uint32_t upr,
+                                                           int64_t px, int64_t pr, int64_t py, DropArgs a) {
+  constexpr int E = unit_elements<TX, TY>();
+  const DropState d(a);
+  const int64_t total = rows * upr, first = ((int64_t)blockIdx.x * U) * 256 + threadIdx.x;
+  Unit<TX, E> xu[U];
+  Unit<TY, E> ru[U];
+  int64_t row[U];
+  uint32_t c0[U];
+  int n[U];                                              // columns of the unit: E, fewer at a row's end, 0 behind the last row
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const int64_t i = first + u * 256;
+    if (total <= 0xffffffffLL) {
+      row[u] = (uint32_t)i / upr;
+    } else {
+      row[u] = i / upr;
+    }
+    c0[u] = (uint32_t)(i - row[u] * upr);
+    const int64_t left = cols - (int64_t)c0[u] * E;
+    n[u] = i < total ? (left < E ? (int)left : E) : 0;
+    if (n[u] == E) {
+      xu[u].load(x + row[u] * px + (int64_t)c0[u] * E);
+      if constexpr (RES) ru[u].load(residual + row[u] * pr + (int64_t)c0[u] * E);
+    }
+  }
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    if (n[u] == 0) continue;
+    const int64_t c = (int64_t)c0[u] * E;
+    Philox4 w[E / 4];
+#pragma unroll
+    for (int b = 0; b < E / 4; ++b) w[b] = a.rng ? d.words(c0[u] * (E / 4) + b, (uint32_t)row[u]) : Philox4{{~0u, ~0u, ~0u, ~0u}};
+    if (n[u] == E) {
+      Unit<TY, E> out;
+#pragma unroll
+      for (int i = 0; i < E; ++i) {
+        float v = d.apply(xu[u].get(i), w[i / 4].w[i % 4]);
+        if constexpr (RES) v = add_rounded(ru[u].get(i), v);
+        out.set(i, v);
+      }
+      out.store_nt(y + row[u] * py + c);
+    } else {
+#pragma unroll
+      for (int i = 0; i < E; ++i)
+        if (i < n[u]) {
+          float v = d.apply(Elem<TX>::load(x + row[u] * px + c + i), w[i / 4].w[i % 4]);
+          if constexpr (RES) v = add_rounded(Elem<TY>::load(residual + row[u] * pr + c + i), v);
+          Elem<TY>::store(y + row[u] * py + c + i, v);
+        }
+    }
+  }
+}
 
 // One thread per four columns: any strides.
 template <typename TX, typename TY>
@@ -101,9 +163,20 @@ chn_status same_shape(const chn_array *a, const chn_array *x, const char *name) 
 
 template <typename TX, typename TY>
 void launch(const chn_array *x, const chn_array *r, const chn_array *y, const DropShape &s, const DropArgs &a, hipStream_t st) {
-  const int64_t total = s.rows * s.units, want = (total + 255) / 256, most = 1 << 20;
-  hipLaunchKernelGGL((dropout_kernel<TX, TY>), dim3((unsigned)(want < most ? want : most)), dim3(256), 0, st, static_cast<const TX *>(x->data),
-                     r ? static_cast<const TY *>(r->data) : nullptr, static_cast<TY *>(y->data), s, a);
+  const TX *xp = static_cast<const TX *>(x->data);
+  const TY *rp = r ? static_cast<const TY *>(r->data) : nullptr;
+  TY *yp = static_cast<TY *>(y->data);
+  constexpr int E = unit_elements<TX, TY>(), U = CHN_DROP_U;
+  const int64_t upr = (s.cols + E - 1) / E, fast = (s.rows * upr + 256 * U - 1) / (256 * U);
+  // (a row shorter than a unit leaves most of a thread idle either way, and the general kernel takes four columns, not E)
+  if (s.lead <= 1 && s.cx == 1 && s.cy == 1 && (!r || s.cr == 1) && s.cols >= E && fast <= 0x7fffffffLL && upr <= 0xffffffffLL / (E / 4)) {
+    const int64_t px = s.lead ? s.sx[0] : 0, pr = s.lead ? s.sr[0] : 0, py = s.lead ? s.sy[0] : 0;
+    if (r) hipLaunchKernelGGL((dropout_rows_kernel<TX, TY, true, U>), dim3((unsigned)fast), dim3(256), 0, st, xp, rp, yp, s.rows, s.cols, (uint32_t)upr, px, pr, py, a);
+    else hipLaunchKernelGGL((dropout_rows_kernel<TX, TY, false, U>), dim3((unsigned)fast), dim3(256), 0, st, xp, rp, yp, s.rows, s.cols, (uint32_t)upr, px, pr, py, a);
+    return;
+  }
+  const int64_t want = (s.rows * s.units + 255) / 256, most = 1 << 20;
+  hipLaunchKernelGGL((dropout_kernel<TX, TY>), dim3((unsigned)(want < most ? want : most)), dim3(256), 0, st, xp, rp, yp, s, a);
 }
 
 }  // namespace
