@@ -72,37 +72,29 @@ def sample(logits, u, temperature=None, top_k=None, top_p=None, min_p=None):
     logits = np.asarray(logits, np.float64)
     out = []
     for n, z in enumerate(logits):
-        ids = [i for i in range(len(z)) if z[i] > -np.inf]
-        if not ids:
+        ids = np.nonzero(z > -np.inf)[0]
+        if len(ids) == 0:
             out.append(-1)
             continue
-        best = max(z[i] for i in ids)
+        best = z[ids].max()
         t = 1.0 if temperature is None else float(temperature[n])
         if not t > 0:
-            out.append(next(i for i in ids if z[i] == best))
+            out.append(ids[z[ids] == best][0])
             continue
         with np.errstate(all="ignore"):
-            w = {i: 1.0 if z[i] == best else float(np.exp((z[i] - best) / t)) for i in ids}
-        order = sorted(ids, key=lambda i: (-z[i], i))
+            w = np.where(z == best, 1.0, np.exp((z - best) / t))
+        order = ids[np.lexsort((ids, -z[ids]))]                  # descending logits, equals by index
         if top_k is not None and top_k[n] > 0:
             order = order[:int(top_k[n])]
         if top_p is not None and float(top_p[n]) < 1:
-            whole, before, cut = sum(w[i] for i in order), 0.0, []
-            for i in order:
-                if cut and not before < float(top_p[n]) * whole:
-                    break
-                cut.append(i)
-                before += w[i]
-            order = cut
+            before = np.concatenate([[0.0], np.cumsum(w[order])])
+            keep = before[:-1] < float(top_p[n]) * before[-1]
+            keep[0] = True
+            order = order[keep]
         if min_p is not None and float(min_p[n]) > 0:
-            order = [i for i in order if w[i] >= min(float(min_p[n]), 1.0)]
-        whole, run, token = sum(w[i] for i in sorted(order)), 0.0, None
-        kept = [i for i in sorted(order) if w[i] > 0]
-        un = float(u[n])
-        for i in kept:
-            run += w[i]
-            if not un > 0 or run > un * whole:
-                token = i
-                break
-        out.append(kept[-1] if token is None else token)
+            order = order[w[order] >= min(float(min_p[n]), 1.0)]
+        kept = np.sort(order[w[order] > 0])
+        run, un = np.cumsum(w[kept]), float(u[n])
+        hit = np.nonzero(run > un * run[-1])[0] if un > 0 else np.array([0])
+        out.append(kept[hit[0]] if len(hit) else kept[-1])
     return np.array(out, np.int64)

@@ -75,6 +75,18 @@ __device__ __forceinline__ float sum64(float v) {
   return (a + b) + (c + d);
 }
 
+// The largest over the wave, uniform.
+template <int CTRL>
+__device__ __forceinline__ float dpp_max(float v) {
+  return fmaxf(v, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, true)));
+}
+__device__ __forceinline__ float max64(float v) {
+  v = dpp_max<0x140>(dpp_max<0x141>(dpp_max<0x4E>(dpp_max<0xB1>(v))));
+  const float a = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 0)), b = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 16));
+  const float c = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 32)), d = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 48));
+  return fmaxf(fmaxf(a, b), fmaxf(c, d));
+}
+
 // Sums of two values over the G lanes of a row, in all of them.  smem: the group's 2 x G / 64 pairs for G > 64; `turn` alternates from call to
 // call, so that one barrier is enough: what is overwritten was read before the barrier of the call in between.
 template <int G>

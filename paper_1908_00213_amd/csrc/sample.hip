@@ -8,12 +8,30 @@
 // border: the tokens from some number on are kept.  A border is found without sorting the row: sums (top-p) or counts (top-k) in 2048 bins of
 // equal width in the logit, the bin that the border lies in, and the few tokens of that bin in their exact order.  Where top-k or
 // min-p leaves only a few tokens anyway, these are gathered first and the rest of the row is never looked at again: the k-th largest of
-// the threads' maxima is a bound that at least k tokens reach.
+// the maxima of parts of the row is a bound that at least k tokens reach.
+//
+// A row is the work of one block of 1024 threads.  Few long rows are cut in chunks, in four launches that exchange through the workspace:
+// maxima of all parts; bins, candidates or sums; the bin of the border and the sums above it; the draw (see the rule at chunks_of).
 #include "common.h"
 #include "rows.h"
 
 namespace chn {
 namespace {
+
+typedef unsigned long long u64;
+constexpr int kThreads = 1024, kWaves = kThreads / 64;
+constexpr int kBins = 2048;          // two for each thread
+constexpr int kSmall = 1024;         // tokens that are ordered by comparing each with each
+constexpr int kMaxChunks = 32, kMaxParts = 4096;
+
+// What the launches over chunks leave for each other, of one row.
+struct RowSpace {
+  u64 bins[kBins];                   // sums by bin
+  u64 list[kSmall];                  // tokens of the border's bin
+  u64 sums[kMaxChunks];              // kept weights of each chunk
+  float maxima[kMaxParts];           // of parts of 64 units; the tokens behind the last unit count to the last part
+  int count, pad[63];
+};
 
 struct SampleArgs {
   int64_t N, pitch;
@@ -24,12 +42,9 @@ struct SampleArgs {
   int k64;
   void *out;
   int out64;
+  RowSpace *space;
+  int chunks, chunk_units, parts;    // chunks are whole parts
 };
-
-typedef unsigned long long u64;
-constexpr int kThreads = 1024, kWaves = kThreads / 64;
-constexpr int kBins = 2048;          // two for each thread
-constexpr int kSmall = 1024;         // tokens that are ordered by comparing each with each
 
 // Monotone in the logit, -0 and 0 alike.  0: not a token that can be drawn (-inf, NaN).
 __device__ __forceinline__ uint32_t key_of(float z) {
@@ -47,33 +62,102 @@ __device__ __forceinline__ Rank rank_of(float z, uint32_t index) {
 }
 __device__ __forceinline__ uint32_t index_of(Rank r) { return 0xffffffffu - (uint32_t)r; }
 
+// 2^(-j / 32)
+__constant__ const double kPowers[32] = {
+    0x1.0000000000000p+0, 0x1.f50765b6e4540p-1, 0x1.ea4afa2a490dap-1, 0x1.dfc97337b9b5fp-1, 0x1.d5818dcfba487p-1, 0x1.cb720dcef9069p-1,
+    0x1.c199bdd85529cp-1, 0x1.b7f76f2fb5e47p-1, 0x1.ae89f995ad3adp-1, 0x1.a5503b23e255dp-1, 0x1.9c49182a3f090p-1, 0x1.93737b0cdc5e5p-1,
+    0x1.8ace5422aa0dbp-1, 0x1.82589994cce13p-1, 0x1.7a11473eb0187p-1, 0x1.71f75e8ec5f74p-1, 0x1.6a09e667f3bcdp-1, 0x1.6247eb03a5585p-1,
+    0x1.5ab07dd485429p-1, 0x1.5342b569d4f82p-1, 0x1.4bfdad5362a27p-1, 0x1.44e086061892dp-1, 0x1.3dea64c123422p-1, 0x1.371a7373aa9cbp-1,
+    0x1.306fe0a31b715p-1, 0x1.29e9df51fdee1p-1, 0x1.2387a6e756238p-1, 0x1.1d4873168b9aap-1, 0x1.172b83c7d517bp-1, 0x1.11301d0125b51p-1,
+    0x1.0b5586cf9890fp-1, 0x1.059b0d3158574p-1};
+
+struct Shared {
+  u64 bins[kBins];
+  u64 sorted[kSmall];                // the small set in descending order
+  u64 weight[kSmall];
+  u64 list[kSmall];                  // the small set as it was gathered
+  u64 waves[kWaves];
+  double powers[32];                 // kPowers: 64 banks' worth, no two lanes meet in one unless they read the same number
+  float fmax[kWaves], fmin[kWaves], part[kThreads];
+  u64 result, above;
+  int count, slot;
+};
+
 // exp((z - best) / t) and the weight it stands for.
+//
+// exp = 2^(-y / 32), y = 32 (best - z) / (t ln 2): with n the whole number next to y, 2^((n - y) / 32) by a polynomial of degree four through the Chebyshev
+// nodes (relative error below 2e-13), the low five bits of n by a table and the others taken off the exponent.  To tell a token from its
+// neighbour by the same u takes an error of about a token's share of the sum, which is 1e-6 of it at the least.
 struct Weights {
   float best;
-  double c, magic;
-  __device__ __forceinline__ Weights(float best_, float t, int shift) : best(best_) {
-    c = 1.4426950408889634074 / (double)t;
-    magic = __longlong_as_double((long long)(1023 + 52 - shift) << 52);   // adding it leaves a whole number of 2^-shift in the low bits
+  double c;                          // 32 / (t ln 2)
+  double magic;                      // adding it leaves a whole number of 2^-shift in the low bits
+  const double *powers;
+  __device__ __forceinline__ Weights(float best_, float t, int shift, const Shared &sh) : best(best_), powers(sh.powers) {
+    c = 46.166241308446828384 / (double)t;
+    magic = __longlong_as_double((long long)(1023 + 52 - shift) << 52);
   }
-  // 2^-y, y = (best - z) c: 2^f, |f| <= 1/2, by a polynomial through the Chebyshev nodes of degree nine (relative error below 4e-14) and
-  // the exponent.  To tell a token from its neighbour by the same u takes an error of about a token's share, which is 1e-6 at the least.
+  __device__ __forceinline__ double distance(float z) const { return ((double)best - (double)z) * c; }
+  // For every number below `best` and best itself.
   __device__ __forceinline__ double exponential(float z) const {
     if (z == best) return 1.0;
-    const double y = fmin(((double)best - (double)z) * c, 1100.0);        // (infinities and NaN: 1100)
-    const double n = rint(y), f = n - y;
-    double p = 0x1.b63880a30e9ffp-24;
-    p = fma(p, f, 0x1.63d136366db24p-20);
-    p = fma(p, f, 0x1.ffcb9515a8016p-17);
-    p = fma(p, f, 0x1.4308ac85aa947p-13);
-    p = fma(p, f, 0x1.5d87fe86fe88ep-10);
-    p = fma(p, f, 0x1.3b2ab7181b755p-7);
-    p = fma(p, f, 0x1.c6b08d7047e52p-5);
-    p = fma(p, f, 0x1.ebfbdff823cedp-3);
-    p = fma(p, f, 0x1.62e42fefa39efp-1);
-    return ldexp(fma(p, f, 1.0), -(int)n);
+    return exp2(distance(z) * -0.03125);
   }
-  __device__ __forceinline__ u64 of(double e) const { return (u64)(__double_as_longlong(e + magic) - __double_as_longlong(magic)); }
+  // From here on weights are not zero, and what lies above is near enough for `near`.  (Sixty octaves below the largest logit, rounded to a
+  // number of its kind; the lowest finite one at the least.)
+  __device__ __forceinline__ float zero(float t) const { return fmaxf((float)((double)best - 41.6 * (double)t), -3.4028234663852886e38f); }
+  // For logits whose distance is below 32 * 1000; any number for others.  y + 1.5 2^52 has the whole number next to y in its low word: no
+  // rounding, conversion or ldexp.
+  __device__ __forceinline__ double near(float z) const {
+    const double dz = (double)best - (double)z, rough = fma(dz, c, 0x1.8p52), n = rough - 0x1.8p52, r = fma(-dz, c, n);
+    const int m = __double2loint(rough);
+    double q = fma(0x1.3b2b07bdf358dp-27, r, 0x1.c6b13c3465457p-20);
+    q = fma(q, r, 0x1.ebfbdff82240ap-13);
+    q = fma(q, r, 0x1.62e42fef8dc67p-6);
+    const double p = powers[m & 31], e = fma(p, q * r, p);
+    return __hiloint2double(__double2hiint(e) - ((m & ~31) << 15), __double2loint(e));
+  }
+  __device__ __forceinline__ u64 of(double e) const { return (u64)__double_as_longlong(e + magic) & 0xfffffffffffffull; }
 };
+
+// Tokens that are kept: logits above `z`, and of those equal to it the ones before index `end`.
+struct Limit {
+  float z;
+  uint32_t end;
+  __device__ __forceinline__ bool keeps(float v, uint32_t i) const { return v > z || (v == z && i < end); }
+  __device__ __forceinline__ void not_below(float least) {
+    if (least > z) {
+      z = least;
+      end = 0xffffffffu;
+    }
+  }
+};
+
+// The smallest logit whose exponential is at least m, 0 < m <= 1: near the logarithm's, 64 of them tried at once, or by search, 64 at a time.
+__device__ __forceinline__ float least_logit(const Weights &wt, float t, float m) {
+  const uint32_t lane = threadIdx.x & 63, low = 0x00800000u, high = key_of(wt.best);   // (from the lowest finite number on)
+  const uint32_t guess = key_of(fmaxf((float)((double)wt.best + (double)t * (double)logf(m)), -3.4028234663852886e38f));
+  uint32_t a = guess - low > 31 ? guess - 31 : low, b = high;
+  const uint32_t mine = b - a < lane ? b : a + lane;
+  const u64 hit = __ballot(wt.exponential(logit_of(mine)) >= (double)m);
+  const int first = __ffsll((long long)hit) - 1;
+  if (first > 0) return logit_of(b - a < (uint32_t)first ? b : a + first);
+  a = low;
+  while (a < b) {
+    const uint32_t step = (b - a + 63) / 64, at = b - a < lane * (u64)step ? b : a + lane * step;
+    const int f = __ffsll((long long)__ballot(wt.exponential(logit_of(at)) >= (double)m)) - 1;    // the first lane for which it holds
+    if (f == 0) {
+      b = a;
+    } else if (f < 0) {
+      a += 63 * step + 1;
+    } else {
+      const uint32_t to = b - a < f * (u64)step ? b : a + f * step;
+      a += (f - 1) * step + 1;
+      b = to;
+    }
+  }
+  return logit_of(b);
+}
 
 __device__ __forceinline__ u64 wave_sum_u64(u64 v) {
 #pragma unroll
@@ -90,17 +174,6 @@ __device__ __forceinline__ u64 wave_upto_u64(u64 v) {
   }
   return v;
 }
-
-struct Shared {
-  u64 bins[kBins];
-  u64 sorted[kSmall];                // the small set in descending order
-  u64 weight[kSmall];
-  u64 list[kSmall];                  // the small set as it was gathered
-  u64 waves[kWaves];
-  float fmax[kWaves], fmin[kWaves];
-  u64 result, above;
-  int count, slot;
-};
 
 // Sum over the threads before this one; *all: over all of them.
 __device__ __forceinline__ u64 block_before_u64(u64 v, Shared &sh, u64 *all) {
@@ -119,42 +192,55 @@ __device__ __forceinline__ u64 block_before_u64(u64 v, Shared &sh, u64 *all) {
   return before;
 }
 
-// A row as the block walks over it: every wave has a stretch of neighbouring tokens, in units of whole 16-byte pieces; the last wave has those
-// behind the last whole unit too.
+// What a block walks over: a row or a chunk of it.  Every wave has a stretch of neighbouring tokens, in units of whole 16-byte pieces; the
+// last wave has those behind the row's last whole unit too, where they belong to the block.
 template <typename T>
-struct Row {
+struct Span {
   static constexpr int E = unit_elements<T>();
   const T *z;
-  int V, whole, first, end;          // units of this wave
-  __device__ __forceinline__ Row(const T *z_, int V_) : z(z_), V(V_) {
-    whole = V / E;
-    const int per = (whole + kWaves - 1) / kWaves, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    first = min(whole, wave * per);
-    end = min(whole, first + per);
+  int V, whole, from, to;            // units of the block
+  bool tail;
+  int per, first, end;               // units of a wave; this wave's
+  // (to_ > whole: to the end of the row)
+  __device__ __forceinline__ Span(const T *z_, int V_, int from_, int to_) : z(z_), V(V_), whole(V_ / E) {
+    from = min(from_, whole);
+    to = max(from, min(to_, whole));
+    tail = to_ > whole;
+    per = (to - from + kWaves - 1) / kWaves;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    first = min(to, from + wave * per);
+    end = min(to, first + per);
   }
-  // U units are loaded together
-  template <int U = 8 / E, typename F>
-  __device__ __forceinline__ void stretch(int from, int to, F f) const {
-    for (int u = from + (threadIdx.x & 63); u < to; u += 64 * U) {
-      Unit<T, E> t[U];
+  // U units are on their way while one is worked on.  (Where one unit ends and the next begins is fixed: work on several mixed up by the
+  // compiler takes more registers than there are.)
+  template <int U, typename F>
+  __device__ __forceinline__ void stretch(int u0, int u1, F f) const {
+    Unit<T, E> t[U];
+    int u = u0 + (int)(threadIdx.x & 63);
 #pragma unroll
-      for (int j = 0; j < U; ++j)
-        if (u + 64 * j < to) t[j].load(z + (u + 64 * j) * E);
+    for (int j = 0; j < U; ++j)
+      if (u + 64 * j < u1) t[j].load(z + (u + 64 * j) * E);
+    for (; u - (int)(threadIdx.x & 63) < u1; u += 64 * U) {
 #pragma unroll
-      for (int j = 0; j < U; ++j)
-        if (u + 64 * j < to) {
+      for (int j = 0; j < U; ++j) {
+        const int at = u + 64 * j;
+        __builtin_amdgcn_sched_barrier(0);
+        if (at < u1) {
+          const Unit<T, E> now = t[j];
+          if (at + 64 * U < u1) t[j].load(z + (at + 64 * U) * E);
 #pragma unroll
-          for (int i = 0; i < E; ++i) f(t[j].get(i), (uint32_t)((u + 64 * j) * E + i));
+          for (int i = 0; i < E; ++i) f(now.get(i), (uint32_t)(at * E + i));
         }
+      }
     }
   }
   template <typename F>
   __device__ __forceinline__ void behind(F f) const {
     const int i = whole * E + (int)(threadIdx.x & 63);
-    if ((threadIdx.x >> 6) == kWaves - 1 && i < V) f(Elem<T>::load(z + i), (uint32_t)i);
+    if (tail && (threadIdx.x >> 6) == kWaves - 1 && i < V) f(Elem<T>::load(z + i), (uint32_t)i);
   }
-  // f(logit, index) for every token of the row, by some thread
-  template <int U = 8 / E, typename F>
+  // f(logit, index) for every token of the block, by some thread
+  template <int U = 4, typename F>
   __device__ __forceinline__ void each(F f) const {
     stretch<U>(first, end, f);
     behind(f);
@@ -164,6 +250,9 @@ struct Row {
 // Bins of equal width below the largest logit.
 struct Bins {
   float best, scale;
+  __device__ __forceinline__ Bins(float best_, float width) : best(best_), scale((float)kBins / width) {
+    if (!(scale < INFINITY)) scale = 0.0f;               // (all in the first bin)
+  }
   __device__ __forceinline__ int of(float z) const { return z == best ? 0 : (int)fminf((best - z) * scale, (float)(kBins - 1)); }   // (NaN: the last)
 };
 
@@ -219,10 +308,22 @@ __device__ __forceinline__ void sort_small(Shared &sh, int M) {
   __syncthreads();
 }
 
-// The rank from which on the sum of W over the row's tokens of at least `border` reaches the target, and the sum before it in sh.above.
-// W(logit): a token's share.
+// The rank in sh.list[0 .. M), none below the border, from which on the sum of W reaches the target; `before`: the sum over the tokens above all of these.
+template <typename FW>
+__device__ __forceinline__ Rank border_in_list(Shared &sh, int M, u64 before, u64 target, FW W) {
+  sort_small(sh, M);
+  const Rank r = (int)threadIdx.x < M ? sh.sorted[threadIdx.x] : 0;
+  const u64 w = r ? W(logit_of((uint32_t)(r >> 32))) : 0;
+  u64 all;
+  const u64 upto = before + block_before_u64(w, sh, &all);
+  if (r && upto < target && target <= upto + w) sh.result = r;
+  __syncthreads();
+  return sh.result;
+}
+
+// The rank from which on the sum of W over the row's tokens of at least `border` reaches the target.  W(logit): a token's share.
 template <typename R, typename FW>
-__device__ Rank find_border(const R &row, Shared &sh, const Bins &bins, Rank border, u64 target, FW W) {
+__device__ __forceinline__ Rank find_border(const R &row, Shared &sh, const Bins &bins, Rank border, u64 target, FW W) {
   // (sh.bins holds the sums by bin)
   const int bin = crossing_bin(sh, target);
   const u64 before = sh.above;
@@ -234,26 +335,14 @@ __device__ Rank find_border(const R &row, Shared &sh, const Bins &bins, Rank bor
   });
   __syncthreads();
   const int M = sh.count;
-  if (M <= kSmall) {
-    sort_small(sh, M);
-    const Rank r = (int)threadIdx.x < M ? sh.sorted[threadIdx.x] : 0;
-    const u64 w = r ? W(logit_of((uint32_t)(r >> 32))) : 0;
-    u64 all;
-    const u64 upto = before + block_before_u64(w, sh, &all);
-    if (r && upto < target && target <= upto + w) {
-      sh.result = r;
-      sh.above = upto;
-    }
-    __syncthreads();
-    return sh.result;
-  }
+  if (M <= kSmall) return border_in_list(sh, M, before, target, W);
   // More than that in one bin (many equal logits): the rank's bits, eleven at a time, over the tokens that share the bits found so far.
   Rank found = 0;
   u64 sum = before;
   for (int low = 53; ; low = low > 11 ? low - 11 : 0) {
     const int width = low == 0 ? 9 : 11, high = low + width;
     clear_bins(sh);
-    row.each([&](float z, uint32_t i) {
+    row.template each<1>([&](float z, uint32_t i) {
       if (bins.of(z) != bin) return;
       const Rank r = rank_of(z, i);
       if (r == 0 || r < border || (high < 64 && (r >> high) != (found >> high))) return;
@@ -269,229 +358,43 @@ __device__ Rank find_border(const R &row, Shared &sh, const Bins &bins, Rank bor
     __syncthreads();
     if (low == 0) break;
   }
-  if (threadIdx.x == 0) sh.above = sum;
-  __syncthreads();
   return found;
 }
 
-template <typename T>
-__global__ __launch_bounds__(kThreads) void sample_kernel(const T *logits, SampleArgs a) {
-  __shared__ Shared sh;
-  const int64_t n = blockIdx.x;
-  const Row<T> row(logits + n * a.pitch, a.V);
+// The token of a span at which the running sum of W, which is `start` before the span, passes point(its sum over the span): the wave in whose
+// stretch that is, the sixteenth of this stretch, the token.
+template <int U, typename T, typename FT, typename FW, typename FP>
+__device__ __forceinline__ void locate(const Span<T> &span, Shared &sh, u64 start, FT point, FW W, FP put) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const auto put = [&](int64_t token) {
-    if (a.out64) static_cast<int64_t *>(a.out)[n] = token;
-    else static_cast<int32_t *>(a.out)[n] = (int32_t)token;
-  };
-  // the largest logit, the threads' own, and the smallest of those
-  float mine = -INFINITY;
-  row.template each<4>([&](float z, uint32_t) { mine = fmaxf(mine, z); });
-  const float wmax = wave_max(mine), wmin = -wave_max(mine > -INFINITY ? -mine : -INFINITY);
-  if (lane == 0) {
-    sh.fmax[wave] = wmax;
-    sh.fmin[wave] = wmin;
-  }
-  clear_bins(sh);
-  float best = sh.fmax[0], low = sh.fmin[0];
-#pragma unroll
-  for (int w = 1; w < kWaves; ++w) {
-    best = fmaxf(best, sh.fmax[w]);
-    low = fminf(low, sh.fmin[w]);
-  }
-  if (best == -INFINITY) {                               // nothing to choose from
-    if (threadIdx.x == 0) put(-1);
-    return;
-  }
-  const float t = a.temperature ? a.temperature[n * a.st] : 1.0f;
-  const float u = a.u[n * a.su];
-  int64_t k = 0;
-  if (a.top_k) k = a.k64 ? static_cast<const int64_t *>(a.top_k)[n * a.sk] : static_cast<const int32_t *>(a.top_k)[n * a.sk];
-  const float p = a.top_p ? a.top_p[n * a.sp] : 1.0f;
-  const float m0 = a.min_p ? a.min_p[n * a.sm] : 0.0f, minp = m0 > 0.0f ? fminf(m0, 1.0f) : 0.0f;
-  const bool greedy = !(t > 0.0f);
-  const Weights wt(best, greedy ? 1.0f : t, a.shift);
-  if (greedy) {
-    if (threadIdx.x == 0) sh.slot = a.V;
-    __syncthreads();
-    row.each([&](float z, uint32_t i) {
-      if (z == best) atomicMin(&sh.slot, (int)i);
-    });
-    __syncthreads();
-    if (threadIdx.x == 0) put(sh.slot);
-    return;
-  }
-  // ---- a row that comes down to a few tokens: all of them from a bound on
-  int M = kSmall + 1;
-  Bins few{best, 0.0f};
-  int last = -1;                                         // tokens in bins up to this one are the few
-  if (k > 0 && k <= kThreads) {
-    few.scale = (float)kBins / (best - low);             // (infinite or NaN where all maxima are equal: they fall in the first bin)
-    if (!(few.scale < INFINITY)) few.scale = 0.0f;
-    if (mine > -INFINITY) atomicAdd(&sh.bins[few.of(mine)], 1ull);
-    __syncthreads();
-    const u64 x = sh.bins[2 * threadIdx.x], y = sh.bins[2 * threadIdx.x + 1];
-    u64 all;
-    const u64 before = block_before_u64(x + y, sh, &all);
-    if (threadIdx.x == 0) sh.slot = -1;
-    __syncthreads();
-    if (before < (u64)k && (u64)k <= before + x + y) sh.slot = 2 * threadIdx.x + ((u64)k > before + x ? 1 : 0);
-    __syncthreads();
-    last = sh.slot;                                      // (-1: fewer threads than k hold a token)
-  }
-  if (last >= 0) {
-    row.each([&](float z, uint32_t i) {
-      if (z > -INFINITY && few.of(z) <= last) gather(sh, rank_of(z, i));
-    });
-    __syncthreads();
-    M = sh.count;
-  } else if (k <= 0 && !(p < 1.0f) && minp > 0.0f) {
-    row.each([&](float z, uint32_t i) {
-      if (wt.exponential(z) >= (double)minp) gather(sh, rank_of(z, i));
-    });
-    __syncthreads();
-    M = sh.count;
-  }
-  if (M <= kSmall) {
-    sort_small(sh, M);
-    const Rank r = (int)threadIdx.x < M && !(k > 0 && (int64_t)threadIdx.x >= k) ? sh.sorted[threadIdx.x] : 0;
-    const double e = r ? wt.exponential(logit_of((uint32_t)(r >> 32))) : 0.0;
-    const u64 w = wt.of(e);
-    bool kept = r != 0;
-    if (p < 1.0f) {
-      u64 all;
-      const u64 before = block_before_u64(w, sh, &all);
-      const u64 target = p > 0.0f ? (u64)ceil((double)p * (double)all) : 1;
-      kept = kept && (before < target || threadIdx.x == 0);
-    }
-    kept = kept && e >= (double)minp;
-    if (u > 0.0f && u < 1.0f) {
-      u64 all;
-      block_before_u64(kept ? w : 0, sh, &all);
-      const u64 target = (u64)((double)u * (double)all);
-      if ((int)threadIdx.x < M) {
-        sh.list[threadIdx.x] = r;
-        sh.weight[threadIdx.x] = kept ? w : 0;
-      }
-      __syncthreads();
-      // running sums in the order of indices, by comparing each with each
-      int size = 1;
-      while (size < M) size <<= 1;
-      const int parts = min(64, kThreads / size), me = (int)threadIdx.x / parts, part = (int)threadIdx.x % parts;
-      const uint32_t index = me < M ? index_of(sh.list[me]) : 0;
-      u64 before = 0;
-      if (me < M)
-        for (int j = part; j < M; j += parts)
-          if (index_of(sh.list[j]) < index) before += sh.weight[j];
-      for (int o = 1; o < parts; o <<= 1) before += __shfl_xor(before, o, 64);
-      if (me < M && part == 0 && before <= target && target < before + sh.weight[me]) put(index);
-    } else {
-      if (threadIdx.x == 0) sh.slot = u >= 1.0f ? -1 : a.V;
-      __syncthreads();
-      if (kept && e > 0.0) {
-        if (u >= 1.0f) atomicMax(&sh.slot, (int)index_of(r));
-        else atomicMin(&sh.slot, (int)index_of(r));
-      }
-      __syncthreads();
-      if (threadIdx.x == 0) put(sh.slot);
-    }
-    return;
-  }
-  // ---- the whole row
-  Rank border = 1;
-  if (k > 0) {
-    float least = INFINITY;
-    int have = 0;
-    row.each([&](float z, uint32_t) {
-      if (z > -INFINITY) {
-        least = fminf(least, z);
-        ++have;
-      }
-    });
-    u64 all;
-    block_before_u64((u64)have, sh, &all);
-    if ((u64)k < all) {
-      least = -wave_max(-least);
-      if (lane == 0) sh.fmin[wave] = least;
-      clear_bins(sh);
-#pragma unroll
-      for (int w = 0; w < kWaves; ++w) least = fminf(least, sh.fmin[w]);
-      Bins bins{best, (float)kBins / (best - least)};
-      if (!(bins.scale < INFINITY)) bins.scale = 0.0f;
-      row.each([&](float z, uint32_t) {
-        if (z > -INFINITY) add_to_bin(sh, bins.of(z), z, 1);
-      });
-      __syncthreads();
-      border = find_border(row, sh, bins, 1, (u64)k, [](float) -> u64 { return 1; });
-    }
-  }
-  if (p < 1.0f) {
-    // (from 33 temperatures below the largest logit on, weights are zero)
-    Bins bins{best, (float)kBins / (33.0f * t)};
-    if (!(bins.scale < INFINITY)) bins.scale = 0.0f;
-    clear_bins(sh);
-    row.each([&](float z, uint32_t i) {
-      if (z > -INFINITY && (border <= 1 || rank_of(z, i) >= border)) add_to_bin(sh, bins.of(z), z, wt.of(wt.exponential(z)));
-    });
-    __syncthreads();
-    u64 all;
-    block_before_u64(sh.bins[2 * threadIdx.x] + sh.bins[2 * threadIdx.x + 1], sh, &all);
-    u64 target = p > 0.0f ? (u64)ceil((double)p * (double)all) : 1;
-    if (target < 1) target = 1;
-    __syncthreads();
-    border = find_border(row, sh, bins, border, target, [&](float z) -> u64 { return wt.of(wt.exponential(z)); });
-  }
-  const auto kept = [&](float z, uint32_t i) -> double {
-    const Rank r = rank_of(z, i);
-    if (r == 0 || r < border) return 0.0;
-    const double e = wt.exponential(z);
-    return e >= (double)minp ? e : 0.0;
-  };
-  if (!(u > 0.0f) || u >= 1.0f) {                        // the ends of the range: the first and the last token, however light
-    __syncthreads();
-    if (threadIdx.x == 0) sh.slot = u >= 1.0f ? -1 : a.V;
-    __syncthreads();
-    row.each([&](float z, uint32_t i) {
-      if (kept(z, i) > 0.0) {
-        if (u >= 1.0f) atomicMax(&sh.slot, (int)i);
-        else atomicMin(&sh.slot, (int)i);
-      }
-    });
-    __syncthreads();
-    if (threadIdx.x == 0) put(sh.slot);
-    return;
-  }
-  // the wave in whose stretch the running sum passes the target, then the sixteenth of that stretch, then the token
-  u64 sum = 0;
-  row.each([&](float z, uint32_t i) { sum += wt.of(kept(z, i)); });
+  u64 sum = 0, all;
+  span.template each<U>([&](float z, uint32_t i) { sum += W(z, i); });
   sum = wave_sum_u64(sum);
-  u64 all;
-  u64 before = block_before_u64(lane == 0 ? sum : 0, sh, &all);
-  const u64 target = (u64)((double)u * (double)all);     // below `all`: u is at most 1 - 2^-24
+  u64 before = start + block_before_u64(lane == 0 ? sum : 0, sh, &all);
+  const u64 target = point(all);
   if (lane == 0 && before <= target && target < before + sum) {
     sh.slot = wave;
     sh.result = before;
   }
   __syncthreads();
-  const int per = (row.whole + kWaves - 1) / kWaves, s0 = min(row.whole, sh.slot * per), s1 = min(row.whole, s0 + per);
-  const bool tail = sh.slot == kWaves - 1;
-  const u64 start = sh.result;
+  const int s0 = min(span.to, span.from + sh.slot * span.per), s1 = min(span.to, s0 + span.per);
+  const bool tail = span.tail && sh.slot == kWaves - 1;
+  const u64 from = sh.result;
   const int sub = (s1 - s0 + kWaves - 1) / kWaves, t0 = min(s1, s0 + wave * sub), t1 = min(s1, t0 + sub);
   sum = 0;
-  row.stretch(t0, t1, [&](float z, uint32_t i) { sum += wt.of(kept(z, i)); });
-  if (tail) row.behind([&](float z, uint32_t i) { sum += wt.of(kept(z, i)); });
+  span.template stretch<1>(t0, t1, [&](float z, uint32_t i) { sum += W(z, i); });
+  if (tail) span.behind([&](float z, uint32_t i) { sum += W(z, i); });
   sum = wave_sum_u64(sum);
-  before = start + block_before_u64(lane == 0 ? sum : 0, sh, &all);
+  before = from + block_before_u64(lane == 0 ? sum : 0, sh, &all);
   before = __shfl(before, 0, 64);
   if (!(before <= target && target < before + sum)) return;
   // one wave: its units in order, 64 at a time, then the tokens behind the last unit
-  constexpr int E = Row<T>::E;
+  constexpr int E = Span<T>::E;
   for (int u0 = t0; u0 < t1; u0 += 64) {
     const int unit = u0 + lane;
     u64 w[E], own = 0;
 #pragma unroll
     for (int i = 0; i < E; ++i) {
-      w[i] = unit < t1 ? wt.of(kept(Elem<T>::load(row.z + unit * E + i), (uint32_t)(unit * E + i))) : 0;
+      w[i] = unit < t1 ? W(Elem<T>::load(span.z + unit * E + i), (uint32_t)(unit * E + i)) : 0;
       own += w[i];
     }
     const u64 upto = wave_upto_u64(own);
@@ -506,11 +409,561 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(const T *logits, Sampl
     before += __shfl(upto, 63, 64);
   }
   if (tail && wave == kWaves - 1) {
-    const int i = row.whole * E + lane;
-    const u64 w = i < a.V ? wt.of(kept(Elem<T>::load(row.z + i), (uint32_t)i)) : 0;
+    const int i = span.whole * E + lane;
+    const u64 w = i < span.V ? W(Elem<T>::load(span.z + i), (uint32_t)i) : 0;
     const u64 at = before + wave_upto_u64(w) - w;
     if (at <= target && target < at + w) put(i);
   }
+}
+
+// What the caller asks of a row.
+struct Asked {
+  float t, u, p, minp;
+  int64_t k;
+  __device__ __forceinline__ Asked(const SampleArgs &a, int64_t n) {
+    t = a.temperature ? a.temperature[n * a.st] : 1.0f;
+    u = a.u[n * a.su];
+    p = a.top_p ? a.top_p[n * a.sp] : 1.0f;
+    const float m = a.min_p ? a.min_p[n * a.sm] : 0.0f;
+    minp = m > 0.0f ? fminf(m, 1.0f) : 0.0f;
+    k = 0;
+    if (a.top_k) k = a.k64 ? static_cast<const int64_t *>(a.top_k)[n * a.sk] : static_cast<const int32_t *>(a.top_k)[n * a.sk];
+  }
+  __device__ __forceinline__ bool greedy() const { return !(t > 0.0f); }
+  __device__ __forceinline__ bool inside() const { return u > 0.0f && u < 1.0f; }
+  // up to where the weights of the kept tokens have to sum, of `all`
+  __device__ __forceinline__ u64 share(u64 all) const {
+    const u64 target = p > 0.0f ? (u64)ceil((double)p * (double)all) : 1;
+    return target < 1 ? 1 : target;
+  }
+  __device__ __forceinline__ u64 point(u64 all) const { return (u64)((double)u * (double)all); }   // below `all`: u is at most 1 - 2^-24
+};
+
+struct Put {
+  const SampleArgs &a;
+  int64_t n;
+  __device__ __forceinline__ void operator()(int64_t token) const {
+    if (a.out64) static_cast<int64_t *>(a.out)[n] = token;
+    else static_cast<int32_t *>(a.out)[n] = (int32_t)token;
+  }
+};
+
+// A logit such that at least those in bins up to `last` are not below it.
+__device__ __forceinline__ float bound_of(const Bins &few, int last) {
+  // the smallest key of these bins, by search: 64 at a time
+  uint32_t a = 0x00800000u, b = key_of(few.best);
+  while (a < b) {
+    const uint32_t step = (b - a + 63) / 64, lane = threadIdx.x & 63, at = b - a < lane * (u64)step ? b : a + lane * step;
+    const int f = __ffsll((long long)__ballot(few.of(logit_of(at)) <= last)) - 1;
+    if (f == 0) {
+      b = a;
+    } else if (f < 0) {
+      a += 63 * step + 1;
+    } else {
+      const uint32_t to = b - a < f * (u64)step ? b : a + f * step;
+      a += (f - 1) * step + 1;
+      b = to;
+    }
+  }
+  return logit_of(b);
+}
+
+// The last bin of those that hold the k largest of n values (-inf: none), -1 if there are fewer than k.  sh.bins has to be clear.
+__device__ __forceinline__ int bin_of_kth(Shared &sh, const Bins &few, const float *values, int n, int64_t k) {
+  for (int i = threadIdx.x; i < n; i += kThreads)
+    if (values[i] > -INFINITY) atomicAdd(&sh.bins[few.of(values[i])], 1ull);
+  if (threadIdx.x == 0) sh.slot = -1;
+  __syncthreads();
+  const u64 x = sh.bins[2 * threadIdx.x], y = sh.bins[2 * threadIdx.x + 1];
+  u64 all;
+  const u64 before = block_before_u64(x + y, sh, &all);
+  if (before < (u64)k && (u64)k <= before + x + y) sh.slot = 2 * threadIdx.x + ((u64)k > before + x ? 1 : 0);
+  __syncthreads();
+  return sh.slot;
+}
+
+// The draw from sh.list[0 .. M): every token that top-k (with top-p and min-p) or min-p alone can keep.
+__device__ __forceinline__ void draw_small(Shared &sh, int M, const Asked &q, const Weights &wt, int V, const Put &put) {
+  sort_small(sh, M);
+  const Rank r = (int)threadIdx.x < M && !(q.k > 0 && (int64_t)threadIdx.x >= q.k) ? sh.sorted[threadIdx.x] : 0;
+  const double e = r ? wt.exponential(logit_of((uint32_t)(r >> 32))) : 0.0;
+  const u64 w = wt.of(e);
+  bool kept = r != 0;
+  if (q.p < 1.0f) {
+    u64 all;
+    const u64 before = block_before_u64(w, sh, &all);
+    kept = kept && (before < q.share(all) || threadIdx.x == 0);
+  }
+  kept = kept && e >= (double)q.minp;
+  if (q.inside()) {
+    u64 all;
+    block_before_u64(kept ? w : 0, sh, &all);
+    const u64 target = q.point(all);
+    if ((int)threadIdx.x < M) {
+      sh.list[threadIdx.x] = r;
+      sh.weight[threadIdx.x] = kept ? w : 0;
+    }
+    __syncthreads();
+    // running sums in the order of indices, by comparing each with each
+    int size = 1;
+    while (size < M) size <<= 1;
+    const int parts = min(64, kThreads / size), me = (int)threadIdx.x / parts, part = (int)threadIdx.x % parts;
+    const uint32_t index = me < M ? index_of(sh.list[me]) : 0;
+    u64 before = 0;
+    if (me < M)
+      for (int j = part; j < M; j += parts)
+        if (index_of(sh.list[j]) < index) before += sh.weight[j];
+    for (int o = 1; o < parts; o <<= 1) before += __shfl_xor(before, o, 64);
+    if (me < M && part == 0 && before <= target && target < before + sh.weight[me]) put(index);
+  } else {                                               // the ends of the range: the first and the last token, however light
+    if (threadIdx.x == 0) sh.slot = q.u >= 1.0f ? -1 : V;
+    __syncthreads();
+    if (kept && e > 0.0) {
+      if (q.u >= 1.0f) atomicMax(&sh.slot, (int)index_of(r));
+      else atomicMin(&sh.slot, (int)index_of(r));
+    }
+    __syncthreads();
+    if (threadIdx.x == 0) put(sh.slot);
+  }
+}
+
+// The draw from a whole row whose largest logit is known, in passes over it.
+template <typename T>
+__device__ __forceinline__ void draw_whole(const Span<T> &row, Shared &sh, const Asked &q, const Weights &wt, const Put &put) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const float best = wt.best;
+  if (best == INFINITY) {                                // equal weights for the tokens that have it, none for the others
+    u64 m = 0, all;
+    row.template each<1>([&](float z, uint32_t) { m += z == INFINITY; });
+    block_before_u64(m, sh, &all);
+    if (q.k > 0 && (u64)q.k < all) all = (u64)q.k;
+    if (q.p < 1.0f) all = q.share(all);
+    const u64 target = !(q.u > 0.0f) ? 0 : q.u >= 1.0f ? all - 1 : q.point(all);
+    locate<1>(row, sh, 0, [=](u64) { return target; }, [](float z, uint32_t) -> u64 { return z == INFINITY; }, put);
+    return;
+  }
+  Rank border = 1;
+  // first the border of top-k, counting tokens, then that of top-p among what is left, adding weights (one piece of code)
+#pragma unroll 1
+  for (int by_weight = 0; by_weight < 2; ++by_weight) {
+    float width;                                         // of what the bins cover
+    if (by_weight) {
+      if (!(q.p < 1.0f)) break;
+      width = 33.0f * q.t;                               // further below the largest logit weights are zero
+    } else {
+      if (q.k <= 0) continue;
+      float least = INFINITY;
+      int have = 0;
+      row.template each<1>([&](float z, uint32_t) {
+        if (z > -INFINITY) {
+          least = fminf(least, z);
+          ++have;
+        }
+      });
+      u64 all;
+      block_before_u64((u64)have, sh, &all);
+      if ((u64)q.k >= all) continue;
+      least = -wave_max(-least);
+      if (lane == 0) sh.fmin[wave] = least;
+      __syncthreads();
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) least = fminf(least, sh.fmin[w]);
+      width = best - least;
+    }
+    const Bins bins(best, width);
+    const float zero = by_weight ? wt.zero(q.t) : -INFINITY;
+    const auto share = [&](float z) -> u64 { return by_weight ? (z >= zero ? wt.of(wt.near(z)) : 0) : 1; };
+    clear_bins(sh);
+    row.each([&](float z, uint32_t i) {
+      if (z > -INFINITY && (border <= 1 || rank_of(z, i) >= border)) add_to_bin(sh, bins.of(z), z, share(z));
+    });
+    __syncthreads();
+    u64 target = (u64)q.k;
+    if (by_weight) {
+      u64 all;
+      block_before_u64(sh.bins[2 * threadIdx.x] + sh.bins[2 * threadIdx.x + 1], sh, &all);
+      target = q.share(all);
+      __syncthreads();
+    }
+    border = find_border(row, sh, bins, border, target, share);
+    __syncthreads();
+  }
+  Limit limit = border <= 1 ? Limit{-INFINITY, 0} : Limit{logit_of((uint32_t)(border >> 32)), index_of(border) + 1};
+  if (q.minp > 0.0f) limit.not_below(least_logit(wt, q.t, q.minp));
+  if (!q.inside()) {                                     // the ends of the range: the first and the last token, however light
+    __syncthreads();
+    if (threadIdx.x == 0) sh.slot = q.u >= 1.0f ? -1 : row.V;
+    __syncthreads();
+    row.template each<1>([&](float z, uint32_t i) {
+      if (limit.keeps(z, i) && wt.exponential(z) > 0.0) {
+        if (q.u >= 1.0f) atomicMax(&sh.slot, (int)i);
+        else atomicMin(&sh.slot, (int)i);
+      }
+    });
+    __syncthreads();
+    if (threadIdx.x == 0) put(sh.slot);
+    return;
+  }
+  limit.not_below(wt.zero(q.t));
+  const auto W = [&](float z, uint32_t i) -> u64 { return wt.of(limit.keeps(z, i) ? wt.near(z) : 0.0); };
+  locate<4>(row, sh, 0, [&](u64 all) { return q.point(all); }, W, put);
+}
+
+__device__ __forceinline__ void start(Shared &sh) {
+  if (threadIdx.x < 32) sh.powers[threadIdx.x] = kPowers[threadIdx.x];
+  clear_bins(sh);
+}
+
+template <typename T>
+__global__ __launch_bounds__(kThreads) void sample_kernel(const T *logits, SampleArgs a) {
+  __shared__ Shared sh;
+  const int64_t n = blockIdx.x;
+  const Span<T> row(logits + n * a.pitch, a.V, 0, a.V);
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const Put put{a, n};
+  // the largest logit, the threads' own, and the smallest of those
+  float mine = -INFINITY;
+  row.each([&](float z, uint32_t) { mine = fmaxf(mine, z); });
+  const float wmax = wave_max(mine), wmin = -wave_max(mine > -INFINITY ? -mine : -INFINITY);
+  if (lane == 0) {
+    sh.fmax[wave] = wmax;
+    sh.fmin[wave] = wmin;
+  }
+  start(sh);
+  float best = sh.fmax[0], low = sh.fmin[0];
+#pragma unroll
+  for (int w = 1; w < kWaves; ++w) {
+    best = fmaxf(best, sh.fmax[w]);
+    low = fminf(low, sh.fmin[w]);
+  }
+  if (best == -INFINITY) {                               // nothing to choose from
+    if (threadIdx.x == 0) put(-1);
+    return;
+  }
+  const Asked q(a, n);
+  if (q.greedy()) {
+    if (threadIdx.x == 0) sh.slot = a.V;
+    __syncthreads();
+    if (mine == best)                                    // (the others have nothing to find)
+      row.template each<1>([&](float z, uint32_t i) {
+        if (z == best) atomicMin(&sh.slot, (int)i);
+      });
+    __syncthreads();
+    if (threadIdx.x == 0) put(sh.slot);
+    return;
+  }
+  const Weights wt(best, q.t, a.shift, sh);
+  // a row that comes down to a few tokens: all of them from a bound on
+  int M = kSmall + 1;
+  if (best < INFINITY) {
+    if (q.k > 0 && q.k <= kThreads) {
+      const Bins few(best, best - low);
+      sh.part[threadIdx.x] = mine;
+      const int last = bin_of_kth(sh, few, sh.part, kThreads, q.k);
+      if (last >= 0) {
+        row.each([&](float z, uint32_t i) {
+          if (z > -INFINITY && few.of(z) <= last) gather(sh, rank_of(z, i));
+        });
+        __syncthreads();
+        M = sh.count;
+      }
+    } else if (q.k <= 0 && !(q.p < 1.0f) && q.minp > 0.0f) {
+      const float least = least_logit(wt, q.t, q.minp);
+      row.each([&](float z, uint32_t i) {
+        if (z >= least) gather(sh, rank_of(z, i));
+      });
+      __syncthreads();
+      M = sh.count;
+    }
+  }
+  if (M <= kSmall) draw_small(sh, M, q, wt, a.V, put);
+  else draw_whole(row, sh, q, wt, put);
+}
+
+// ---- rows in chunks -------------------------------------------------------------------------------------------------
+// The code of these kernels runs once through, from a cold instruction cache: loops work on one or two units at a time, not on four.
+template <typename T>
+__device__ __forceinline__ Span<T> chunk_of(const T *logits, const SampleArgs &a, int64_t n, int chunk) {
+  return Span<T>(logits + n * a.pitch, a.V, chunk * a.chunk_units, chunk + 1 == a.chunks ? a.V : (chunk + 1) * a.chunk_units);
+}
+
+// Launch 1: the maxima of all parts; what later launches add to is cleared.
+template <typename T>
+__global__ __launch_bounds__(kThreads) void sample_maxima_kernel(const T *logits, SampleArgs a) {
+  constexpr int E = Span<T>::E, U = 4;
+  const int64_t n = blockIdx.y;
+  const int chunk = blockIdx.x, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  RowSpace &space = a.space[n];
+  if (chunk == 0) {
+    space.bins[2 * threadIdx.x] = 0;
+    space.bins[2 * threadIdx.x + 1] = 0;
+    if (threadIdx.x == 0) space.count = 0;
+  }
+  const T *z = logits + n * a.pitch;
+  const int whole = a.V / E, p0 = chunk * (a.chunk_units / 64), p1 = min(a.parts, p0 + a.chunk_units / 64);
+  for (int p = p0 + wave; p < p1; p += kWaves * U) {
+    Unit<T, E> t[U];
+#pragma unroll
+    for (int j = 0; j < U; ++j) {
+      const int u = (p + j * kWaves) * 64 + lane;
+      if (p + j * kWaves < p1 && u < whole) t[j].load(z + u * E);
+    }
+#pragma unroll
+    for (int j = 0; j < U; ++j) {
+      const int at = p + j * kWaves, u = at * 64 + lane;
+      if (at >= p1) break;
+      float m = -INFINITY;
+      if (u < whole) {
+#pragma unroll
+        for (int i = 0; i < E; ++i) m = fmaxf(m, t[j].get(i));
+      }
+      if (at == a.parts - 1 && whole * E + lane < a.V) m = fmaxf(m, Elem<T>::load(z + whole * E + lane));
+      m = max64(m);
+      if (lane == 0) space.maxima[at] = m;
+    }
+  }
+}
+
+// How a row is drawn from, the same in all launches that follow.
+enum Way { kNothing, kGreedy, kFew, kSums, kPlain, kWhole };
+struct Plan {
+  Way way;
+  float best, low;                   // largest and smallest of the parts' maxima
+};
+
+__device__ __forceinline__ Plan plan_row(Shared &sh, const SampleArgs &a, const RowSpace &space, const Asked &q) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  float top = -INFINITY, down = INFINITY;
+  for (int p = threadIdx.x; p < a.parts; p += kThreads) {
+    const float m = space.maxima[p];
+    top = fmaxf(top, m);
+    if (m > -INFINITY) down = fminf(down, m);
+  }
+  top = max64(top);
+  down = -max64(-down);
+  if (lane == 0) {
+    sh.fmax[wave] = top;
+    sh.fmin[wave] = down;
+  }
+  start(sh);
+  Plan plan{kNothing, sh.fmax[0], sh.fmin[0]};
+#pragma unroll
+  for (int w = 1; w < kWaves; ++w) {
+    plan.best = fmaxf(plan.best, sh.fmax[w]);
+    plan.low = fminf(plan.low, sh.fmin[w]);
+  }
+  if (plan.best == -INFINITY) return plan;
+  plan.way = q.greedy() ? kGreedy : plan.best < INFINITY ? (q.k > 0 ? kFew : !q.inside() ? kWhole : q.p < 1.0f ? kSums : kPlain) : kWhole;
+  return plan;
+}
+
+// Launch 2: sums by bin where top-p asks for them, otherwise the chunk's sum.
+template <typename T>
+__global__ __launch_bounds__(kThreads) void sample_bins_kernel(const T *logits, SampleArgs a) {
+  __shared__ Shared sh;
+  const int64_t n = blockIdx.y;
+  const Asked q(a, n);
+  if (q.greedy() || q.k > 0) return;
+  const int chunk = blockIdx.x;
+  RowSpace &space = a.space[n];
+  const Plan plan = plan_row(sh, a, space, q);
+  if (plan.way != kSums && plan.way != kPlain) return;
+  const Span<T> span = chunk_of(logits, a, n, chunk);
+  const Weights wt(plan.best, q.t, a.shift, sh);
+  float least = wt.zero(q.t);
+  if (plan.way == kSums) {
+    const Bins bins(plan.best, 33.0f * q.t);
+    span.template each<8 / Span<T>::E>([&](float z, uint32_t) {
+      if (z >= least) add_to_bin(sh, bins.of(z), z, wt.of(wt.near(z)));
+    });
+    __syncthreads();
+    for (int b = threadIdx.x; b < kBins; b += kThreads)
+      if (sh.bins[b]) atomicAdd(&space.bins[b], sh.bins[b]);
+  } else {
+    if (q.minp > 0.0f) least = fmaxf(least, least_logit(wt, q.t, q.minp));
+    u64 sum = 0, all;
+    span.template each<8 / Span<T>::E>([&](float z, uint32_t) { sum += wt.of(z >= least ? wt.near(z) : 0.0); });
+    block_before_u64(sum, sh, &all);
+    if (threadIdx.x == 0) space.sums[chunk] = all;
+  }
+}
+
+// The bin of top-p's border; the sum before it in sh.above, the target in *target.
+__device__ __forceinline__ int border_bin(Shared &sh, const RowSpace &space, const Asked &q, u64 *target) {
+  sh.bins[2 * threadIdx.x] = space.bins[2 * threadIdx.x];
+  sh.bins[2 * threadIdx.x + 1] = space.bins[2 * threadIdx.x + 1];
+  u64 all;
+  block_before_u64(sh.bins[2 * threadIdx.x] + sh.bins[2 * threadIdx.x + 1], sh, &all);
+  *target = q.share(all);
+  return crossing_bin(sh, *target);
+}
+
+// Launch 3, rows with top-p alone: the tokens of the border's bin, and the chunk's sum over the tokens above it that min-p keeps.
+template <typename T>
+__global__ __launch_bounds__(kThreads) void sample_border_kernel(const T *logits, SampleArgs a) {
+  __shared__ Shared sh;
+  const int64_t n = blockIdx.y;
+  const Asked q(a, n);
+  if (q.k > 0 || !(q.p < 1.0f) || !q.inside() || q.greedy()) return;
+  const int chunk = blockIdx.x;
+  RowSpace &space = a.space[n];
+  const Plan plan = plan_row(sh, a, space, q);
+  if (plan.way != kSums) return;
+  const Span<T> span = chunk_of(logits, a, n, chunk);
+  const Weights wt(plan.best, q.t, a.shift, sh);
+  const Bins bins(plan.best, 33.0f * q.t);
+  u64 target, all, sum = 0;
+  const int bin = border_bin(sh, space, q, &target);
+  float least = wt.zero(q.t);
+  if (q.minp > 0.0f) least = fmaxf(least, least_logit(wt, q.t, q.minp));
+  span.template each<8 / Span<T>::E>([&](float z, uint32_t i) {
+    const int b = bins.of(z);
+    if (b == bin && z > -INFINITY) {
+      const int at = atomicAdd(&space.count, 1);
+      if (at < kSmall) space.list[at] = rank_of(z, i);
+    }
+    if (b < bin && z >= least) sum += wt.of(wt.near(z));
+  });
+  block_before_u64(sum, sh, &all);
+  if (threadIdx.x == 0) space.sums[chunk] = all;
+}
+
+// f(logit, index) for every token of the parts whose maxima are at least `least`, by some thread.
+template <typename T, typename F>
+__device__ __forceinline__ void parts_from(Shared &sh, const T *z, const SampleArgs &a, const RowSpace &space, float least, F f) {
+  constexpr int E = Span<T>::E;
+  int *hits = reinterpret_cast<int *>(sh.weight);        // (room for 2048)
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), whole = a.V / E;
+  for (int base = 0; base < a.parts; base += 2 * kSmall) {
+    __syncthreads();
+    if (threadIdx.x == 0) sh.slot = 0;
+    __syncthreads();
+    for (int p = base + threadIdx.x; p < min(a.parts, base + 2 * kSmall); p += kThreads)
+      if (space.maxima[p] >= least) hits[atomicAdd(&sh.slot, 1)] = p;
+    __syncthreads();
+    const int n = sh.slot;
+    for (int h = wave; h < n; h += 2 * kWaves) {
+      Unit<T, E> t[2];
+      int u[2];
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        u[j] = h + j * kWaves < n ? __builtin_amdgcn_readfirstlane(hits[h + j * kWaves]) * 64 + lane : whole;
+        if (u[j] < whole) t[j].load(z + u[j] * E);
+      }
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+        if (u[j] < whole) {
+#pragma unroll
+          for (int i = 0; i < E; ++i) f(t[j].get(i), (uint32_t)(u[j] * E + i));
+        }
+    }
+  }
+  // the tokens behind the last unit
+  const int i = whole * E + (int)threadIdx.x;
+  if (i < a.V) f(Elem<T>::load(z + i), (uint32_t)i);
+  __syncthreads();
+}
+
+// Launch 4: a block for each row.
+template <typename T>
+__global__ __launch_bounds__(kThreads) void sample_draw_kernel(const T *logits, SampleArgs a) {
+  __shared__ Shared sh;
+  const int64_t n = blockIdx.x;
+  const Put put{a, n};
+  const RowSpace &space = a.space[n];
+  const Asked q(a, n);
+  const Plan plan = plan_row(sh, a, space, q);
+  const T *z = logits + n * a.pitch;
+  if (plan.way == kNothing) {
+    if (threadIdx.x == 0) put(-1);
+    return;
+  }
+  if (plan.way == kGreedy) {
+    if (threadIdx.x == 0) sh.count = a.V;
+    parts_from(sh, z, a, space, plan.best, [&](float v, uint32_t i) {
+      if (v == plan.best) atomicMin(&sh.count, (int)i);
+    });
+    if (threadIdx.x == 0) put(sh.count);
+    return;
+  }
+  const Weights wt(plan.best, q.t, a.shift, sh);
+  bool whole = plan.way == kWhole;
+  if (plan.way == kFew) {
+    // the k-th largest of the parts' maxima is a bound (to the width of a bin)
+    const Bins few(plan.best, plan.best - plan.low);
+    const int last = q.k <= a.parts ? bin_of_kth(sh, few, space.maxima, a.parts, q.k) : -1;
+    whole = last < 0;
+    if (!whole) {
+      const float bound = bound_of(few, last);
+      if (threadIdx.x == 0) sh.count = 0;
+      parts_from(sh, z, a, space, bound, [&](float v, uint32_t i) {
+        if (v >= bound) gather(sh, rank_of(v, i));
+      });
+      const int M = sh.count;
+      if (M <= kSmall) {
+        draw_small(sh, M, q, wt, a.V, put);
+        return;
+      }
+      whole = true;
+    }
+  } else if (plan.way == kSums) {
+    whole = space.count > kSmall;
+  }
+  if (whole) {
+    draw_whole(Span<T>(z, a.V, 0, a.V), sh, q, wt, put);
+    return;
+  }
+  Limit limit{-INFINITY, 0};
+  const float zero = wt.zero(q.t);
+  float least = zero;
+  if (q.minp > 0.0f) least = fmaxf(least, least_logit(wt, q.t, q.minp));
+  u64 sum = (int)threadIdx.x < a.chunks ? space.sums[threadIdx.x] : 0;
+  if (plan.way == kSums) {
+    const int M = space.count;
+    if ((int)threadIdx.x < M) sh.list[threadIdx.x] = space.list[threadIdx.x];
+    u64 target;
+    border_bin(sh, space, q, &target);
+    const u64 before = sh.above;
+    __syncthreads();
+    const Rank border = border_in_list(sh, M, before, target, [&](float v) -> u64 { return v >= zero ? wt.of(wt.near(v)) : 0; });
+    limit = Limit{logit_of((uint32_t)(border >> 32)), index_of(border) + 1};
+    // the kept tokens of the border's bin belong to their chunks' sums
+    clear_bins(sh);
+    if ((int)threadIdx.x < M && sh.list[threadIdx.x] >= border) {
+      const Rank r = sh.list[threadIdx.x];
+      const float v = logit_of((uint32_t)(r >> 32));
+      const int unit = (int)(index_of(r) / Span<T>::E);
+      if (v >= least) atomicAdd(&sh.bins[min(a.chunks - 1, unit / a.chunk_units)], wt.of(wt.near(v)));
+    }
+    __syncthreads();
+    if ((int)threadIdx.x < a.chunks) sum += sh.bins[threadIdx.x];
+  }
+  limit.not_below(least);
+  u64 all;
+  const u64 before = block_before_u64(sum, sh, &all);
+  const u64 target = q.point(all);
+  if (before <= target && target < before + sum) {
+    sh.slot = threadIdx.x;
+    sh.result = before;
+  }
+  __syncthreads();
+  const int chunk = sh.slot;
+  const u64 from = sh.result;
+  __syncthreads();
+  locate<8 / Span<T>::E>(chunk_of(logits, a, n, chunk), sh, from, [=](u64) { return target; },
+                         [&](float v, uint32_t i) -> u64 { return wt.of(limit.keeps(v, i) ? wt.near(v) : 0.0); }, put);
+}
+
+// Chunks that a row is cut in; 1: a block has it whole.  Measured in us (whole rows / chunks; fp32, each with parameters by row: top-k, top-p, none):
+//   1 x 32768 15 38 19 / 17 32 19    1 x 131072 27 104 47 / 17 33 19    32 x 65536 28 63 29 / 24 44 23    128 x 65536 29 65 30 / 35 84 41
+//   256 x 131072 73 144 71 / 58 148 81, with all filters mixed 123 / 86 (chunks even out rows that ask for more than others)
+//   512 x 131072 130 262 134 / 106 244 138
+int chunks_of(int64_t N, int64_t V) {
+  if (V < 65536 || V < 512 * N || V > (int64_t)kMaxParts * 64 * 4) return 1;   // (a unit has four elements at the least)
+  int64_t n = V / 4096;                                  // a unit or two for each thread
+  const int64_t most = (2048 + N - 1) / N;               // and about eight blocks for each compute unit
+  if (n > most) n = most;
+  return n > kMaxChunks ? kMaxChunks : (int)n;
 }
 
 chn_status check_row_parameter(const chn_array *v, const char *name, int64_t n, int64_t *stride) {
@@ -518,6 +971,25 @@ chn_status check_row_parameter(const chn_array *v, const char *name, int64_t n, 
   if (v->ndim != 1 || v->shape[0] != n) return fail(CHN_ERR_SHAPE, "sample: %s must have shape (%lld,)", name, (long long)n);
   *stride = n > 1 ? v->strides[0] / dtype_size(v->dtype) : 1;
   return CHN_OK;
+}
+
+template <typename T>
+void launch(const chn_array *logits, SampleArgs &a, hipStream_t st) {
+  const T *z = static_cast<const T *>(logits->data);
+  const dim3 rows((unsigned)a.N), threads(kThreads);
+  if (a.chunks == 1) {
+    hipLaunchKernelGGL((sample_kernel<T>), rows, threads, 0, st, z, a);
+    return;
+  }
+  const int units = a.V / Span<T>::E;
+  a.parts = (units + 63) / 64;
+  a.chunk_units = (a.parts + a.chunks - 1) / a.chunks * 64;
+  a.chunks = (a.parts * 64 + a.chunk_units - 1) / a.chunk_units;   // (none without a part)
+  const dim3 grid((unsigned)a.chunks, (unsigned)a.N);
+  hipLaunchKernelGGL((sample_maxima_kernel<T>), grid, threads, 0, st, z, a);
+  hipLaunchKernelGGL((sample_bins_kernel<T>), grid, threads, 0, st, z, a);
+  if (a.top_p) hipLaunchKernelGGL((sample_border_kernel<T>), grid, threads, 0, st, z, a);
+  hipLaunchKernelGGL((sample_draw_kernel<T>), rows, threads, 0, st, z, a);
 }
 
 chn_status check_row_float(const chn_array *v, const char *name, int64_t n, const float **data, int64_t *stride) {
@@ -534,8 +1006,8 @@ chn_status check_row_float(const chn_array *v, const char *name, int64_t n, cons
 extern "C" {
 
 size_t chn_sample_workspace_bytes(const chn_array *logits) {
-  (void)logits;
-  return 0;
+  if (!logits || logits->ndim != 2 || logits->shape[0] <= 0 || logits->shape[1] <= 0) return 0;
+  return chn::chunks_of(logits->shape[0], logits->shape[1]) > 1 ? (size_t)logits->shape[0] * sizeof(chn::RowSpace) : 0;
 }
 
 chn_status chn_sample(const chn_array *logits, const chn_array *u, const chn_array *temperature, const chn_array *top_k, const chn_array *top_p,
@@ -570,13 +1042,12 @@ chn_status chn_sample(const chn_array *logits, const chn_array *u, const chn_arr
   while (a.shift > 0 && (V >> (63 - a.shift)) > 0) --a.shift;
   a.out = out->data;
   a.out64 = out->dtype == CHN_I64;
-  (void)ws;
-  (void)ws_bytes;
   hipStream_t st = as_stream(stream);
-  if (logits->dtype == CHN_F32)
-    hipLaunchKernelGGL((sample_kernel<float>), dim3((unsigned)a.N), dim3(kThreads), 0, st, static_cast<const float *>(logits->data), a);
-  else
-    hipLaunchKernelGGL((sample_kernel<bf16_raw>), dim3((unsigned)a.N), dim3(kThreads), 0, st, static_cast<const bf16_raw *>(logits->data), a);
+  const size_t need = chn_sample_workspace_bytes(logits);
+  a.chunks = need > 0 && ws && ws_bytes >= need && reinterpret_cast<uintptr_t>(ws) % 256 == 0 ? chunks_of(a.N, V) : 1;
+  a.space = static_cast<RowSpace *>(ws);
+  if (logits->dtype == CHN_F32) launch<float>(logits, a, st);
+  else launch<bf16_raw>(logits, a, st);
   return check_launch("sample");
 }
 

@@ -170,3 +170,50 @@ def test_sample_on_a_stream_and_in_a_graph():
         torch.cuda.synchronize()
         assert np.array_equal(out.cpu().numpy(), w)
         B.sample(torch.zeros(2, 9, device="cuda"), torch.rand(2, device="cuda"), torch.empty(2, dtype=torch.int64, device="cuda"))
+
+
+@pytest.mark.parametrize("v", [65536, 70003, 131072])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_rows_of_every_kind_in_one_batch(v, dtype):
+    """Long rows are cut in chunks where the call brings a workspace: every way a row can go, beside all the others, and the same tokens without."""
+    n = 24
+    rng = np.random.default_rng(v)
+    z = logits(n, v, dtype, v + 1, 2.0, 1)
+    z[0] = -np.inf                                       # nothing to choose from
+    z[1] = 0.25                                          # all equal
+    z[2, 10:] = float("nan")
+    z[3, ::3] = np.inf                                   # equal infinities
+    z[4] = torch.finfo(z.dtype).min
+    z[5, :-1] = -np.inf                                  # one token, the last
+    z[6] = torch.round(z[6] * 2) / 2                     # few values, many ties at every border
+    z[7] = torch.round(z[7] * 2) / 2
+    z[8] = z[8] * 1e-3                                   # nearly flat
+    z[9] = z[9] * 1e4
+    z[10, 100] = np.inf                                  # one infinity
+    params = dict(temperature=rng.choice([0.0, 0.5, 1.0, 1.7], n), top_k=rng.choice([0, 0, 1, 50, 600, 5000, v], n),
+                  top_p=rng.choice([1.0, 0.0, 0.3, 0.9, 0.999], n), min_p=rng.choice([0.0, 0.0, 0.01, 0.3, 1.0], n))
+    params["temperature"][:12] = 0.9
+    u = rng.random(n, dtype=np.float32)
+    u[12], u[13] = 0.0, np.nextafter(np.float32(1), np.float32(0))
+    for names in ((), ("top_k",), ("top_p",), ("min_p",), ("temperature", "top_p", "min_p"), ("temperature", "top_k", "top_p", "min_p")):
+        check(z, u, **{k: params[k] for k in names})
+
+
+def test_two_calls_at_once_have_their_own_workspaces():
+    v = 131072
+    a, b = logits(3, v, "f32", 31).contiguous(), logits(5, v, "f32", 32).contiguous()
+    ua, ub = torch.rand(3, device="cuda"), torch.rand(5, device="cuda")
+    p = torch.full((5,), 0.9, device="cuda")
+    alone = draw(a, ua, top_p=p[:3]), draw(b, ub, top_p=p)
+    torch.cuda.synchronize()
+    streams, outs, spaces = [torch.cuda.Stream() for _ in range(2)], [], []
+    for s, z, u in zip(streams, (a, b), (ua, ub)):
+        spaces.append(torch.empty(B.sample_workspace_bytes(z), dtype=torch.uint8, device="cuda"))
+        outs.append(torch.empty(z.shape[0], dtype=torch.int64, device="cuda"))
+    torch.cuda.synchronize()
+    for _ in range(4):
+        for s, z, u, o, w in zip(streams, (a, b), (ua, ub), outs, spaces):
+            with torch.cuda.stream(s):
+                B.sample(z, u, o, top_p=p[:z.shape[0]], ws=w)
+    torch.cuda.synchronize()
+    assert np.array_equal(outs[0].cpu().numpy(), alone[0]) and np.array_equal(outs[1].cpu().numpy(), alone[1])
