@@ -31,6 +31,7 @@ __all__ = ["Variable", "Parameter", "VariableNode", "FunctionNode", "GpuBackend"
            "embed_id", "lstm", "split_rows", "concat_rows", "Linear", "SGD", "Adam", "live_function_nodes",
            "grad", "mul", "sub", "scale", "tanh", "sum_all", "sum_rows", "broadcast_to", "broadcast_rows", "transpose",
            "relu_grad", "user_elementwise",
+           "Masks", "dropout", "layer_norm", "residual_norm", "LayerNorm",
            "MLP", "LSTMLanguageModel"]
 
 
@@ -177,6 +178,28 @@ class GpuBackend:
 
     def embed_bwd(self, ids, dout, dtable, accumulate):
         self.B.embed_bwd(ids, dout, dtable, accumulate)
+
+    def dropout(self, x, y, ratio, rng, site, residual=None):
+        self.B.dropout(x, y, ratio, rng, site, residual)
+
+    def rng_advance(self, rng, steps):
+        self.B.rng_advance(rng, steps)
+
+    def layer_norm_fwd(self, x, y, gamma, beta, eps, mean, rstd):
+        self.B.layer_norm_fwd(x, y, gamma, beta, eps, mean, rstd)
+
+    def layer_norm_bwd(self, dy, x, mean, rstd, dx, gamma, dgamma, dbeta):
+        self.B.layer_norm_bwd(dy, x, mean, rstd, dx, gamma, dgamma, dbeta, ws=self._bytes(self.B.layer_norm_bwd_workspace_bytes(x)))
+
+    def residual_norm_fwd(self, x, residual, s, y, gamma, beta, eps, mean, rstd, ratio, rng, site):
+        self.B.residual_norm_fwd(x, residual, s, y, gamma, beta, eps, mean, rstd, ratio, rng, site)
+
+    def residual_norm_bwd(self, dy, ds, s, mean, rstd, dresidual, dx, gamma, dgamma, dbeta, ratio, rng, site):
+        self.B.residual_norm_bwd(dy, ds, s, mean, rstd, dresidual, dx, gamma, dgamma, dbeta, ratio, rng, site,
+                                 ws=self._bytes(self.B.layer_norm_bwd_workspace_bytes(s)))
+
+    def sample(self, logits, u, out, temperature=None, top_k=None, top_p=None, min_p=None):
+        self.B.sample(logits, u, out, temperature, top_k, top_p, min_p, ws=self._bytes(self.B.sample_workspace_bytes(logits)))
 
     def sgd_update_multi(self, params, grads, lr, lowp_copies):
         self.B.sgd_update_multi(params, grads, lr, lowp_copies)
@@ -1456,6 +1479,142 @@ class NStepLSTM(FunctionNode):
         return tuple(out)
 
 
+class Masks:
+    """Where dropout's masks come from: a seed and an offset on the device (what the kernels read when they run) and a number for
+    each place that draws.  A mask is a function of these, so none is kept: the backward pass draws it again.
+
+    ``advance()`` begins another step: the offset moves on the stream (in a captured step: at every replay) and places are numbered from
+    0 again.  Not between a forward and its backward pass: the backward pass would draw other masks, and says so instead."""
+
+    def __init__(self, seed, offset=0):
+        import numpy as np
+        self.rng = backend().from_numpy(np.array([(seed + 2 ** 63) % 2 ** 64 - 2 ** 63, offset], dtype=np.int64))
+        self.steps = self.sites = 0
+
+    def advance(self):
+        backend().rng_advance(self.rng, 1)
+        self.steps, self.sites = self.steps + 1, 0
+
+    def site(self):
+        """The next place, with the step that it belongs to."""
+        self.sites += 1
+        return self.steps, self.sites - 1
+
+
+def _draw(masks, ratio, place):
+    """(rng, site) of a place, for the kernels; nothing where nothing is dropped."""
+    if ratio == 0.0:
+        return None, 0
+    if masks.steps != place[0]:
+        raise RuntimeError("Masks.advance() was called between a forward pass and its backward pass: the masks are those of another step now")
+    return masks.rng, place[1]
+
+
+def _place(masks, ratio):
+    if ratio == 0.0:
+        return None
+    if masks is None:
+        raise ValueError("dropout needs Masks to draw from")
+    return masks.site()
+
+
+class Dropout(FunctionNode):
+    """keep * x / (1 - ratio), the mask from `masks` at one place.  Linear, and nothing is retained: the gradient is the same call on the
+    gradient, any number of times."""
+    fresh = (0,)
+
+    def __init__(self, ratio, masks, place, out_dtype=None, gx_dtype=None):
+        super().__init__()
+        self.ratio, self.masks, self.place, self.out_dtype, self.gx_dtype = float(ratio), masks, place, out_dtype, gx_dtype
+
+    def _run(self, x, dtype):
+        F = backend()
+        y = F.empty(x.shape, dtype)
+        F.dropout(x, y, self.ratio, *_draw(self.masks, self.ratio, self.place))
+        return y
+
+    def forward(self, xs):
+        F = backend()
+        if self.gx_dtype is None:
+            self.gx_dtype = F.dtype(xs[0])
+        return (self._run(xs[0], self.out_dtype or F.dtype(xs[0])),)
+
+    def backward(self, indexes, gys):
+        return (self._run(gys[0], self.gx_dtype),)
+
+    def backward_vars(self, indexes, gys):
+        return (Dropout(self.ratio, self.masks, self.place, self.gx_dtype).apply((gys[0],))[0],)
+
+
+class LayerNormFunction(FunctionNode):
+    """(x, gamma, beta) -> (x - mean) * rstd * gamma + beta over the rows of x; gamma and beta fp32.  Retains x and gamma and keeps the
+    rows' statistics, so that the backward pass is one walk over x and the gradient."""
+    fresh = (0, 1, 2)
+
+    def __init__(self, eps=1e-5, out_dtype=None):
+        super().__init__()
+        self.eps, self.out_dtype, self.mean, self.rstd = float(eps), out_dtype, None, None
+
+    def forward(self, xs):
+        F = backend()
+        x, gamma, beta = xs
+        y = F.empty(x.shape, self.out_dtype or F.dtype(x))
+        self.mean, self.rstd = F.empty((x.shape[0],), "f32"), F.empty((x.shape[0],), "f32")
+        F.layer_norm_fwd(x, y, gamma, beta, self.eps, self.mean, self.rstd)
+        self.retain_inputs((0, 1))
+        return (y,)
+
+    def release_locals(self):
+        self.mean = self.rstd = None
+
+    def backward(self, indexes, gys):
+        F = backend()
+        x, gamma = self.get_retained_inputs()
+        new = lambda i: F.empty((x.shape[1],), "f32") if i in indexes else None
+        out = {0: F.empty(x.shape, F.dtype(x)), 1: new(1), 2: new(2)}
+        F.layer_norm_bwd(gys[0], x, self.mean, self.rstd, out[0], gamma, out[1], out[2])
+        return tuple(out[i] for i in indexes)
+
+
+class ResidualNorm(FunctionNode):
+    """(x, residual, gamma, beta) -> (y, s): s = residual + dropout(x), y = layer_norm(s), in one pass over the rows; s has the
+    residual's type, y that of x.  Retains s and gamma; the backward pass joins both outputs' gradients."""
+    fresh = (0, 1, 2, 3)
+
+    def __init__(self, ratio, masks, place, eps=1e-5):
+        super().__init__()
+        self.ratio, self.masks, self.place, self.eps = float(ratio), masks, place, float(eps)
+        self.mean = self.rstd = None
+
+    def forward(self, xs):
+        F = backend()
+        x, residual, gamma, beta = xs
+        s, y = F.empty(residual.shape, F.dtype(residual)), F.empty(x.shape, F.dtype(x))
+        self.mean, self.rstd = F.empty((x.shape[0],), "f32"), F.empty((x.shape[0],), "f32")
+        F.residual_norm_fwd(x, residual, s, y, gamma, beta, self.eps, self.mean, self.rstd, self.ratio, *_draw(self.masks, self.ratio, self.place))
+        self.layer = F.dtype(x)
+        self.retain_inputs((2,))
+        self.retain_outputs((1,))
+        return (y, s)
+
+    def release_locals(self):
+        self.mean = self.rstd = None
+
+    def backward(self, indexes, gys):
+        F = backend()
+        gamma, = self.get_retained_inputs()
+        s, = self.get_retained_outputs()
+        gy, gs = gys
+        if gy is None:                                   # (only the sum was used)
+            gy = F.empty(s.shape, self.layer)
+            F.elementwise_broadcast("fill", [], gy, (0.0,))
+        new = lambda i, shape, dtype: F.empty(shape, dtype) if i in indexes else None
+        out = {0: new(0, s.shape, self.layer), 1: new(1, s.shape, F.dtype(s)), 2: new(2, (s.shape[1],), "f32"), 3: new(3, (s.shape[1],), "f32")}
+        F.residual_norm_bwd(gy, gs, s, self.mean, self.rstd, out[1], out[0], gamma, out[2], out[3], self.ratio,
+                            *_draw(self.masks, self.ratio, self.place))
+        return tuple(out[i] for i in indexes)
+
+
 class SplitRows(FunctionNode):
     """Cut a (n*r, d) array into n views of r rows (no copy; the views keep the buffer alive).
     The backward gathers the pieces' gradients into one array, zero where a piece was unused."""
@@ -1598,6 +1757,21 @@ def n_step_lstm(c0, h0, zx, U, bias, n_steps, lowp=False):
     return NStepLSTM(n_steps, lowp).apply((c0, h0, zx, U, bias))
 
 
+def dropout(x, ratio, masks=None, out_dtype=None, gx_dtype=None):
+    """x with a share `ratio` of its elements dropped and the others scaled up, by the next place of `masks`.  ``out_dtype`` /
+    ``gx_dtype``: storage type of the result and of the gradient (default: x's)."""
+    return Dropout(ratio, masks, _place(masks, ratio), out_dtype, gx_dtype).apply((x,))[0]
+
+
+def layer_norm(x, gamma, beta, eps=1e-5, out_dtype=None):
+    return LayerNormFunction(eps, out_dtype).apply((x, gamma, beta))[0]
+
+
+def residual_norm(x, residual, gamma, beta, ratio=0.0, masks=None, eps=1e-5):
+    """Returns (y, s): s = residual + dropout(x), y = layer_norm(s)."""
+    return ResidualNorm(ratio, masks, _place(masks, ratio), eps).apply((x, residual, gamma, beta))
+
+
 def split_rows(x, n):
     return SplitRows(n).apply((x,))
 
@@ -1620,6 +1794,22 @@ class Linear:
 
     def __call__(self, x, act=None, out_dtype=None):
         return linear(x, self.W, self.b, act, out_dtype)
+
+
+class LayerNorm:
+    """The parameters of a layer normalisation, gamma and beta (n,), bound to its forward code; with `residual` that of a residual
+    block, which returns (y, s)."""
+
+    def __init__(self, gamma, beta, eps=1e-5):
+        self.gamma, self.beta, self.eps = Parameter(gamma, None, "gamma"), Parameter(beta, None, "beta"), eps
+
+    def params(self):
+        return [self.gamma, self.beta]
+
+    def __call__(self, x, residual=None, ratio=0.0, masks=None, out_dtype=None):
+        if residual is None:
+            return layer_norm(x, self.gamma, self.beta, self.eps, out_dtype)
+        return residual_norm(x, residual, self.gamma, self.beta, ratio, masks, self.eps)
 
 
 class SGD:
@@ -1677,11 +1867,16 @@ class MLP:
     ``lowp``: bf16 working copies of the weights, bf16 activations and activation gradients; fp32
     logits, loss, weight/bias gradients and master weights.  ``fused_activation=False`` applies the
     activation as a function node of its own instead of in the product's epilogue.
+
+    ``norms``: a (gamma, beta) for each hidden layer.  The hidden layers are then residual blocks: each adds its output to a stream (fp32
+    with ``lowp``) and hands on the stream's layer normalisation; where the width changes the stream begins anew.  ``ratio``: dropout
+    of the hidden layers' outputs while ``train`` is true, by ``masks``.
     """
 
-    def __init__(self, params, act="relu", lowp=False, fused_activation=True):
+    def __init__(self, params, act="relu", lowp=False, fused_activation=True, norms=None, ratio=0.0, masks=None):
         F = backend()
         self.act, self.lowp, self.fused = act, lowp, fused_activation
+        self.ratio, self.masks, self.train = float(ratio), masks, True
         self.layers = []
         for W, b in params:
             low = None
@@ -1689,17 +1884,31 @@ class MLP:
                 low = F.empty(W.shape, "bf16")
                 F.elementwise_broadcast("copy", [W], low)
             self.layers.append(Linear(W, b, low))
+        self.norms = None if norms is None else [LayerNorm(g, b) for g, b in norms]
+        if self.norms is not None and len(self.norms) != len(self.layers) - 1:
+            raise ValueError("MLP: %d norms for %d hidden layers" % (len(self.norms), len(self.layers) - 1))
+        if self.ratio > 0.0 and masks is None:
+            raise ValueError("MLP: dropout needs masks")
 
     def params(self):
-        return [p for l in self.layers for p in l.params()]
+        return [p for l in self.layers + (self.norms or []) for p in l.params()]
 
     def __call__(self, x):
-        h = x
-        for l in self.layers[:-1]:
+        h, stream = x, None
+        ratio = self.ratio if self.train else 0.0
+        for k, l in enumerate(self.layers[:-1]):
             if self.fused:
                 h = l(h, act=self.act)
             else:
                 h = (relu if self.act == "relu" else gelu)(l(h))
+            if self.norms is None:
+                if ratio > 0.0:
+                    h = dropout(h, ratio, self.masks)
+            elif stream is not None and tuple(stream.shape) == tuple(h.shape):
+                h, stream = self.norms[k](h, stream, ratio, self.masks)
+            else:
+                stream = dropout(h, ratio, self.masks, "f32") if ratio > 0.0 or self.lowp else h
+                h = self.norms[k](stream, out_dtype="bf16" if self.lowp else None)
         return self.layers[-1](h, out_dtype="f32")
 
     def loss(self, x, t):
@@ -1713,11 +1922,18 @@ class LSTMLanguageModel:
     time steps is whatever the batch at hand has.  ``n_step``: the recurrent layer is one
     ``n_step_lstm`` node instead of a product, a sum and a cell per time step."""
 
-    def __init__(self, P, n_step=False, lowp=False):
+    def __init__(self, P, n_step=False, lowp=False, ratio=0.0, masks=None):
         """lowp (with n_step): bf16 working copies of E, W, U and W_out feed the products, as do bf16
-        embeddings, hidden states and their gradients; everything else stays fp32."""
+        embeddings, hidden states and their gradients; everything else stays fp32.
+
+        ratio, masks: dropout of the embeddings and of the hidden states on their way to the output layer (not from step to step)
+        while `train` is true.  gamma and beta (H,) in P: layer normalisation of those hidden states."""
         if lowp and not n_step:
             raise ValueError("LSTMLanguageModel: lowp needs n_step=True")
+        if ratio > 0.0 and masks is None:
+            raise ValueError("LSTMLanguageModel: dropout needs masks")
+        if ("gamma" in P) != ("beta" in P):
+            raise ValueError("LSTMLanguageModel: gamma and beta come together")
         F = backend()
         self.P = {}
         for k, v in P.items():
@@ -1727,15 +1943,18 @@ class LSTMLanguageModel:
                 F.elementwise_broadcast("copy", [v], low)
             self.P[k] = Parameter(v, low, k)
         self.n_step, self.lowp = n_step, lowp
+        self.ratio, self.masks, self.train = float(ratio), masks, True
 
     def params(self):
         return list(self.P.values())
 
-    def loss(self, ids, targets, n_steps, state=None):
-        """ids, targets: flat (T*B,) integer arrays.  Returns (loss, (c, h)) so that a caller may
-        carry the state into the next window (after ``unchain`` for truncated back-propagation)."""
+    def _hidden(self, ids, n_steps, state):
+        """The hidden states of all steps, (T*B, H), as the output layer is to see them, and the state after the last."""
         P, F = self.P, backend()
+        ratio = self.ratio if self.train else 0.0
         X = embed_id(ids, P["E"])
+        if ratio > 0.0:
+            X = dropout(X, ratio, self.masks, gx_dtype="f32")
         zx = matmul(X, P["W"], out_dtype="f32", gx_dtype="f32")
         if state is None:
             Bn, H = ids.shape[0] // n_steps, P["U"].shape[0]
@@ -1746,12 +1965,49 @@ class LSTMLanguageModel:
             c, h = state
         if self.n_step:
             c, h, hs = n_step_lstm(c, h, zx, P["U"], P["b"], n_steps, self.lowp)
-            logits = linear(hs, P["W_out"], P["b_out"], out_dtype="f32")
-            return softmax_cross_entropy(logits, targets, grad_dtype="bf16" if self.lowp else None), (c, h)
-        zs = split_rows(zx, n_steps)
-        hs = []
-        for t in range(n_steps):
-            c, h = lstm(c, add(zs[t], matmul(h, P["U"])), P["b"])
-            hs.append(h)
-        logits = linear(concat_rows(hs), P["W_out"], P["b_out"])
-        return softmax_cross_entropy(logits, targets), (c, h)
+        else:
+            zs = split_rows(zx, n_steps)
+            hs = []
+            for t in range(n_steps):
+                c, h = lstm(c, add(zs[t], matmul(h, P["U"])), P["b"])
+                hs.append(h)
+            hs = concat_rows(hs)
+        return hs, (c, h)
+
+    def _logits(self, hs):
+        P = self.P
+        ratio = self.ratio if self.train else 0.0
+        if ratio > 0.0:
+            hs = dropout(hs, ratio, self.masks)
+        if "gamma" in P:
+            hs = layer_norm(hs, P["gamma"], P["beta"])
+        return linear(hs, P["W_out"], P["b_out"], out_dtype="f32" if self.n_step else None)
+
+    def loss(self, ids, targets, n_steps, state=None):
+        """ids, targets: flat (T*B,) integer arrays.  Returns (loss, (c, h)) so that a caller may
+        carry the state into the next window (after ``unchain`` for truncated back-propagation)."""
+        hs, state = self._hidden(ids, n_steps, state)
+        return softmax_cross_entropy(self._logits(hs), targets, grad_dtype="bf16" if self.lowp else None), state
+
+    def generate(self, ids, n_steps, u, state=None, temperature=None, top_k=None, top_p=None, min_p=None):
+        """Continues a prompt.  ids: flat (T*B,) integer array of `n_steps` steps, time-major; u: (n, B) array of fp32 numbers in [0, 1), one for
+        each token that is wanted.  temperature, top_k, top_p, min_p: a number, an array with one for each of the B sequences, or None
+        (not used).  Returns the (n, B) int64 array of tokens and the state after the last but one, which has seen everything but the
+        last token.  Nothing is recorded and nothing is dropped."""
+        import numpy as np
+        F = backend()
+        Bn = ids.shape[0] // n_steps
+        row = lambda v, dt: v if v is None or hasattr(v, "shape") else F.from_numpy(np.full((Bn,), v, dtype=dt))
+        filters = (row(temperature, np.float32), row(top_k, np.int64), row(top_p, np.float32), row(min_p, np.float32))
+        out = F.empty(tuple(u.shape), "i64")
+        was, self.train = self.train, False
+        try:
+            with no_backprop_mode():
+                for t in range(u.shape[0]):
+                    hs, state = self._hidden(ids, n_steps, state)
+                    last = Variable(hs.array[(n_steps - 1) * Bn:], requires_grad=False)
+                    F.sample(self._logits(last).array, u[t], out[t], *filters)
+                    ids, n_steps = out[t], 1
+        finally:
+            self.train = was
+        return out, state
