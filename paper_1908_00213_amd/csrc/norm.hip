@@ -512,76 +512,97 @@ __global__ __launch_bounds__(256) void norm_bwd_sums_kernel(const TY *dy, const 
   if (threadIdx.x == 0) a.sums[row * a.segments + blockIdx.y] = t;
 }
 
-// Then the gradients: a thread has E columns and walks over the neighbouring rows of a strip, so that the column sums need no exchange.
+// Then the gradients: a thread has E columns and walks over the neighbouring rows of a strip, R of them in flight together; the column sums need no
+// exchange.
 template <typename TX, typename TY, typename TS, bool RES>
 __global__ __launch_bounds__(256) void norm_bwd_wide_kernel(const TY *dy, const TS *s, const TS *ds, TS *dres, TX *dx, NormBwdArgs a) {
-  constexpr int E = unit_elements<TX, TY, TS>();
+  constexpr int E = unit_elements<TX, TY, TS>(), R = 4;
+  __shared__ float2 rows[2][R];
   const int64_t c0 = ((int64_t)blockIdx.x * 256 + threadIdx.x) * E;
-  if (c0 >= a.C) return;
   const DropState d(a.drop);
   const float inv = 1.0f / (float)a.C;
-  const int n = a.C - c0 < E ? (int)(a.C - c0) : E;     // columns of this thread
+  const int n = a.C - c0 < E ? (a.C > c0 ? (int)(a.C - c0) : 0) : E;   // columns of this thread
   const bool all = n == E;
   float gm[E], ag[E] = {}, ab[E] = {};
 #pragma unroll
   for (int i = 0; i < E; ++i) gm[i] = a.gamma && i < n ? a.gamma[c0 + i] : 1.0f;
   const int64_t per = (a.N + a.strips - 1) / a.strips, r0 = blockIdx.y * per, r1 = r0 + per < a.N ? r0 + per : a.N;
-  for (int64_t row = r0; row < r1; ++row) {
-    const float mean = a.mean[row], rstd = a.rstd[row];
-    float sg = 0.0f, sgh = 0.0f;
-    for (int k = 0; k < a.segments; ++k) {
-      const float2 t = a.sums[row * a.segments + k];
-      sg += t.x;
-      sgh += t.y;
-    }
-    const float c1 = sg * inv, c2 = sgh * inv;
-    const TY *yr = dy + row * a.pdy + c0;
-    const TS *sr = s + row * a.ps + c0, *er = RES && ds ? ds + row * a.pds + c0 : nullptr;
-    Unit<TY, E> yu;
-    Unit<TS, E> su, eu;
-    eu.zero();
-    if (all) {
-      yu.load(yr);
-      su.load(sr);
-      if (RES && ds) eu.load(er);
-    } else {
-      yu.zero();
-      su.zero();
-#pragma unroll
-      for (int i = 0; i < E; ++i)
-        if (i < n) {
-          yu.set(i, Elem<TY>::load(yr + i));
-          su.set(i, Elem<TS>::load(sr + i));
-          if (RES && ds) eu.set(i, Elem<TS>::load(er + i));
+  for (int64_t first = r0, turn = 0; first < r1; first += R, turn ^= 1) {
+    Unit<TY, E> yu[R];
+    Unit<TS, E> su[R], eu[R];
+    float mean[R], rstd[R];
+    float2 part = make_float2(0.0f, 0.0f);               // sixteen lanes add up the segments of a row
+    if (threadIdx.x < 16 * R) {
+      const int64_t row = first + threadIdx.x / 16;
+      if (row < r1)
+        for (int k = threadIdx.x % 16; k < a.segments; k += 16) {
+          const float2 t = a.sums[row * a.segments + k];
+          part.x += t.x;
+          part.y += t.y;
         }
     }
-    float o[E];
 #pragma unroll
-    for (int i = 0; i < E; ++i) {
-      const float v = yu.get(i), h = (su.get(i) - mean) * rstd;
-      ag[i] = fmaf(v, h, ag[i]);
-      ab[i] += v;
-      o[i] = rstd * (v * gm[i] - c1 - h * c2);
-      if (RES && ds) o[i] += eu.get(i);
-    }
-    const auto put = [&](auto *p) __attribute__((always_inline)) {
-      using T = std::remove_pointer_t<decltype(p)>;
+    for (int j = 0; j < R; ++j) {
+      const int64_t row = first + j < r1 ? first + j : r1 - 1;         // (the last one again, and not used)
+      const TY *yr = dy + row * a.pdy + c0;
+      const TS *sr = s + row * a.ps + c0, *er = RES && ds ? ds + row * a.pds + c0 : nullptr;
       if (all) {
-        Unit<T, E> out;
-#pragma unroll
-        for (int i = 0; i < E; ++i) out.set(i, o[i]);
-        out.store_nt(p);
+        yu[j].load(yr);
+        su[j].load(sr);
+        if (RES && ds) eu[j].load(er);
       } else {
+        yu[j].zero();
+        su[j].zero();
+        eu[j].zero();
 #pragma unroll
         for (int i = 0; i < E; ++i)
-          if (i < n) Elem<T>::store(p + i, o[i]);
+          if (i < n) {
+            yu[j].set(i, Elem<TY>::load(yr + i));
+            su[j].set(i, Elem<TS>::load(sr + i));
+            if (RES && ds) eu[j].set(i, Elem<TS>::load(er + i));
+          }
       }
-    };
-    if constexpr (RES) {
-      if (dres) put(dres + row * a.pdr + c0);
-      if (dx && a.drop.rng) drop_unit<E>(d, (uint32_t)c0, (uint32_t)row, o);
+      mean[j] = a.mean[row];
+      rstd[j] = a.rstd[row];
     }
-    if (!RES || dx) put(dx + row * a.pdx + c0);
+    if (threadIdx.x < 16 * R) {
+      part = make_float2(sum16(part.x), sum16(part.y));
+      if (threadIdx.x % 16 == 0) rows[turn][threadIdx.x / 16] = part;
+    }
+    __syncthreads();                                     // (the other half of `rows` was read before the barrier in between)
+#pragma unroll
+    for (int j = 0; j < R; ++j) {
+      const int64_t row = first + j;
+      if (row >= r1) break;
+      const float d1 = rows[turn][j].x * inv, d2 = rows[turn][j].y * inv;
+      float o[E];
+#pragma unroll
+      for (int i = 0; i < E; ++i) {
+        const float v = yu[j].get(i), h = (su[j].get(i) - mean[j]) * rstd[j];
+        ag[i] = fmaf(v, h, ag[i]);
+        ab[i] += v;
+        o[i] = rstd[j] * (v * gm[i] - d1 - h * d2);
+        if (RES && ds) o[i] += eu[j].get(i);
+      }
+      const auto put = [&](auto *p) __attribute__((always_inline)) {
+        using T = std::remove_pointer_t<decltype(p)>;
+        if (all) {
+          Unit<T, E> out;
+#pragma unroll
+          for (int i = 0; i < E; ++i) out.set(i, o[i]);
+          out.store_nt(p);
+        } else {
+#pragma unroll
+          for (int i = 0; i < E; ++i)
+            if (i < n) Elem<T>::store(p + i, o[i]);
+        }
+      };
+      if constexpr (RES) {
+        if (dres) put(dres + row * a.pdr + c0);
+        if (dx && a.drop.rng) drop_unit<E>(d, (uint32_t)c0, (uint32_t)row, o);
+      }
+      if (!RES || dx) put(dx + row * a.pdx + c0);
+    }
   }
   if (!a.partial) return;
 #pragma unroll
@@ -592,24 +613,28 @@ __global__ __launch_bounds__(256) void norm_bwd_wide_kernel(const TY *dy, const 
     }
 }
 
-// The strips' sums, 2 C columns of them: a block has sixteen columns and 64 threads for each, every 64th strip a thread; the threads' sums are added
-// in their order by halves.
+// The strips' sums, 2 C columns of them: a block has 1024 / SLICES columns, a thread every SLICES-th strip of one; the threads' sums are added
+// sixteen at a time, the same way at every call.
+template <int SLICES>
 __global__ __launch_bounds__(1024) void norm_fold_kernel(const float *partial, int strips, int64_t C, float *dgamma, float *dbeta) {
-  __shared__ float part[64][17];
-  const int col = threadIdx.x & 15, slice = threadIdx.x >> 4;
-  const int64_t c = (int64_t)blockIdx.x * 16 + col;
+  constexpr int COLS = 1024 / SLICES;
+  __shared__ float part[SLICES][COLS + 1];
+  const int col = threadIdx.x % COLS, slice = threadIdx.x / COLS;
+  const int64_t c = (int64_t)blockIdx.x * COLS + col;
   float v = 0.0f;
   if (c < 2 * C) {
 #pragma unroll 4
-    for (int k = slice; k < strips; k += 64) v += partial[k * 2 * C + c];
+    for (int k = slice; k < strips; k += SLICES) v += partial[k * 2 * C + c];
   }
   part[slice][col] = v;
   __syncthreads();
-  // thread (column, slice) of one wave: sixteen lanes' worth of slices at a time
-  if (threadIdx.x < 256) {
+  if (threadIdx.x < COLS * 16) {
     const int cc = threadIdx.x >> 4, k = threadIdx.x & 15;
-    const float t = sum16((part[k][cc] + part[k + 16][cc]) + (part[k + 32][cc] + part[k + 48][cc]));
-    const int64_t o = (int64_t)blockIdx.x * 16 + cc;
+    float t = part[k][cc];
+#pragma unroll
+    for (int q = 1; q < SLICES / 16; ++q) t += part[k + 16 * q][cc];
+    t = sum16(t);
+    const int64_t o = (int64_t)blockIdx.x * COLS + cc;
     if (k == 0 && o < 2 * C) {
       if (o < C) {
         if (dgamma) dgamma[o] = t;
@@ -803,8 +828,13 @@ chn_status norm_bwd(const chn_array *dy, const chn_array *ds, const chn_array *s
   }
 #undef CHN_GO
   CHN_TRY(check_launch(what));
-  if (a.partial)
-    hipLaunchKernelGGL(norm_fold_kernel, dim3((unsigned)((2 * a.C + 15) / 16)), dim3(1024), 0, st, a.partial, (int)strips, a.C, floats_out(dgamma), floats_out(dbeta));
+  if (a.partial) {
+    // (64 columns a block for few strips, sixteen for many: 99 x 20011 with 25 strips 6.0 us with sixteen)
+    if (strips <= 64)
+      hipLaunchKernelGGL(norm_fold_kernel<16>, dim3((unsigned)((2 * a.C + 63) / 64)), dim3(1024), 0, st, a.partial, (int)strips, a.C, floats_out(dgamma), floats_out(dbeta));
+    else
+      hipLaunchKernelGGL(norm_fold_kernel<64>, dim3((unsigned)((2 * a.C + 15) / 16)), dim3(1024), 0, st, a.partial, (int)strips, a.C, floats_out(dgamma), floats_out(dbeta));
+  }
   return check_launch(what);
 }
 

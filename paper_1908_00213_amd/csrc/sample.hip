@@ -159,21 +159,28 @@ __device__ __forceinline__ float least_logit(const Weights &wt, float t, float m
   return logit_of(b);
 }
 
-__device__ __forceinline__ u64 wave_sum_u64(u64 v) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
-  return v;
+// v of the lane that CTRL names, 0 where there is none (or where a row of sixteen lanes is not in ROWS)
+template <int CTRL, int ROWS>
+__device__ __forceinline__ u64 dpp_u64(u64 v) {
+  const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)v, CTRL, ROWS, 0xf, false);
+  const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)(v >> 32), CTRL, ROWS, 0xf, false);
+  return (u64)hi << 32 | lo;
 }
-// Sum over the lanes up to this one.
+__device__ __forceinline__ u64 lane_u64(u64 v, int lane) {
+  return (u64)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(v >> 32), lane) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)v, lane);
+}
+// Sum over the lanes up to this one, exchanged inside the registers: within rows of sixteen lanes, then each row's last lane to the
+// next row, then the first half's to the second.  (By shuffles through LDS twelve of these in a draw took 4 us more.)
 __device__ __forceinline__ u64 wave_upto_u64(u64 v) {
-  const int lane = threadIdx.x & 63;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const u64 other = __shfl_up(v, o, 64);
-    if (lane >= o) v += other;
-  }
+  v += dpp_u64<0x111, 0xf>(v);    // row_shr 1, 2, 4, 8
+  v += dpp_u64<0x112, 0xf>(v);
+  v += dpp_u64<0x114, 0xf>(v);
+  v += dpp_u64<0x118, 0xf>(v);
+  v += dpp_u64<0x142, 0xa>(v);    // row_bcast 15 into rows 1 and 3
+  v += dpp_u64<0x143, 0xc>(v);    // row_bcast 31 into rows 2 and 3
   return v;
 }
+__device__ __forceinline__ u64 wave_sum_u64(u64 v) { return lane_u64(wave_upto_u64(v), 63); }
 
 // Sum over the threads before this one; *all: over all of them.
 __device__ __forceinline__ u64 block_before_u64(u64 v, Shared &sh, u64 *all) {
@@ -385,7 +392,7 @@ __device__ __forceinline__ void locate(const Span<T> &span, Shared &sh, u64 star
   if (tail) span.behind([&](float z, uint32_t i) { sum += W(z, i); });
   sum = wave_sum_u64(sum);
   before = from + block_before_u64(lane == 0 ? sum : 0, sh, &all);
-  before = __shfl(before, 0, 64);
+  before = lane_u64(before, 0);
   if (!(before <= target && target < before + sum)) return;
   // one wave: its units in order, 64 at a time, then the tokens behind the last unit
   constexpr int E = Span<T>::E;
@@ -406,7 +413,7 @@ __device__ __forceinline__ void locate(const Span<T> &span, Shared &sh, u64 star
         at += w[i];
       }
     }
-    before += __shfl(upto, 63, 64);
+    before += lane_u64(upto, 63);
   }
   if (tail && wave == kWaves - 1) {
     const int i = span.whole * E + lane;
@@ -486,7 +493,8 @@ __device__ __forceinline__ int bin_of_kth(Shared &sh, const Bins &few, const flo
 __device__ __forceinline__ void draw_small(Shared &sh, int M, const Asked &q, const Weights &wt, int V, const Put &put) {
   sort_small(sh, M);
   const Rank r = (int)threadIdx.x < M && !(q.k > 0 && (int64_t)threadIdx.x >= q.k) ? sh.sorted[threadIdx.x] : 0;
-  const double e = r ? wt.exponential(logit_of((uint32_t)(r >> 32))) : 0.0;
+  const float v = logit_of((uint32_t)(r >> 32));
+  const double e = r == 0 ? 0.0 : !q.inside() ? wt.exponential(v) : v >= wt.zero(q.t) ? wt.near(v) : 0.0;   // (the ends ask for the lightest)
   const u64 w = wt.of(e);
   bool kept = r != 0;
   if (q.p < 1.0f) {
@@ -563,7 +571,7 @@ __device__ __forceinline__ void draw_whole(const Span<T> &row, Shared &sh, const
       u64 all;
       block_before_u64((u64)have, sh, &all);
       if ((u64)q.k >= all) continue;
-      least = -wave_max(-least);
+      least = -max64(-least);
       if (lane == 0) sh.fmin[wave] = least;
       __syncthreads();
 #pragma unroll
@@ -624,7 +632,7 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(const T *logits, Sampl
   // the largest logit, the threads' own, and the smallest of those
   float mine = -INFINITY;
   row.each([&](float z, uint32_t) { mine = fmaxf(mine, z); });
-  const float wmax = wave_max(mine), wmin = -wave_max(mine > -INFINITY ? -mine : -INFINITY);
+  const float wmax = max64(mine), wmin = -max64(mine > -INFINITY ? -mine : -INFINITY);
   if (lane == 0) {
     sh.fmax[wave] = wmax;
     sh.fmin[wave] = wmin;
