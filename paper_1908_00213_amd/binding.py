@@ -266,6 +266,13 @@ def _ws(t):
         return t._chn_ws
 
 
+def _ws_here(t):
+    """The same for calls whose arrays have to lie on the current device."""
+    if t is not None and t.get_device() != (_raw_device() if _raw_device is not None else torch.cuda.current_device()):
+        raise ValueError("the workspace does not lie on the current device")
+    return _ws(t)
+
+
 def version():
     return lib().chn_version()
 
@@ -605,7 +612,7 @@ def layer_norm_bwd_workspace_bytes(x):
 
 
 def layer_norm_bwd(dy, x, mean, rstd, dx, gamma=None, dgamma=None, dbeta=None, ws=None, stream=None):
-    p, n = _ws(ws)
+    p, n = _ws_here(ws)
     _check(lib().chn_layer_norm_bwd(*_here(dy, x, mean, rstd, gamma, dx, dgamma, dbeta), p, n, _stream() if stream is None else stream))
     return dx
 
@@ -620,7 +627,7 @@ def residual_norm_fwd(x, residual, s, y, gamma=None, beta=None, eps=1e-5, mean=N
 
 def residual_norm_bwd(dy, ds, s, mean, rstd, dresidual, dx, gamma=None, dgamma=None, dbeta=None, ratio=0.0, rng=None, site=0, ws=None, stream=None):
     """dresidual and dx from the gradients dy of y and ds of s (or None)."""
-    p, n = _ws(ws)
+    p, n = _ws_here(ws)
     a = _here(dy, ds, s, mean, rstd, gamma, rng, dresidual, dx, dgamma, dbeta)
     _check(lib().chn_residual_norm_bwd(*a[:6], float(ratio), a[6], int(site), *a[7:], p, n, _stream() if stream is None else stream))
     return dx
@@ -632,7 +639,7 @@ def sample_workspace_bytes(logits):
 
 def sample(logits, u, out, temperature=None, top_k=None, top_p=None, min_p=None, ws=None, stream=None):
     """out[n]: a token of row n, drawn by u[n]; parameters are tensors of one value for each row (stride 0: one for all), None: not used."""
-    p, n = _ws(ws)
+    p, n = _ws_here(ws)
     _check(lib().chn_sample(*_here(logits, u, temperature, top_k, top_p, min_p, out), p, n, _stream() if stream is None else stream))
     return out
 

@@ -55,7 +55,7 @@ __global__ __launch_bounds__(G > 256 ? G : 256) void norm_fwd_rows_kernel(const 
   const int C = (int)a.C, whole = C / E, left = C - whole * E;
   const float inv = 1.0f / (float)C;
   const int g = threadIdx.x % G;
-  int64_t row = (int64_t)blockIdx.x * GROUPS;
+  int64_t row = block_number() * GROUPS;
   if constexpr (G == 64) row += __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
   else if constexpr (G < 64) row += threadIdx.x / G;
   if (row >= a.N) return;                                // (groups that share a block meet at no barrier)
@@ -155,7 +155,8 @@ __global__ __launch_bounds__(1024) void norm_fwd_wide_kernel(const TX *x, const 
   constexpr int E = unit_elements<TX, TY, TS>();
   __shared__ float2 smem[32];
   const float inv = 1.0f / (float)a.C;
-  const int64_t row = blockIdx.x, whole = a.C / E;
+  const int64_t row = block_number(), whole = a.C / E;
+  if (row >= a.N) return;
   const TX *xr = x + row * a.px;
   TY *yr = y + row * a.py;
   TS *sr = RES ? s + row * a.ps : nullptr;
@@ -479,7 +480,8 @@ template <typename TY, typename TS>
 __global__ __launch_bounds__(256) void norm_bwd_sums_kernel(const TY *dy, const TS *s, NormBwdArgs a) {
   constexpr int E = unit_elements<TY, TS>();
   __shared__ float2 smem[8];
-  const int64_t row = blockIdx.x, units = (a.C + E - 1) / E, per = (units + a.segments - 1) / a.segments;
+  const int64_t row = (int64_t)blockIdx.z * gridDim.x + blockIdx.x, units = (a.C + E - 1) / E, per = (units + a.segments - 1) / a.segments;
+  if (row >= a.N) return;
   const int64_t u0 = blockIdx.y * per, u1 = u0 + per < units ? u0 + per : units;
   const TY *yr = dy + row * a.pdy;
   const TS *sr = s + row * a.ps;
@@ -675,14 +677,14 @@ void launch_fwd(const TX *x, const TS *residual, TS *s, TY *y, const NormArgs &a
   constexpr int E = unit_elements<TX, TY, TS>();
   const int64_t held = a.C / E * E;                      // (the elements behind the last whole unit come on top)
 #define CHN_ROWS(G, KE)                                                                                                             \
-  hipLaunchKernelGGL((norm_fwd_rows_kernel<TX, TY, TS, RES, G, KE>), dim3((unsigned)((a.N + (G < 256 ? 256 / G : 1) - 1) / (G < 256 ? 256 / G : 1))), \
+  hipLaunchKernelGGL((norm_fwd_rows_kernel<TX, TY, TS, RES, G, KE>), grid_of((a.N + (G < 256 ? 256 / G : 1) - 1) / (G < 256 ? 256 / G : 1)), \
                      dim3(G > 256 ? G : 256), 0, st, x, residual, s, y, a)
   if (held <= 16 * 16) CHN_ROWS(16, 16);
   else if (held <= 64 * 16) CHN_ROWS(64, 16);
   else if (held <= 256 * 16) CHN_ROWS(256, 16);
   else if (held <= 1024 * 16) CHN_ROWS(1024, 16);
   else if (held <= 1024 * 32) CHN_ROWS(1024, 32);
-  else hipLaunchKernelGGL((norm_fwd_wide_kernel<TX, TY, TS, RES>), dim3((unsigned)a.N), dim3(1024), 0, st, x, residual, s, y, a);
+  else hipLaunchKernelGGL((norm_fwd_wide_kernel<TX, TY, TS, RES>), grid_of(a.N), dim3(1024), 0, st, x, residual, s, y, a);
 #undef CHN_ROWS
 }
 
@@ -767,7 +769,7 @@ int64_t launch_bwd(const TY *dy, const TS *s, const TS *ds, TS *dres, TX *dx, No
   if (a.C <= kHeld) CHN_ROWS(512, 16, 512);
 #undef CHN_ROWS
   if (a.N > 0)
-    hipLaunchKernelGGL((norm_bwd_sums_kernel<TY, TS>), dim3((unsigned)a.N, (unsigned)a.segments), dim3(256), 0, st, dy, s, a);
+    hipLaunchKernelGGL((norm_bwd_sums_kernel<TY, TS>), dim3(grid_of(a.N).x, (unsigned)a.segments, grid_of(a.N).y), dim3(256), 0, st, dy, s, a);
   hipLaunchKernelGGL((norm_bwd_wide_kernel<TX, TY, TS, RES>), dim3((unsigned)((a.C + 256 * E - 1) / (256 * E)), (unsigned)a.strips), dim3(256), 0, st,
                      dy, s, ds, dres, dx, a);
   return a.strips;

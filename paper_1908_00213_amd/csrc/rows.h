@@ -10,6 +10,13 @@
 namespace chn {
 #if defined(__HIPCC__)
 
+// A grid of n blocks of up to 1024 threads each: a launch takes fewer than 2^32 threads along a dimension, so rows of blocks beyond 2^20.
+inline dim3 grid_of(int64_t n) {
+  const int64_t x = n < (1 << 20) ? n : (1 << 20);
+  return dim3((unsigned)x, (unsigned)((n + x - 1) / x));
+}
+__device__ __forceinline__ int64_t block_number() { return (int64_t)blockIdx.y * gridDim.x + blockIdx.x; }
+
 // elements of a unit: as many as the narrowest type has in 16 bytes
 template <typename... T>
 constexpr int unit_elements() {

@@ -625,7 +625,8 @@ __device__ __forceinline__ void start(Shared &sh) {
 template <typename T>
 __global__ __launch_bounds__(kThreads) void sample_kernel(const T *logits, SampleArgs a) {
   __shared__ Shared sh;
-  const int64_t n = blockIdx.x;
+  const int64_t n = block_number();
+  if (n >= a.N) return;
   const Span<T> row(logits + n * a.pitch, a.V, 0, a.V);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const Put put{a, n};
@@ -984,9 +985,9 @@ chn_status check_row_parameter(const chn_array *v, const char *name, int64_t n, 
 template <typename T>
 void launch(const chn_array *logits, SampleArgs &a, hipStream_t st) {
   const T *z = static_cast<const T *>(logits->data);
-  const dim3 rows((unsigned)a.N), threads(kThreads);
+  const dim3 threads(kThreads);
   if (a.chunks == 1) {
-    hipLaunchKernelGGL((sample_kernel<T>), rows, threads, 0, st, z, a);
+    hipLaunchKernelGGL((sample_kernel<T>), grid_of(a.N), threads, 0, st, z, a);
     return;
   }
   const int units = a.V / Span<T>::E;
@@ -997,7 +998,7 @@ void launch(const chn_array *logits, SampleArgs &a, hipStream_t st) {
   hipLaunchKernelGGL((sample_maxima_kernel<T>), grid, threads, 0, st, z, a);
   hipLaunchKernelGGL((sample_bins_kernel<T>), grid, threads, 0, st, z, a);
   if (a.top_p) hipLaunchKernelGGL((sample_border_kernel<T>), grid, threads, 0, st, z, a);
-  hipLaunchKernelGGL((sample_draw_kernel<T>), rows, threads, 0, st, z, a);
+  hipLaunchKernelGGL((sample_draw_kernel<T>), dim3((unsigned)a.N), threads, 0, st, z, a);
 }
 
 chn_status check_row_float(const chn_array *v, const char *name, int64_t n, const float **data, int64_t *stride) {
@@ -1045,9 +1046,9 @@ chn_status chn_sample(const chn_array *logits, const chn_array *u, const chn_arr
   if (V > (1LL << 30) || a.N > 0x7fffffffLL) return fail(CHN_ERR_SHAPE, "sample: more than 2^30 tokens or 2^31 - 1 rows");
   if (a.N == 0) return CHN_OK;
   a.V = (int)V;
-  // the sum of V weights of at most 2^shift fits 63 bits; 46 bits leave nothing to tell the draw from the exact one's
+  // the sum of V weights of at most 2^shift is at most 2^63; 46 bits leave nothing to tell the draw from the exact one's
   a.shift = 46;
-  while (a.shift > 0 && (V >> (63 - a.shift)) > 0) --a.shift;
+  while ((V - 1) >> (63 - a.shift) > 0) --a.shift;
   a.out = out->data;
   a.out64 = out->dtype == CHN_I64;
   hipStream_t st = as_stream(stream);

@@ -286,3 +286,30 @@ def test_arrays_of_the_host_are_refused():
         B.layer_norm_fwd(torch.ones(4, 8, device="cuda"), torch.empty(4, 8, device="cuda"), torch.ones(8))
     with pytest.raises(ValueError):
         B.sample(x.cuda(), torch.ones(4), torch.empty(4, dtype=torch.int64, device="cuda"))
+
+
+def test_more_rows_than_a_line_of_the_grid_has_blocks():
+    n, c = 2 ** 24 + 37, 3                               # sixteen rows to a block
+    g = torch.Generator(device="cuda").manual_seed(4)
+    x = torch.randn(n, c, device="cuda", generator=g)
+    y, mean, rstd = torch.empty_like(x), torch.empty(n, device="cuda"), torch.empty(n, device="cuda")
+    B.layer_norm_fwd(x, y, None, None, 1e-2, mean, rstd)
+    d = x.double()
+    m = d.mean(1, keepdim=True)
+    r = 1.0 / torch.sqrt(((d - m) ** 2).mean(1, keepdim=True) + 1e-2)
+    # three terms: a handful of roundings of values of at most 1 / sqrt(eps) times the spread
+    assert float((y - (d - m) * r).abs().max()) < 16 * U * 10 * float(x.abs().max())
+    z = torch.empty_like(x)
+    B.dropout(x, z, 0.5, rng_state(), SITE)
+    tail = torch.arange(n - 5, n)
+    for row in tail.tolist() + [0, 2 ** 20, 2 ** 24]:
+        words = R.philox4x32([0, row, OFFSET, SITE], [SEED & R.LOW, SEED >> 32], 7)[:3]
+        want = [float(v) * 2 if w >= 2 ** 31 else 0.0 for v, w in zip(x[row].tolist(), words)]
+        assert z[row].tolist() == want, row
+
+
+def test_a_workspace_of_the_host_is_refused():
+    x, v = torch.ones(4, 8, device="cuda"), torch.ones(8, device="cuda")
+    m = torch.ones(4, device="cuda")
+    with pytest.raises(ValueError):
+        B.layer_norm_bwd(x, x, m, m, torch.empty_like(x), v, v.clone(), v.clone(), ws=torch.empty(1 << 16, dtype=torch.uint8))

@@ -146,11 +146,12 @@ def test_tokens_come_as_often_as_their_weights_say():
     assert np.all(np.abs(counts - n * p) < 5 * np.sqrt(n * p * (1 - p)))
 
 
-def test_sample_on_a_stream_and_in_a_graph():
-    z, u = logits(5, 30000, "f32", 10).contiguous(), torch.rand(5, device="cuda")
-    k = torch.full((5,), 20, device="cuda", dtype=torch.int32)
+@pytest.mark.parametrize("v", [30000, 100000])           # a block for a row, and rows in chunks
+def test_sample_on_a_stream_and_in_a_graph(v):
+    z, u = logits(5, v, "f32", 10).contiguous(), torch.rand(5, device="cuda")
+    k = torch.tensor([20, 0, 20, 0, 1], device="cuda", dtype=torch.int32)
     want = []
-    inputs = [(logits(5, 30000, "f32", 20 + i).contiguous(), torch.rand(5, device="cuda")) for i in range(3)]
+    inputs = [(logits(5, v, "f32", 20 + i).contiguous(), torch.rand(5, device="cuda")) for i in range(3)]
     for zi, ui in inputs:
         want.append(draw(zi, ui, top_k=k))
     side = torch.cuda.Stream()
@@ -217,3 +218,15 @@ def test_two_calls_at_once_have_their_own_workspaces():
                 B.sample(z, u, o, top_p=p[:z.shape[0]], ws=w)
     torch.cuda.synchronize()
     assert np.array_equal(outs[0].cpu().numpy(), alone[0]) and np.array_equal(outs[1].cpu().numpy(), alone[1])
+
+
+def test_a_row_for_every_block_beyond_a_line_of_the_grid():
+    n = 2 ** 20 + 3
+    z = torch.randn(n, 3, device="cuda", generator=torch.Generator(device="cuda").manual_seed(2))
+    u = torch.rand(n, device="cuda", generator=torch.Generator(device="cuda").manual_seed(3))
+    out = torch.empty(n, dtype=torch.int32, device="cuda")
+    B.sample(z, u, out)
+    w = torch.exp(z.double() - z.double().max(1, keepdim=True).values)
+    cum = torch.cumsum(w, 1)
+    want = (cum > u.double()[:, None] * cum[:, -1:]).to(torch.uint8).argmax(1).int()
+    assert torch.equal(out, want)
