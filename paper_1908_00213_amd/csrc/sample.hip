@@ -21,6 +21,7 @@ namespace {
 typedef unsigned long long u64;
 constexpr int kThreads = 1024, kWaves = kThreads / 64;
 constexpr int kBins = 2048;          // two for each thread
+constexpr int kFewBins = 256;        // for a bound: coarser, and read by every wave
 constexpr int kSmall = 1024;         // tokens that are ordered by comparing each with each
 constexpr int kMaxChunks = 32, kMaxParts = 4096;
 
@@ -78,7 +79,7 @@ struct Shared {
   u64 list[kSmall];                  // the small set as it was gathered
   u64 waves[kWaves];
   double powers[32];                 // kPowers: 64 banks' worth, no two lanes meet in one unless they read the same number
-  float fmax[kWaves], fmin[kWaves], part[kThreads];
+  float fmax[kWaves], fmin[kWaves];
   u64 result, above;
   int count, slot;
 };
@@ -241,6 +242,26 @@ struct Span {
       }
     }
   }
+  // f(unit, index of its first token) for every unit of the block
+  template <int U = 4, typename F>
+  __device__ __forceinline__ void units(F f) const {
+    Unit<T, E> t[U];
+    int u = first + (int)(threadIdx.x & 63);
+#pragma unroll
+    for (int j = 0; j < U; ++j)
+      if (u + 64 * j < end) t[j].load(z + (u + 64 * j) * E);
+    for (; u - (int)(threadIdx.x & 63) < end; u += 64 * U) {
+#pragma unroll
+      for (int j = 0; j < U; ++j) {
+        const int at = u + 64 * j;
+        if (at < end) {
+          const Unit<T, E> now = t[j];
+          if (at + 64 * U < end) t[j].load(z + (at + 64 * U) * E);
+          f(now, (uint32_t)(at * E));
+        }
+      }
+    }
+  }
   template <typename F>
   __device__ __forceinline__ void behind(F f) const {
     const int i = whole * E + (int)(threadIdx.x & 63);
@@ -255,12 +276,13 @@ struct Span {
 };
 
 // Bins of equal width below the largest logit.
+template <int N = kBins>
 struct Bins {
   float best, scale;
-  __device__ __forceinline__ Bins(float best_, float width) : best(best_), scale((float)kBins / width) {
+  __device__ __forceinline__ Bins(float best_, float width) : best(best_), scale((float)N / width) {
     if (!(scale < INFINITY)) scale = 0.0f;               // (all in the first bin)
   }
-  __device__ __forceinline__ int of(float z) const { return z == best ? 0 : (int)fminf((best - z) * scale, (float)(kBins - 1)); }   // (NaN: the last)
+  __device__ __forceinline__ int of(float z) const { return z == best ? 0 : (int)fminf((best - z) * scale, (float)(N - 1)); }   // (NaN: the last)
 };
 
 // The bin in which the sum over bins, from the first on, reaches the target (at least 1 and at most the whole sum); the sum before it in
@@ -301,6 +323,22 @@ __device__ __forceinline__ void gather(Shared &sh, Rank r) {
   if (at < kSmall) sh.list[at] = r;
 }
 
+// Those of a unit's tokens for which `take`: a place for all of a lane's at once, so that the waves wait for the counter once a unit.
+template <int E, typename FU, typename F>
+__device__ __forceinline__ void gather_unit(Shared &sh, FU logit, uint32_t first, F take) {
+  uint32_t hits = 0;
+#pragma unroll
+  for (int i = 0; i < E; ++i) hits |= take(logit(i)) ? 1u << i : 0u;
+  if (hits == 0) return;
+  int at = atomicAdd(&sh.count, __popc(hits));
+#pragma unroll
+  for (int i = 0; i < E; ++i)
+    if (hits >> i & 1) {
+      if (at < kSmall) sh.list[at] = rank_of(logit(i), first + i);
+      ++at;
+    }
+}
+
 // sh.list[0 .. M) into sh.sorted, descending, with every token's place found by comparing it with all the others; P threads share a token.
 __device__ __forceinline__ void sort_small(Shared &sh, int M) {
   int size = 1;
@@ -309,6 +347,7 @@ __device__ __forceinline__ void sort_small(Shared &sh, int M) {
   const Rank mine = me < M ? sh.list[me] : 0;
   int place = 0;
   if (me < M)
+#pragma unroll 4
     for (int j = part; j < M; j += parts) place += sh.list[j] > mine;
   for (int o = 1; o < parts; o <<= 1) place += __shfl_xor(place, o, 64);
   if (me < M && part == 0) sh.sorted[place] = mine;
@@ -330,7 +369,7 @@ __device__ __forceinline__ Rank border_in_list(Shared &sh, int M, u64 before, u6
 
 // The rank from which on the sum of W over the row's tokens of at least `border` reaches the target.  W(logit): a token's share.
 template <typename R, typename FW>
-__device__ __forceinline__ Rank find_border(const R &row, Shared &sh, const Bins &bins, Rank border, u64 target, FW W) {
+__device__ __forceinline__ Rank find_border(const R &row, Shared &sh, const Bins<> &bins, Rank border, u64 target, FW W) {
   // (sh.bins holds the sums by bin)
   const int bin = crossing_bin(sh, target);
   const u64 before = sh.above;
@@ -423,6 +462,46 @@ __device__ __forceinline__ void locate(const Span<T> &span, Shared &sh, u64 star
   }
 }
 
+// The same for a row whose units the threads hold, U each at most: the waves' running sums unit by unit, then the token.
+template <int U, typename T, int E, typename FT, typename FW, typename FP>
+__device__ __forceinline__ void locate_held(const Span<T> &row, Shared &sh, const Unit<T, E> (&held)[U], FT point, FW W, FP put) {
+  const int lane = threadIdx.x & 63;
+  u64 own[U], upto[U], sum = 0, all, behind = 0;
+  const int u0 = row.first + lane, last = row.whole * E + lane;
+#pragma unroll
+  for (int j = 0; j < U; ++j) {
+    own[j] = 0;
+    if (u0 + 64 * j < row.end) {
+#pragma unroll
+      for (int i = 0; i < E; ++i) own[j] += W(held[j].get(i), (uint32_t)((u0 + 64 * j) * E + i));
+    }
+  }
+  row.behind([&](float z, uint32_t i) { behind = W(z, i); });
+#pragma unroll
+  for (int j = 0; j < U; ++j) {
+    upto[j] = sum + wave_upto_u64(own[j]);
+    sum = lane_u64(upto[j], 63);
+  }
+  const u64 upto_behind = sum + wave_upto_u64(behind);
+  sum = lane_u64(upto_behind, 63);
+  const u64 before = lane_u64(block_before_u64(lane == 0 ? sum : 0, sh, &all), 0), target = point(all);
+  if (!(before <= target && target < before + sum)) return;
+#pragma unroll
+  for (int j = 0; j < U; ++j) {
+    u64 at = before + upto[j] - own[j];
+    if (at <= target && target < at + own[j]) {
+#pragma unroll
+      for (int i = 0; i < E; ++i) {
+        const u64 w = W(held[j].get(i), (uint32_t)((u0 + 64 * j) * E + i));
+        if (at <= target && target < at + w) put((u0 + 64 * j) * E + i);
+        at += w;
+      }
+    }
+  }
+  const u64 at = before + upto_behind - behind;
+  if (at <= target && target < at + behind) put(last);
+}
+
 // What the caller asks of a row.
 struct Asked {
   float t, u, p, minp;
@@ -456,7 +535,8 @@ struct Put {
 };
 
 // A logit such that at least those in bins up to `last` are not below it.
-__device__ __forceinline__ float bound_of(const Bins &few, int last) {
+template <int N>
+__device__ __forceinline__ float bound_of(const Bins<N> &few, int last) {
   // the smallest key of these bins, by search: 64 at a time
   uint32_t a = 0x00800000u, b = key_of(few.best);
   while (a < b) {
@@ -475,18 +555,24 @@ __device__ __forceinline__ float bound_of(const Bins &few, int last) {
   return logit_of(b);
 }
 
-// The last bin of those that hold the k largest of n values (-inf: none), -1 if there are fewer than k.  sh.bins has to be clear.
-__device__ __forceinline__ int bin_of_kth(Shared &sh, const Bins &few, const float *values, int n, int64_t k) {
-  for (int i = threadIdx.x; i < n; i += kThreads)
-    if (values[i] > -INFINITY) atomicAdd(&sh.bins[few.of(values[i])], 1ull);
-  if (threadIdx.x == 0) sh.slot = -1;
+// The last bin of those that hold the k largest of the values that the threads add, -1 if there are fewer than k: 256 bins of counts, which
+// every wave reads and sums by itself, so that one barrier is enough.  sh.bins has to be clear, and is not afterwards.
+template <typename F>
+__device__ __forceinline__ int bin_of_kth(Shared &sh, int64_t k, F add) {
+  uint32_t *counts = reinterpret_cast<uint32_t *>(sh.bins);
+  add([&](int bin) { atomicAdd(&counts[bin], 1u); });
   __syncthreads();
-  const u64 x = sh.bins[2 * threadIdx.x], y = sh.bins[2 * threadIdx.x + 1];
-  u64 all;
-  const u64 before = block_before_u64(x + y, sh, &all);
-  if (before < (u64)k && (u64)k <= before + x + y) sh.slot = 2 * threadIdx.x + ((u64)k > before + x ? 1 : 0);
-  __syncthreads();
-  return sh.slot;
+  const int lane = threadIdx.x & 63;
+  static_assert(kFewBins == 256, "four for each lane");
+  const uint4 c = *reinterpret_cast<const uint4 *>(counts + 4 * lane);
+  const u64 upto = wave_upto_u64((u64)(c.x + c.y + c.z + c.w));
+  const u64 enough = __ballot(upto >= (u64)k);
+  if (enough == 0) return -1;
+  const int l = __ffsll((long long)enough) - 1;
+  const uint32_t x = __builtin_amdgcn_readlane(c.x, l), y = __builtin_amdgcn_readlane(c.y, l), z = __builtin_amdgcn_readlane(c.z, l),
+                 w = __builtin_amdgcn_readlane(c.w, l);
+  const uint32_t need = (uint32_t)((u64)k - (lane_u64(upto, l) - (x + y + z + w)));
+  return 4 * l + (need <= x ? 0 : need <= x + y ? 1 : need <= x + y + z ? 2 : 3);
 }
 
 // The draw from sh.list[0 .. M): every token that top-k (with top-p and min-p) or min-p alone can keep.
@@ -519,8 +605,8 @@ __device__ __forceinline__ void draw_small(Shared &sh, int M, const Asked &q, co
     const uint32_t index = me < M ? index_of(sh.list[me]) : 0;
     u64 before = 0;
     if (me < M)
-      for (int j = part; j < M; j += parts)
-        if (index_of(sh.list[j]) < index) before += sh.weight[j];
+#pragma unroll 4
+      for (int j = part; j < M; j += parts) before += index_of(sh.list[j]) < index ? sh.weight[j] : 0;
     for (int o = 1; o < parts; o <<= 1) before += __shfl_xor(before, o, 64);
     if (me < M && part == 0 && before <= target && target < before + sh.weight[me]) put(index);
   } else {                                               // the ends of the range: the first and the last token, however light
@@ -535,9 +621,9 @@ __device__ __forceinline__ void draw_small(Shared &sh, int M, const Asked &q, co
   }
 }
 
-// The draw from a whole row whose largest logit is known, in passes over it.
-template <typename T>
-__device__ __forceinline__ void draw_whole(const Span<T> &row, Shared &sh, const Asked &q, const Weights &wt, const Put &put) {
+// The draw from a whole row whose largest logit is known, in passes over it; `finish` makes the draw once it is known what is kept.
+template <typename T, typename FF>
+__device__ __forceinline__ void draw_whole(const Span<T> &row, Shared &sh, const Asked &q, const Weights &wt, const Put &put, FF finish) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const float best = wt.best;
   if (best == INFINITY) {                                // equal weights for the tokens that have it, none for the others
@@ -578,7 +664,7 @@ __device__ __forceinline__ void draw_whole(const Span<T> &row, Shared &sh, const
       for (int w = 0; w < kWaves; ++w) least = fminf(least, sh.fmin[w]);
       width = best - least;
     }
-    const Bins bins(best, width);
+    const Bins<> bins(best, width);
     const float zero = by_weight ? wt.zero(q.t) : -INFINITY;
     const auto share = [&](float z) -> u64 { return by_weight ? (z >= zero ? wt.of(wt.near(z)) : 0) : 1; };
     clear_bins(sh);
@@ -614,12 +700,15 @@ __device__ __forceinline__ void draw_whole(const Span<T> &row, Shared &sh, const
   }
   limit.not_below(wt.zero(q.t));
   const auto W = [&](float z, uint32_t i) -> u64 { return wt.of(limit.keeps(z, i) ? wt.near(z) : 0.0); };
-  locate<4>(row, sh, 0, [&](u64 all) { return q.point(all); }, W, put);
+  finish(W);
 }
 
-__device__ __forceinline__ void start(Shared &sh) {
+// What a kernel begins with; the next barrier makes it everybody's.
+__device__ __forceinline__ void begin(Shared &sh) {
   if (threadIdx.x < 32) sh.powers[threadIdx.x] = kPowers[threadIdx.x];
-  clear_bins(sh);
+  sh.bins[2 * threadIdx.x] = 0;
+  sh.bins[2 * threadIdx.x + 1] = 0;
+  if (threadIdx.x == 0) sh.count = 0;
 }
 
 template <typename T>
@@ -627,18 +716,38 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(const T *logits, Sampl
   __shared__ Shared sh;
   const int64_t n = block_number();
   if (n >= a.N) return;
+  const Asked q(a, n);                                   // (first, so that its loads are under way with the row's)
+  begin(sh);
   const Span<T> row(logits + n * a.pitch, a.V, 0, a.V);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const Put put{a, n};
-  // the largest logit, the threads' own, and the smallest of those
+  // the largest logit, the threads' own, and the smallest of those; the units of rows of up to four a thread stay in registers
+  constexpr int E = Span<T>::E, U = 4;
+  Unit<T, E> held[U];
+  const bool holds = row.per <= 64 * U;
   float mine = -INFINITY;
-  row.each([&](float z, uint32_t) { mine = fmaxf(mine, z); });
+  if (holds) {
+#pragma unroll
+    for (int j = 0; j < U; ++j) {
+      held[j].zero();
+      if (row.first + lane + 64 * j < row.end) held[j].load(row.z + (row.first + lane + 64 * j) * E);
+    }
+#pragma unroll
+    for (int j = 0; j < U; ++j)
+      if (row.first + lane + 64 * j < row.end) {
+#pragma unroll
+        for (int i = 0; i < E; ++i) mine = fmaxf(mine, held[j].get(i));
+      }
+    row.behind([&](float z, uint32_t) { mine = fmaxf(mine, z); });
+  } else {
+    row.each([&](float z, uint32_t) { mine = fmaxf(mine, z); });
+  }
   const float wmax = max64(mine), wmin = -max64(mine > -INFINITY ? -mine : -INFINITY);
   if (lane == 0) {
     sh.fmax[wave] = wmax;
     sh.fmin[wave] = wmin;
   }
-  start(sh);
+  __syncthreads();
   float best = sh.fmax[0], low = sh.fmin[0];
 #pragma unroll
   for (int w = 1; w < kWaves; ++w) {
@@ -649,7 +758,6 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(const T *logits, Sampl
     if (threadIdx.x == 0) put(-1);
     return;
   }
-  const Asked q(a, n);
   if (q.greedy()) {
     if (threadIdx.x == 0) sh.slot = a.V;
     __syncthreads();
@@ -666,13 +774,25 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(const T *logits, Sampl
   int M = kSmall + 1;
   if (best < INFINITY) {
     if (q.k > 0 && q.k <= kThreads) {
-      const Bins few(best, best - low);
-      sh.part[threadIdx.x] = mine;
-      const int last = bin_of_kth(sh, few, sh.part, kThreads, q.k);
+      const Bins<kFewBins> few(best, best - low);
+      const int last = bin_of_kth(sh, q.k, [&](auto add) {
+        if (mine > -INFINITY) add(few.of(mine));
+      });
       if (last >= 0) {
-        row.each([&](float z, uint32_t i) {
-          if (z > -INFINITY && few.of(z) <= last) gather(sh, rank_of(z, i));
-        });
+        const auto take = [&](float z) { return z > -INFINITY && few.of(z) <= last; };
+        if (few.of(mine) <= last) {                      // (the others hold none)
+          if (holds) {
+#pragma unroll
+            for (int j = 0; j < U; ++j)
+              if (row.first + lane + 64 * j < row.end)
+                gather_unit<E>(sh, [&](int i) { return held[j].get(i); }, (uint32_t)((row.first + lane + 64 * j) * E), take);
+          } else {
+            row.units([&](const Unit<T, E> &t, uint32_t first) { gather_unit<E>(sh, [&](int i) { return t.get(i); }, first, take); });
+          }
+          row.behind([&](float z, uint32_t i) {
+            if (take(z)) gather(sh, rank_of(z, i));
+          });
+        }
         __syncthreads();
         M = sh.count;
       }
@@ -686,7 +806,11 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(const T *logits, Sampl
     }
   }
   if (M <= kSmall) draw_small(sh, M, q, wt, a.V, put);
-  else draw_whole(row, sh, q, wt, put);
+  else draw_whole(row, sh, q, wt, put, [&](auto W) __attribute__((always_inline)) {
+    const auto point = [&](u64 all) { return q.point(all); };
+    if (holds) locate_held(row, sh, held, point, W, put);
+    else locate<4>(row, sh, 0, point, W, put);
+  });
 }
 
 // ---- rows in chunks -------------------------------------------------------------------------------------------------
@@ -742,6 +866,7 @@ struct Plan {
 
 __device__ __forceinline__ Plan plan_row(Shared &sh, const SampleArgs &a, const RowSpace &space, const Asked &q) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  begin(sh);
   float top = -INFINITY, down = INFINITY;
   for (int p = threadIdx.x; p < a.parts; p += kThreads) {
     const float m = space.maxima[p];
@@ -754,7 +879,7 @@ __device__ __forceinline__ Plan plan_row(Shared &sh, const SampleArgs &a, const 
     sh.fmax[wave] = top;
     sh.fmin[wave] = down;
   }
-  start(sh);
+  __syncthreads();
   Plan plan{kNothing, sh.fmax[0], sh.fmin[0]};
 #pragma unroll
   for (int w = 1; w < kWaves; ++w) {
@@ -781,7 +906,7 @@ __global__ __launch_bounds__(kThreads) void sample_bins_kernel(const T *logits, 
   const Weights wt(plan.best, q.t, a.shift, sh);
   float least = wt.zero(q.t);
   if (plan.way == kSums) {
-    const Bins bins(plan.best, 33.0f * q.t);
+    const Bins<> bins(plan.best, 33.0f * q.t);
     span.template each<8 / Span<T>::E>([&](float z, uint32_t) {
       if (z >= least) add_to_bin(sh, bins.of(z), z, wt.of(wt.near(z)));
     });
@@ -820,7 +945,7 @@ __global__ __launch_bounds__(kThreads) void sample_border_kernel(const T *logits
   if (plan.way != kSums) return;
   const Span<T> span = chunk_of(logits, a, n, chunk);
   const Weights wt(plan.best, q.t, a.shift, sh);
-  const Bins bins(plan.best, 33.0f * q.t);
+  const Bins<> bins(plan.best, 33.0f * q.t);
   u64 target, all, sum = 0;
   const int bin = border_bin(sh, space, q, &target);
   float least = wt.zero(q.t);
@@ -899,8 +1024,13 @@ __global__ __launch_bounds__(kThreads) void sample_draw_kernel(const T *logits, 
   bool whole = plan.way == kWhole;
   if (plan.way == kFew) {
     // the k-th largest of the parts' maxima is a bound (to the width of a bin)
-    const Bins few(plan.best, plan.best - plan.low);
-    const int last = q.k <= a.parts ? bin_of_kth(sh, few, space.maxima, a.parts, q.k) : -1;
+    const Bins<kFewBins> few(plan.best, plan.best - plan.low);
+    const int last = bin_of_kth(sh, q.k, [&](auto add) {
+      for (int p = threadIdx.x; p < a.parts; p += kThreads) {
+        const float m = space.maxima[p];
+        if (m > -INFINITY) add(few.of(m));
+      }
+    });
     whole = last < 0;
     if (!whole) {
       const float bound = bound_of(few, last);
@@ -919,7 +1049,8 @@ __global__ __launch_bounds__(kThreads) void sample_draw_kernel(const T *logits, 
     whole = space.count > kSmall;
   }
   if (whole) {
-    draw_whole(Span<T>(z, a.V, 0, a.V), sh, q, wt, put);
+    const Span<T> row(z, a.V, 0, a.V);
+    draw_whole(row, sh, q, wt, put, [&](auto W) __attribute__((always_inline)) { locate<4>(row, sh, 0, [&](u64 all) { return q.point(all); }, W, put); });
     return;
   }
   Limit limit{-INFINITY, 0};
