@@ -82,13 +82,14 @@ __device__ __forceinline__ float sum64(float v) {
   return (a + b) + (c + d);
 }
 
-// The largest over the wave, uniform.
 template <int CTRL>
 __device__ __forceinline__ float dpp_max(float v) {
   return fmaxf(v, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, true)));
 }
+__device__ __forceinline__ float max16(float v) { return dpp_max<0x140>(dpp_max<0x141>(dpp_max<0x4E>(dpp_max<0xB1>(v)))); }   // of a row of lanes
+// The largest over the wave, uniform.
 __device__ __forceinline__ float max64(float v) {
-  v = dpp_max<0x140>(dpp_max<0x141>(dpp_max<0x4E>(dpp_max<0xB1>(v))));
+  v = max16(v);
   const float a = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 0)), b = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 16));
   const float c = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 32)), d = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 48));
   return fmaxf(fmaxf(a, b), fmaxf(c, d));

@@ -31,6 +31,7 @@ struct RowSpace {
   u64 list[kSmall];                  // tokens of the border's bin
   u64 sums[kMaxChunks];              // kept weights of each chunk
   float maxima[kMaxParts];           // of parts of 64 units; the tokens behind the last unit count to the last part
+  float minima[kMaxParts];
   int count, pad[63];
 };
 
@@ -79,7 +80,7 @@ struct Shared {
   u64 list[kSmall];                  // the small set as it was gathered
   u64 waves[kWaves];
   double powers[32];                 // kPowers: 64 banks' worth, no two lanes meet in one unless they read the same number
-  float fmax[kWaves], fmin[kWaves];
+  float fmax[kWaves], fmin[kWaves], fleast[kWaves];
   u64 result, above;
   int count, slot;
 };
@@ -185,17 +186,20 @@ __device__ __forceinline__ u64 wave_sum_u64(u64 v) { return lane_u64(wave_upto_u
 
 // Sum over the threads before this one; *all: over all of them.
 __device__ __forceinline__ u64 block_before_u64(u64 v, Shared &sh, u64 *all) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const u64 upto = wave_upto_u64(v);
   __syncthreads();
   if (lane == 63) sh.waves[wave] = upto;
   __syncthreads();
-  u64 before = upto - v, sum = 0;
-#pragma unroll
-  for (int w = 0; w < kWaves; ++w) {
-    if (w < wave) before += sh.waves[w];
-    sum += sh.waves[w];
-  }
+  // every wave sums the sixteen waves' up by itself, in a row of its lanes
+  u64 w = sh.waves[lane & 15];
+  w += dpp_u64<0x111, 0xf>(w);
+  w += dpp_u64<0x112, 0xf>(w);
+  w += dpp_u64<0x114, 0xf>(w);
+  w += dpp_u64<0x118, 0xf>(w);
+  const u64 sum = lane_u64(w, 15);
+  u64 before = upto - v;
+  if (wave > 0) before += lane_u64(w, wave - 1);
   *all = sum;
   return before;
 }
@@ -219,8 +223,8 @@ struct Span {
     first = min(to, from + wave * per);
     end = min(to, first + per);
   }
-  // U units are on their way while one is worked on.  (Where one unit ends and the next begins is fixed: work on several mixed up by the
-  // compiler takes more registers than there are.)
+  // U units are on their way while one is worked on, four tokens at a time: work on more of them mixed up by the compiler takes more registers
+  // than there are.
   template <int U, typename F>
   __device__ __forceinline__ void stretch(int u0, int u1, F f) const {
     Unit<T, E> t[U];
@@ -237,7 +241,10 @@ struct Span {
           const Unit<T, E> now = t[j];
           if (at + 64 * U < u1) t[j].load(z + (at + 64 * U) * E);
 #pragma unroll
-          for (int i = 0; i < E; ++i) f(now.get(i), (uint32_t)(at * E + i));
+          for (int i = 0; i < E; ++i) {
+            if (i == 4) __builtin_amdgcn_sched_barrier(0);
+            f(now.get(i), (uint32_t)(at * E + i));
+          }
         }
       }
     }
@@ -306,11 +313,11 @@ __device__ __forceinline__ void clear_bins(Shared &sh) {
   if (threadIdx.x == 0) sh.count = 0;
   __syncthreads();
 }
-// Adds w to a bin.  Lanes that all bring the same logit (a row of equals) add once together.
-__device__ __forceinline__ void add_to_bin(Shared &sh, int bin, float z, u64 w) {
+// Adds w to a bin.  Lanes that all bring the same `tag`, which says bin and weight (equal logits, say), add once together.
+__device__ __forceinline__ void add_to_bin(Shared &sh, int bin, uint32_t tag, u64 w) {
   const u64 active = __ballot(1);
-  const uint32_t head = __builtin_amdgcn_readfirstlane(__float_as_uint(z));
-  if (__ballot(__float_as_uint(z) != head) == 0) {
+  const uint32_t head = __builtin_amdgcn_readfirstlane(tag);
+  if (__ballot(tag != head) == 0) {
     const int leader = __ffsll((long long)active) - 1;
     if ((int)(threadIdx.x & 63) == leader) atomicAdd(&sh.bins[bin], w * (u64)__popcll(active));
   } else {
@@ -365,46 +372,6 @@ __device__ __forceinline__ Rank border_in_list(Shared &sh, int M, u64 before, u6
   if (r && upto < target && target <= upto + w) sh.result = r;
   __syncthreads();
   return sh.result;
-}
-
-// The rank from which on the sum of W over the row's tokens of at least `border` reaches the target.  W(logit): a token's share.
-template <typename R, typename FW>
-__device__ __forceinline__ Rank find_border(const R &row, Shared &sh, const Bins<> &bins, Rank border, u64 target, FW W) {
-  // (sh.bins holds the sums by bin)
-  const int bin = crossing_bin(sh, target);
-  const u64 before = sh.above;
-  __syncthreads();
-  row.each([&](float z, uint32_t i) {
-    if (bins.of(z) != bin) return;
-    const Rank r = rank_of(z, i);
-    if (r != 0 && r >= border) gather(sh, r);
-  });
-  __syncthreads();
-  const int M = sh.count;
-  if (M <= kSmall) return border_in_list(sh, M, before, target, W);
-  // More than that in one bin (many equal logits): the rank's bits, eleven at a time, over the tokens that share the bits found so far.
-  Rank found = 0;
-  u64 sum = before;
-  for (int low = 53; ; low = low > 11 ? low - 11 : 0) {
-    const int width = low == 0 ? 9 : 11, high = low + width;
-    clear_bins(sh);
-    row.template each<1>([&](float z, uint32_t i) {
-      if (bins.of(z) != bin) return;
-      const Rank r = rank_of(z, i);
-      if (r == 0 || r < border || (high < 64 && (r >> high) != (found >> high))) return;
-      // (descending: the first bin has the largest ranks)
-      const int at = (1 << width) - 1 - (int)((r >> low) & ((1u << width) - 1));
-      if (low >= 32) add_to_bin(sh, at, z, W(z));        // (bits of the logit alone)
-      else atomicAdd(&sh.bins[at], W(z));
-    });
-    __syncthreads();
-    const int at = crossing_bin(sh, target - sum);
-    sum += sh.above;
-    found |= (u64)((1 << width) - 1 - at) << low;
-    __syncthreads();
-    if (low == 0) break;
-  }
-  return found;
 }
 
 // The token of a span at which the running sum of W, which is `start` before the span, passes point(its sum over the span): the wave in whose
@@ -462,6 +429,76 @@ __device__ __forceinline__ void locate(const Span<T> &span, Shared &sh, u64 star
   }
 }
 
+// The largest of the threads' first numbers and the smallest of their second and third ones, in all threads.
+__device__ __forceinline__ void extremes(Shared &sh, float &top, float &low, float &least) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  top = max64(top);
+  low = -max64(-low);
+  least = -max64(-least);
+  if (lane == 0) {
+    sh.fmax[wave] = top;
+    sh.fmin[wave] = low;
+    sh.fleast[wave] = least;
+  }
+  __syncthreads();
+  static_assert(kWaves == 16, "a row of lanes");
+  top = max16(sh.fmax[lane & 15]);
+  low = -max16(-sh.fmin[lane & 15]);
+  least = -max16(-sh.fleast[lane & 15]);
+}
+
+// The rank from which on the sum of W over the row's tokens of at least `border` reaches the target.  W(logit): a token's share.
+template <typename R, typename FW>
+__device__ __forceinline__ Rank find_border(const R &row, Shared &sh, const Bins<> &bins, Rank border, u64 target, FW W) {
+  // (sh.bins holds the sums by bin)
+  const int bin = crossing_bin(sh, target);
+  const u64 before = sh.above;
+  __syncthreads();
+  float high = -INFINITY, low = INFINITY, none = INFINITY;
+  row.each([&](float z, uint32_t i) {
+    if (bins.of(z) != bin) return;
+    const Rank r = rank_of(z, i);
+    if (r == 0 || r < border) return;
+    gather(sh, r);
+    high = fmaxf(high, z);
+    low = fminf(low, z);
+  });
+  __syncthreads();
+  const int M = sh.count;
+  if (M <= kSmall) return border_in_list(sh, M, before, target, W);
+  extremes(sh, high, low, none);
+  if (high == low) {                                     // all equal: so many of them, the first by index
+    const u64 w = W(high), nth = (target - before + w - 1) / w - 1;
+    locate<1>(row, sh, 0, [=](u64) { return nth; }, [&](float z, uint32_t i) -> u64 { return z == high && rank_of(z, i) >= border; },
+              [&](int64_t i) { sh.above = rank_of(high, (uint32_t)i); });
+    __syncthreads();
+    return sh.above;
+  }
+  // More than that in one bin (many nearly equal logits): the rank's bits, eleven at a time, over the tokens that share the bits found so far.
+  Rank found = 0;
+  u64 sum = before;
+  // (the logit's 32 in three turns, the index's in three)
+  for (int low = 53; ; low = low == 53 ? 42 : low == 42 ? 32 : low == 32 ? 21 : low == 21 ? 10 : 0) {
+    const int width = low == 32 || low == 0 ? 10 : 11, high = low + width;
+    clear_bins(sh);
+    row.template each<2>([&](float z, uint32_t i) {
+      if (bins.of(z) != bin) return;
+      const Rank r = rank_of(z, i);
+      if (r == 0 || r < border || (high < 64 && (r >> high) != (found >> high))) return;
+      // (descending: the first bin has the largest ranks; in the bits of the index all logits are equal, above them equal logits have one bin)
+      const int at = (1 << width) - 1 - (int)((r >> low) & ((1u << width) - 1));
+      add_to_bin(sh, at, low < 32 ? (uint32_t)at : __float_as_uint(z), W(z));
+    });
+    __syncthreads();
+    const int at = crossing_bin(sh, target - sum);
+    sum += sh.above;
+    found |= (u64)((1 << width) - 1 - at) << low;
+    __syncthreads();
+    if (low == 0) break;
+  }
+  return found;
+}
+
 // The same for a row whose units the threads hold, U each at most: the waves' running sums unit by unit, then the token.
 template <int U, typename T, int E, typename FT, typename FW, typename FP>
 __device__ __forceinline__ void locate_held(const Span<T> &row, Shared &sh, const Unit<T, E> (&held)[U], FT point, FW W, FP put) {
@@ -501,6 +538,10 @@ __device__ __forceinline__ void locate_held(const Span<T> &row, Shared &sh, cons
   const u64 at = before + upto_behind - behind;
   if (at <= target && target < at + behind) put(last);
 }
+
+// What bins of weights have to cover: 33 temperatures below the largest logit weights are zero, and below the smallest (which is -inf where
+// tokens are masked) there is nothing.
+__device__ __forceinline__ float width_of(const Weights &wt, float t, float least) { return fminf(33.0f * t, wt.best - least); }
 
 // What the caller asks of a row.
 struct Asked {
@@ -623,8 +664,8 @@ __device__ __forceinline__ void draw_small(Shared &sh, int M, const Asked &q, co
 
 // The draw from a whole row whose largest logit is known, in passes over it; `finish` makes the draw once it is known what is kept.
 template <typename T, typename FF>
-__device__ __forceinline__ void draw_whole(const Span<T> &row, Shared &sh, const Asked &q, const Weights &wt, const Put &put, FF finish) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+__device__ __forceinline__ void draw_whole(const Span<T> &row, Shared &sh, const Asked &q, const Weights &wt, float least, const Put &put,
+                                           FF finish) {
   const float best = wt.best;
   if (best == INFINITY) {                                // equal weights for the tokens that have it, none for the others
     u64 m = 0, all;
@@ -643,33 +684,28 @@ __device__ __forceinline__ void draw_whole(const Span<T> &row, Shared &sh, const
     float width;                                         // of what the bins cover
     if (by_weight) {
       if (!(q.p < 1.0f)) break;
-      width = 33.0f * q.t;                               // further below the largest logit weights are zero
+      width = width_of(wt, q.t, least);
     } else {
       if (q.k <= 0) continue;
-      float least = INFINITY;
-      int have = 0;
+      u64 have = 0, all;
+      float none = -INFINITY, lowest = INFINITY;
       row.template each<1>([&](float z, uint32_t) {
         if (z > -INFINITY) {
-          least = fminf(least, z);
+          lowest = fminf(lowest, z);
           ++have;
         }
       });
-      u64 all;
-      block_before_u64((u64)have, sh, &all);
+      block_before_u64(have, sh, &all);
       if ((u64)q.k >= all) continue;
-      least = -max64(-least);
-      if (lane == 0) sh.fmin[wave] = least;
-      __syncthreads();
-#pragma unroll
-      for (int w = 0; w < kWaves; ++w) least = fminf(least, sh.fmin[w]);
-      width = best - least;
+      extremes(sh, none, none, lowest);
+      width = best - lowest;
     }
     const Bins<> bins(best, width);
     const float zero = by_weight ? wt.zero(q.t) : -INFINITY;
     const auto share = [&](float z) -> u64 { return by_weight ? (z >= zero ? wt.of(wt.near(z)) : 0) : 1; };
     clear_bins(sh);
     row.each([&](float z, uint32_t i) {
-      if (z > -INFINITY && (border <= 1 || rank_of(z, i) >= border)) add_to_bin(sh, bins.of(z), z, share(z));
+      if (z > -INFINITY && (border <= 1 || rank_of(z, i) >= border)) add_to_bin(sh, bins.of(z), __float_as_uint(z), share(z));
     });
     __syncthreads();
     u64 target = (u64)q.k;
@@ -719,13 +755,17 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(const T *logits, Sampl
   const Asked q(a, n);                                   // (first, so that its loads are under way with the row's)
   begin(sh);
   const Span<T> row(logits + n * a.pitch, a.V, 0, a.V);
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63;
   const Put put{a, n};
   // the largest logit, the threads' own, and the smallest of those; the units of rows of up to four a thread stay in registers
   constexpr int E = Span<T>::E, U = 4;
   Unit<T, E> held[U];
   const bool holds = row.per <= 64 * U;
-  float mine = -INFINITY;
+  float mine = -INFINITY, least = INFINITY;
+  const auto look = [&](float z) {
+    mine = fmaxf(mine, z);
+    least = fminf(least, z);                             // (-inf where a token is masked: what it is for does without)
+  };
   if (holds) {
 #pragma unroll
     for (int j = 0; j < U; ++j) {
@@ -736,24 +776,14 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(const T *logits, Sampl
     for (int j = 0; j < U; ++j)
       if (row.first + lane + 64 * j < row.end) {
 #pragma unroll
-        for (int i = 0; i < E; ++i) mine = fmaxf(mine, held[j].get(i));
+        for (int i = 0; i < E; ++i) look(held[j].get(i));
       }
-    row.behind([&](float z, uint32_t) { mine = fmaxf(mine, z); });
+    row.behind([&](float z, uint32_t) { look(z); });
   } else {
-    row.each([&](float z, uint32_t) { mine = fmaxf(mine, z); });
+    row.each([&](float z, uint32_t) { look(z); });
   }
-  const float wmax = max64(mine), wmin = -max64(mine > -INFINITY ? -mine : -INFINITY);
-  if (lane == 0) {
-    sh.fmax[wave] = wmax;
-    sh.fmin[wave] = wmin;
-  }
-  __syncthreads();
-  float best = sh.fmax[0], low = sh.fmin[0];
-#pragma unroll
-  for (int w = 1; w < kWaves; ++w) {
-    best = fmaxf(best, sh.fmax[w]);
-    low = fminf(low, sh.fmin[w]);
-  }
+  float best = mine, low = mine > -INFINITY ? mine : INFINITY;
+  extremes(sh, best, low, least);
   if (best == -INFINITY) {                               // nothing to choose from
     if (threadIdx.x == 0) put(-1);
     return;
@@ -806,7 +836,7 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(const T *logits, Sampl
     }
   }
   if (M <= kSmall) draw_small(sh, M, q, wt, a.V, put);
-  else draw_whole(row, sh, q, wt, put, [&](auto W) __attribute__((always_inline)) {
+  else draw_whole(row, sh, q, wt, least, put, [&](auto W) __attribute__((always_inline)) {
     const auto point = [&](u64 all) { return q.point(all); };
     if (holds) locate_held(row, sh, held, point, W, put);
     else locate<4>(row, sh, 0, point, W, put);
@@ -820,7 +850,7 @@ __device__ __forceinline__ Span<T> chunk_of(const T *logits, const SampleArgs &a
   return Span<T>(logits + n * a.pitch, a.V, chunk * a.chunk_units, chunk + 1 == a.chunks ? a.V : (chunk + 1) * a.chunk_units);
 }
 
-// Launch 1: the maxima of all parts; what later launches add to is cleared.
+// Launch 1: the maxima and minima of all parts; what later launches add to is cleared.
 template <typename T>
 __global__ __launch_bounds__(kThreads) void sample_maxima_kernel(const T *logits, SampleArgs a) {
   constexpr int E = Span<T>::E, U = 4;
@@ -845,14 +875,22 @@ __global__ __launch_bounds__(kThreads) void sample_maxima_kernel(const T *logits
     for (int j = 0; j < U; ++j) {
       const int at = p + j * kWaves, u = at * 64 + lane;
       if (at >= p1) break;
-      float m = -INFINITY;
+      float m = -INFINITY, l = INFINITY;
+      const auto look = [&](float v) {
+        m = fmaxf(m, v);
+        l = fminf(l, v);
+      };
       if (u < whole) {
 #pragma unroll
-        for (int i = 0; i < E; ++i) m = fmaxf(m, t[j].get(i));
+        for (int i = 0; i < E; ++i) look(t[j].get(i));
       }
-      if (at == a.parts - 1 && whole * E + lane < a.V) m = fmaxf(m, Elem<T>::load(z + whole * E + lane));
+      if (at == a.parts - 1 && whole * E + lane < a.V) look(Elem<T>::load(z + whole * E + lane));
       m = max64(m);
-      if (lane == 0) space.maxima[at] = m;
+      l = -max64(-l);
+      if (lane == 0) {
+        space.maxima[at] = m;
+        space.minima[at] = l;
+      }
     }
   }
 }
@@ -861,31 +899,20 @@ __global__ __launch_bounds__(kThreads) void sample_maxima_kernel(const T *logits
 enum Way { kNothing, kGreedy, kFew, kSums, kPlain, kWhole };
 struct Plan {
   Way way;
-  float best, low;                   // largest and smallest of the parts' maxima
+  float best, low, least;            // largest and smallest of the parts' maxima, smallest of their minima
 };
 
 __device__ __forceinline__ Plan plan_row(Shared &sh, const SampleArgs &a, const RowSpace &space, const Asked &q) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   begin(sh);
-  float top = -INFINITY, down = INFINITY;
+  float top = -INFINITY, down = INFINITY, least = INFINITY;
   for (int p = threadIdx.x; p < a.parts; p += kThreads) {
     const float m = space.maxima[p];
     top = fmaxf(top, m);
     if (m > -INFINITY) down = fminf(down, m);
+    least = fminf(least, space.minima[p]);
   }
-  top = max64(top);
-  down = -max64(-down);
-  if (lane == 0) {
-    sh.fmax[wave] = top;
-    sh.fmin[wave] = down;
-  }
-  __syncthreads();
-  Plan plan{kNothing, sh.fmax[0], sh.fmin[0]};
-#pragma unroll
-  for (int w = 1; w < kWaves; ++w) {
-    plan.best = fmaxf(plan.best, sh.fmax[w]);
-    plan.low = fminf(plan.low, sh.fmin[w]);
-  }
+  Plan plan{kNothing, top, down, least};
+  extremes(sh, plan.best, plan.low, plan.least);
   if (plan.best == -INFINITY) return plan;
   plan.way = q.greedy() ? kGreedy : plan.best < INFINITY ? (q.k > 0 ? kFew : !q.inside() ? kWhole : q.p < 1.0f ? kSums : kPlain) : kWhole;
   return plan;
@@ -906,9 +933,9 @@ __global__ __launch_bounds__(kThreads) void sample_bins_kernel(const T *logits, 
   const Weights wt(plan.best, q.t, a.shift, sh);
   float least = wt.zero(q.t);
   if (plan.way == kSums) {
-    const Bins<> bins(plan.best, 33.0f * q.t);
+    const Bins<> bins(plan.best, width_of(wt, q.t, plan.least));
     span.template each<8 / Span<T>::E>([&](float z, uint32_t) {
-      if (z >= least) add_to_bin(sh, bins.of(z), z, wt.of(wt.near(z)));
+      if (z >= least) add_to_bin(sh, bins.of(z), __float_as_uint(z), wt.of(wt.near(z)));
     });
     __syncthreads();
     for (int b = threadIdx.x; b < kBins; b += kThreads)
@@ -945,7 +972,7 @@ __global__ __launch_bounds__(kThreads) void sample_border_kernel(const T *logits
   if (plan.way != kSums) return;
   const Span<T> span = chunk_of(logits, a, n, chunk);
   const Weights wt(plan.best, q.t, a.shift, sh);
-  const Bins<> bins(plan.best, 33.0f * q.t);
+  const Bins<> bins(plan.best, width_of(wt, q.t, plan.least));
   u64 target, all, sum = 0;
   const int bin = border_bin(sh, space, q, &target);
   float least = wt.zero(q.t);
@@ -1050,7 +1077,7 @@ __global__ __launch_bounds__(kThreads) void sample_draw_kernel(const T *logits, 
   }
   if (whole) {
     const Span<T> row(z, a.V, 0, a.V);
-    draw_whole(row, sh, q, wt, put, [&](auto W) __attribute__((always_inline)) { locate<4>(row, sh, 0, [&](u64 all) { return q.point(all); }, W, put); });
+    draw_whole(row, sh, q, wt, plan.least, put, [&](auto W) __attribute__((always_inline)) { locate<4>(row, sh, 0, [&](u64 all) { return q.point(all); }, W, put); });
     return;
   }
   Limit limit{-INFINITY, 0};
