@@ -259,11 +259,7 @@ def _check(status):
 def _ws(t):
     if t is None:
         return None, 0
-    try:
-        return t._chn_ws
-    except AttributeError:
-        t._chn_ws = C.c_void_p(t.data_ptr()), t.numel() * t.element_size()
-        return t._chn_ws
+    return C.c_void_p(t.data_ptr()), t.numel() * t.element_size()
 
 
 def _ws_here(t):

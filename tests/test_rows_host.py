@@ -131,3 +131,12 @@ def test_sample_refusals():
     assert call(z=d((4, 0))) == -4                                     # nothing to choose from
     assert call(z=d((4, 2 ** 30 + 1))) == -4
     assert call(z=d((0, 9)), u=d((0,)), out=d((0,), B.I64)) == 0
+
+
+def test_a_workspace_that_grew_in_place_is_described_anew():
+    import torch
+    ws = torch.empty(64, dtype=torch.uint8)
+    assert B._ws(ws)[1] == 64
+    ws.resize_(1 << 20)
+    p, n = B._ws(ws)
+    assert p.value == ws.data_ptr() and n == 1 << 20
