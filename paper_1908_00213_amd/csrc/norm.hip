@@ -622,7 +622,7 @@ __global__ __launch_bounds__(1024) void norm_fold_kernel(const float *partial, i
   constexpr int COLS = 1024 / SLICES;
   __shared__ float part[SLICES][COLS + 1];
   const int col = threadIdx.x % COLS, slice = threadIdx.x / COLS;
-  const int64_t c = (int64_t)blockIdx.x * COLS + col;
+  const int64_t c0 = block_number() * COLS, c = c0 + col;
   float v = 0.0f;
   if (c < 2 * C) {
 #pragma unroll 4
@@ -636,7 +636,7 @@ __global__ __launch_bounds__(1024) void norm_fold_kernel(const float *partial, i
 #pragma unroll
     for (int q = 1; q < SLICES / 16; ++q) t += part[k + 16 * q][cc];
     t = sum16(t);
-    const int64_t o = (int64_t)blockIdx.x * COLS + cc;
+    const int64_t o = c0 + cc;
     if (k == 0 && o < 2 * C) {
       if (o < C) {
         if (dgamma) dgamma[o] = t;
@@ -833,9 +833,9 @@ chn_status norm_bwd(const chn_array *dy, const chn_array *ds, const chn_array *s
   if (a.partial) {
     // (64 columns a block for few strips, sixteen for many: 99 x 20011 with 25 strips 6.0 us with sixteen)
     if (strips <= 64)
-      hipLaunchKernelGGL(norm_fold_kernel<16>, dim3((unsigned)((2 * a.C + 63) / 64)), dim3(1024), 0, st, a.partial, (int)strips, a.C, floats_out(dgamma), floats_out(dbeta));
+      hipLaunchKernelGGL(norm_fold_kernel<16>, grid_of((2 * a.C + 63) / 64), dim3(1024), 0, st, a.partial, (int)strips, a.C, floats_out(dgamma), floats_out(dbeta));
     else
-      hipLaunchKernelGGL(norm_fold_kernel<64>, dim3((unsigned)((2 * a.C + 15) / 16)), dim3(1024), 0, st, a.partial, (int)strips, a.C, floats_out(dgamma), floats_out(dbeta));
+      hipLaunchKernelGGL(norm_fold_kernel<64>, grid_of((2 * a.C + 15) / 16), dim3(1024), 0, st, a.partial, (int)strips, a.C, floats_out(dgamma), floats_out(dbeta));
   }
   return check_launch(what);
 }

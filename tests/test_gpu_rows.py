@@ -313,3 +313,19 @@ def test_a_workspace_of_the_host_is_refused():
     m = torch.ones(4, device="cuda")
     with pytest.raises(ValueError):
         B.layer_norm_bwd(x, x, m, m, torch.empty_like(x), v, v.clone(), v.clone(), ws=torch.empty(1 << 16, dtype=torch.uint8))
+
+
+def test_more_columns_than_a_line_of_the_grid_has_blocks():
+    n, c = 2, 2 ** 27 + 41                               # 64 column sums to a block, 2 c of them
+    g = torch.Generator(device="cuda").manual_seed(5)
+    x, dy = (torch.randn(n, c, device="cuda", generator=g) for _ in range(2))
+    mean, rstd = torch.tensor([0.25, -0.5], device="cuda"), torch.tensor([0.5, 2.0], device="cuda")
+    dgamma, dbeta = (torch.full((c,), 7.0, device="cuda") for _ in range(2))
+    ws = torch.empty(B.layer_norm_bwd_workspace_bytes(x), dtype=torch.uint8, device="cuda")
+    B.layer_norm_bwd(dy, x, mean, rstd, torch.empty_like(x), None, dgamma, dbeta, ws)
+    assert torch.equal(dbeta, dy[0] + dy[1])             # (one rounding either way)
+    for a in range(0, c, 2 ** 25):
+        p, q = (t[:, a:a + 2 ** 25].double() for t in (x, dy))
+        t = (p - mean.double()[:, None]) * rstd.double()[:, None] * q
+        # a difference (the scales are powers of two), a product and a sum
+        assert bool(((dgamma[a:a + 2 ** 25] - t.sum(0)).abs() <= 4 * U * (t.abs().sum(0) + 1e-30)).all()), a
