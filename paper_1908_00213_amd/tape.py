@@ -1996,7 +1996,9 @@ class LSTMLanguageModel:
         last token.  Nothing is recorded and nothing is dropped."""
         import numpy as np
         F = backend()
-        Bn = ids.shape[0] // n_steps
+        if n_steps < 1 or len(u.shape) != 2 or u.shape[0] < 1 or ids.shape[0] != n_steps * u.shape[1]:
+            raise ValueError("LSTMLanguageModel.generate: %d ids of %d steps for u of shape %s" % (ids.shape[0], n_steps, tuple(u.shape)))
+        Bn = u.shape[1]
         row = lambda v, dt: v if v is None or hasattr(v, "shape") else F.from_numpy(np.full((Bn,), v, dtype=dt))
         filters = (row(temperature, np.float32), row(top_k, np.int64), row(top_p, np.float32), row(min_p, np.float32))
         out = F.empty(tuple(u.shape), "i64")

@@ -161,3 +161,11 @@ def test_generate_follows_the_model():
             text = np.concatenate([text, want])
         greedy, _ = model.generate(prompt, 4, u, temperature=0.0)
         assert np.array_equal(greedy[0], model._logits(model._hidden(prompt, 4, None)[0]).array[-Bn:].argmax(1))
+
+
+def test_generate_refuses_a_prompt_that_does_not_fit():
+    with T.using_backend(RowsBackend()):
+        model = T.LSTMLanguageModel(lm_params(np.random.default_rng(6)), n_step=True)
+        for ids, steps, u in ((12, 4, (2, 4)), (12, 4, (0, 3)), (0, 0, (2, 3)), (13, 4, (2, 3)), (12, 4, (3,))):
+            with pytest.raises(ValueError):
+                model.generate(np.zeros(ids, np.int64), steps, np.zeros(u, np.float32))
