@@ -230,3 +230,28 @@ def test_a_row_for_every_block_beyond_a_line_of_the_grid():
     cum = torch.cumsum(w, 1)
     want = (cum > u.double()[:, None] * cum[:, -1:]).to(torch.uint8).argmax(1).int()
     assert torch.equal(out, want)
+
+
+@pytest.mark.parametrize("v", [5000, 70001])
+def test_more_tokens_in_the_bin_of_a_border_than_are_ordered_by_comparing(v):
+    """Bins have equal width between the largest and the smallest logit: one that lies far off leaves all others in one bin."""
+    n = 10
+    rng = np.random.default_rng(v)
+    z = logits(n, v, "f32", v + 2, 1e-3).contiguous()
+    z[:5, v // 2] = -500.0
+    z[5:, v // 3] = 12.0
+    z[1] = z[1].bfloat16().float()                       # ties
+    z[2, : v // 2] = 0.0                                 # equals only, up to the one far off
+    z[2, v // 2 + 1:] = 0.0
+    z[6] = torch.where(z[6] == 12.0, 12.0, -0.5)
+    z[7] = z[7].bfloat16().float()
+    z[3, ::7] = -np.inf
+    z[8, ::7] = float("nan")
+    u, k = rng.random(n, dtype=np.float32), rng.integers(1500, v - v // 6, n)
+    p, t = rng.uniform(0.2, 0.95, n), rng.choice([0.7, 1.0, 1.6], n)
+    for _ in range(3):
+        check(z, u, top_k=k)
+        check(z, u, top_p=p)
+        check(z, u, temperature=t, top_k=k, top_p=p)
+        check(z, u, temperature=t, top_k=k, top_p=p, min_p=[0.999] * 5 + [1e-5] * 5)
+        u, k, p = np.roll(u, 1), np.roll(k, 1), np.roll(p, 1)
