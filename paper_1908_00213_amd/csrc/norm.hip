@@ -25,8 +25,22 @@ struct NormArgs {
   float eps;
   const float *gamma, *beta;
   float *mean, *rstd;
+  bool lines;                        // every row of every output begins a line of the cache
   DropArgs drop;
 };
+
+// Groups of up to sixteen lanes store rows a few hundred bytes at a time: past the usual order of replacement only if those are whole lines
+// (forward, fp32 / bf16, us: 134217 x 250 67 / 31 so, 45 / 24 otherwise; 262144 x 128 40 / 21 so, 42 / 22 otherwise).
+template <int G, typename T, int E>
+__device__ __forceinline__ void put_unit(const Unit<T, E> &u, T *p, bool lines) {
+  if (G >= 32 || lines) {
+    u.store_nt(p);
+  } else {
+    asm volatile("");                                    // (without these two the compiler joins the branches into one ordinary store)
+    u.store(p);
+    asm volatile("");
+  }
+}
 
 // The word of one column, for the elements behind the last whole unit.
 __device__ __forceinline__ uint32_t word_of(const DropState &d, uint32_t c, uint32_t row) {
@@ -45,12 +59,13 @@ __device__ __forceinline__ void drop_unit(const DropState &d, uint32_t c0, uint3
   }
 }
 
-// One row by G lanes of KE elements each; groups of up to 256 lanes share a block of 256.  (Kernels that walk over rows with gamma and beta
+// One row by G lanes of KE elements each; groups of up to 64 lanes share a block of 256.  (Kernels that walk over rows with gamma and beta
 // in registers are slower: 8192 x 4096 bf16 24.9 us with 2048 blocks, 22.1 with a block for each row.)  Results are stored past the
 // caches' usual order of replacement, since nothing of them is read here again: 4480 x 650 fp32 6.1 -> 5.6 us, 1024 x 1000 with residual 5.3 -> 5.0.
 template <typename TX, typename TY, typename TS, bool RES, int G, int KE>
-__global__ __launch_bounds__(G > 256 ? G : 256) void norm_fwd_rows_kernel(const TX *x, const TS *residual, TS *s, TY *y, NormArgs a) {
-  constexpr int E = unit_elements<TX, TY, TS>(), K = KE / E, GROUPS = (G > 256 ? G : 256) / G;
+__global__ __launch_bounds__(G > 64 ? G : 256) void norm_fwd_rows_kernel(const TX *x, const TS *residual, TS *s, TY *y, NormArgs a) {
+  constexpr int E = unit_elements<TX, TY, TS>(), K = KE / E, GROUPS = (G > 64 ? G : 256) / G;
+  static_assert(G >= E - 1, "a lane for each element behind the last whole unit");
   __shared__ float2 smem[G > 64 ? 2 * G / 64 : 1];
   const int C = (int)a.C, whole = C / E, left = C - whole * E;
   const float inv = 1.0f / (float)C;
@@ -93,7 +108,7 @@ __global__ __launch_bounds__(G > 256 ? G : 256) void norm_fwd_rows_kernel(const 
         ru[k].set(i, add_rounded(ru[k].get(i), v[k][i]));
         v[k][i] = ru[k].get(i);
       }
-      if (g + k * G < whole) ru[k].store_nt(sr + c0);
+      if (g + k * G < whole) put_unit<G>(ru[k], sr + c0, a.lines);
     }
     if (g < left) {
       if (a.drop.rng) vl = d.apply(vl, word_of(d, (uint32_t)cl, (uint32_t)row));
@@ -143,7 +158,7 @@ __global__ __launch_bounds__(G > 256 ? G : 256) void norm_fwd_rows_kernel(const 
       Unit<TY, E> yu;
 #pragma unroll
       for (int i = 0; i < E; ++i) yu.set(i, fmaf((v[k][i] - m1) * rstd, a.gamma ? gm.get(i) : 1.0f, a.beta ? bt.get(i) : 0.0f));
-      yu.store_nt(yr + c0);
+      put_unit<G>(yu, yr + c0, a.lines);
     }
   }
   if (g < left) Elem<TY>::store(yr + cl, fmaf((vl - m1) * rstd, a.gamma ? a.gamma[cl] : 1.0f, a.beta ? a.beta[cl] : 0.0f));
@@ -250,6 +265,7 @@ struct NormBwdArgs {
   int64_t strips;                    // wide rows: as many, of neighbouring rows
   float2 *sums;                      // wide rows: [N][segments] sums of g and g h
   int segments;
+  bool lines;
   DropArgs drop;
 };
 
@@ -258,6 +274,7 @@ struct NormBwdArgs {
 template <typename TX, typename TY, typename TS, bool RES, int G, int KE, int THREADS>
 __global__ __launch_bounds__(THREADS) void norm_bwd_rows_kernel(const TY *dy, const TS *s, const TS *ds, TS *dres, TX *dx, NormBwdArgs a) {
   constexpr int E = unit_elements<TX, TY, TS>(), K = KE / E, GROUPS = THREADS / G;
+  static_assert(G >= E - 1, "a lane for each element behind the last whole unit");
   constexpr int PARTS = G < 64 ? THREADS / 64 : GROUPS;   // sets of column sums that a block joins
   constexpr int SPAN = G * KE;
   __shared__ float2 smem[G > 64 ? 2 * THREADS / 64 : 1];
@@ -387,7 +404,7 @@ __global__ __launch_bounds__(THREADS) void norm_bwd_rows_kernel(const TY *dy, co
           Unit<TS, E> out;
 #pragma unroll
           for (int i = 0; i < E; ++i) out.set(i, o[i]);
-          if (g + k * G < whole) out.store_nt(dres + row * a.pdr + c0);
+          if (g + k * G < whole) put_unit<G>(out, dres + row * a.pdr + c0, a.lines);
         }
         if (dx && a.drop.rng) drop_unit<E>(d, c0, (uint32_t)row, o);
       }
@@ -395,7 +412,7 @@ __global__ __launch_bounds__(THREADS) void norm_bwd_rows_kernel(const TY *dy, co
         Unit<TX, E> out;
 #pragma unroll
         for (int i = 0; i < E; ++i) out.set(i, o[i]);
-        if (g + k * G < whole) out.store_nt(dx + row * a.pdx + c0);
+        if (g + k * G < whole) put_unit<G>(out, dx + row * a.pdx + c0, a.lines);
       }
     }
     if (g < left) {
@@ -427,12 +444,10 @@ __global__ __launch_bounds__(THREADS) void norm_bwd_rows_kernel(const TY *dy, co
       pb[cl] = abl;
     }
   } else {
-    // groups of 16 first join within their wave, in the order of the rows of lanes
-    const auto join16 = [&](float v) -> float {
-      if constexpr (G == 16) {
-        const int l = threadIdx.x & 15;
-        return (__shfl(v, l, 64) + __shfl(v, l + 16, 64)) + (__shfl(v, l + 32, 64) + __shfl(v, l + 48, 64));
-      }
+    // groups smaller than a wave first join within it
+    const auto join = [&](float v) -> float {
+#pragma unroll
+      for (int o = G; o < 64; o <<= 1) v += __shfl_xor(v, o, 64);
       return v;
     };
     const int part = threadIdx.x / (G < 64 ? 64 : G);
@@ -442,13 +457,13 @@ __global__ __launch_bounds__(THREADS) void norm_bwd_rows_kernel(const TY *dy, co
     for (int k = 0; k < K; ++k)
 #pragma unroll
       for (int i = 0; i < E; ++i) {
-        const float vg = join16(ag[k][i]), vb = join16(ab[k][i]);
+        const float vg = join(ag[k][i]), vb = join(ab[k][i]);
         if (writes) {
           mg[(g + k * G) * E + i] = vg;
           mb[(g + k * G) * E + i] = vb;
         }
       }
-    const float vg = join16(agl), vb = join16(abl);
+    const float vg = join(agl), vb = join(abl);
     const auto add_up = [&](int c, int at) {
       float sg = joined[at], sb = joined[PARTS * SPAN + at];
 #pragma unroll
@@ -669,6 +684,11 @@ chn_status check_matrix(const chn_array *m, const char *name, bool is_output, in
   return CHN_OK;
 }
 
+// Whether rows of a matrix (NULL: no matter) begin lines of 128 bytes.
+bool at_lines(const chn_array *m, int64_t pitch) {
+  return !m || (reinterpret_cast<uintptr_t>(m->data) | (uintptr_t)(pitch * dtype_size(m->dtype))) % 128 == 0;
+}
+
 const float *floats(const chn_array *v) { return v ? static_cast<const float *>(v->data) : nullptr; }
 float *floats_out(const chn_array *v) { return v ? static_cast<float *>(v->data) : nullptr; }
 
@@ -676,12 +696,24 @@ template <typename TX, typename TY, typename TS, bool RES>
 void launch_fwd(const TX *x, const TS *residual, TS *s, TY *y, const NormArgs &a, hipStream_t st) {
   constexpr int E = unit_elements<TX, TY, TS>();
   const int64_t held = a.C / E * E;                      // (the elements behind the last whole unit come on top)
+  // As few lanes as hold the row, since the others have nothing in flight (us by these / by twice to four times as many: 524288 x 64 fp32 39 / 43, bf16
+  // 25 / 39, 127100 x 264 bf16 28 / 43, 30504 x 1100 bf16 29 / 42, 8176 x 4104 bf16 29 / 52), but stores of at least a line at once (524288 x 64 fp32
+  // with residual 82, by four lanes 126).
 #define CHN_ROWS(G, KE)                                                                                                             \
-  hipLaunchKernelGGL((norm_fwd_rows_kernel<TX, TY, TS, RES, G, KE>), grid_of((a.N + (G < 256 ? 256 / G : 1) - 1) / (G < 256 ? 256 / G : 1)), \
-                     dim3(G > 256 ? G : 256), 0, st, x, residual, s, y, a)
-  if (held <= 16 * 16) CHN_ROWS(16, 16);
+  hipLaunchKernelGGL((norm_fwd_rows_kernel<TX, TY, TS, RES, G, KE>), grid_of((a.N + (G > 64 ? 1 : 256 / G) - 1) / (G > 64 ? 1 : 256 / G)),    \
+                     dim3(G > 64 ? G : 256), 0, st, x, residual, s, y, a)
+  if constexpr (E == 4)                                  // (four lanes have no room for up to seven elements behind the last unit)
+    if (held <= 4 * 8) {
+      CHN_ROWS(4, 8);
+      return;
+    }
+  if (held <= 8 * 16) CHN_ROWS(8, 16);
+  else if (held <= 16 * 16) CHN_ROWS(16, 16);
+  else if (held <= 32 * 16) CHN_ROWS(32, 16);
   else if (held <= 64 * 16) CHN_ROWS(64, 16);
+  else if (held <= 128 * 16) CHN_ROWS(128, 16);
   else if (held <= 256 * 16) CHN_ROWS(256, 16);
+  else if (held <= 512 * 16) CHN_ROWS(512, 16);
   else if (held <= 1024 * 16) CHN_ROWS(1024, 16);
   else if (held <= 1024 * 32) CHN_ROWS(1024, 32);
   else hipLaunchKernelGGL((norm_fwd_wide_kernel<TX, TY, TS, RES>), grid_of(a.N), dim3(1024), 0, st, x, residual, s, y, a);
@@ -709,6 +741,7 @@ chn_status norm_fwd(const chn_array *x, const chn_array *residual, double ratio,
   CHN_TRY(check_drop(rng, ratio, site, a.N, a.C, what, &a.drop));
   if (a.N == 0) return CHN_OK;
   a.eps = (float)eps;
+  a.lines = at_lines(s, a.ps) && at_lines(y, a.py);
   a.gamma = floats(gamma);
   a.beta = floats(beta);
   a.mean = floats_out(mean);
@@ -734,7 +767,7 @@ chn_status norm_fwd(const chn_array *x, const chn_array *residual, double ratio,
 }
 
 // What the backward pass leaves in its workspace: strips of column sums, and for rows longer than a block holds the rows' sums behind them.
-constexpr int64_t kHeld = 512 * 16;                      // elements of a row that a block holds
+constexpr int64_t kHeld = 1024 * 8;                      // elements of a row that a block holds
 constexpr int64_t kStrips = 256;                         // one for each compute unit
 int64_t strips_of(int64_t N, int64_t C) {
   if (C <= kHeld) return N < kStrips ? (N > 0 ? N : 1) : kStrips;
@@ -762,11 +795,19 @@ template <typename TX, typename TY, typename TS, bool RES>
 int64_t launch_bwd(const TY *dy, const TS *s, const TS *ds, TS *dres, TX *dx, NormBwdArgs &a, hipStream_t st) {
   constexpr int E = unit_elements<TX, TY, TS>();
 #define CHN_ROWS(G, KE, THREADS) return launch_bwd_rows<TX, TY, TS, RES, G, KE, THREADS>(dy, s, ds, dres, dx, a, st)
+  // As in the forward pass; blocks of 960 for what leaves much of 1024 idle (us / by the next larger group: 127100 x 264 bf16 45 / 68,
+  // 30504 x 1100 50 / 63, 16320 x 2056 44 / 54); beyond 4096 a block for each row (6710 x 5000 fp32 69, 512 threads with sixteen elements 83).
+  if constexpr (E == 4)
+    if (a.C <= 4 * 8) CHN_ROWS(4, 8, 512);
+  if (a.C <= 8 * 16) CHN_ROWS(8, 16, 512);
   if (a.C <= 16 * 16) CHN_ROWS(16, 16, 512);
+  if (a.C <= 32 * 16) CHN_ROWS(32, 16, 512);
   if (a.C <= 64 * 16) CHN_ROWS(64, 16, 512);
+  if (a.C <= 192 * 8) CHN_ROWS(192, 8, 960);
   if (a.C <= 256 * 8) CHN_ROWS(256, 8, 1024);
+  if (a.C <= 320 * 8) CHN_ROWS(320, 8, 960);
   if (a.C <= 512 * 8) CHN_ROWS(512, 8, 1024);
-  if (a.C <= kHeld) CHN_ROWS(512, 16, 512);
+  if (a.C <= kHeld) CHN_ROWS(1024, 8, 1024);
 #undef CHN_ROWS
   if (a.N > 0)
     hipLaunchKernelGGL((norm_bwd_sums_kernel<TY, TS>), dim3(grid_of(a.N).x, (unsigned)a.segments, grid_of(a.N).y), dim3(256), 0, st, dy, s, a);
@@ -803,9 +844,10 @@ chn_status norm_bwd(const chn_array *dy, const chn_array *ds, const chn_array *s
   a.gamma = floats(gamma);
   a.mean = floats(mean);
   a.rstd = floats(rstd);
+  a.lines = at_lines(dres, a.pdr) && at_lines(dx, a.pdx);
   a.strips = strips_of(a.N, a.C);
-  a.segments = segments_of(a.N, a.C);
   const bool sums = dgamma || dbeta;
+  a.segments = segments_of(a.N, a.C);
   if (!sums && (a.N == 0 || (!dx && !dres))) return CHN_OK;
   const size_t rows_bytes = bwd_sums_bytes(a.N, a.C);
   CHN_TRY(check_ws(ws, ws_bytes, sums ? bwd_workspace(a.N, a.C) : rows_bytes, what));

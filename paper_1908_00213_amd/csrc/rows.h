@@ -66,13 +66,17 @@ __device__ __forceinline__ float dpp_add(float v) {
   return v + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, true));
 }
 
-// Sum over the 16 lanes of a row of the wave, in all of them.
-__device__ __forceinline__ float sum16(float v) {
-  v = dpp_add<0xB1>(v);    // quad_perm 1 0 3 2
-  v = dpp_add<0x4E>(v);    // quad_perm 2 3 0 1
-  v = dpp_add<0x141>(v);   // row_half_mirror
-  return dpp_add<0x140>(v);  // row_mirror
+// Sum over G = 4, 8, 16 (a row of the wave) or 32 neighbouring lanes, in all of them.
+template <int G>
+__device__ __forceinline__ float sum_lanes(float v) {
+  v = dpp_add<0xB1>(v);                          // quad_perm 1 0 3 2
+  v = dpp_add<0x4E>(v);                          // quad_perm 2 3 0 1
+  if constexpr (G >= 8) v = dpp_add<0x141>(v);   // row_half_mirror
+  if constexpr (G >= 16) v = dpp_add<0x140>(v);  // row_mirror
+  if constexpr (G >= 32) v += __shfl_xor(v, 16, 64);
+  return v;
 }
+__device__ __forceinline__ float sum16(float v) { return sum_lanes<16>(v); }
 
 // Sum over the wave, uniform: the four rows' sums added in their order.
 __device__ __forceinline__ float sum64(float v) {
@@ -99,8 +103,8 @@ __device__ __forceinline__ float max64(float v) {
 // call, so that one barrier is enough: what is overwritten was read before the barrier of the call in between.
 template <int G>
 __device__ __forceinline__ float2 group_sum(float2 v, float2 *smem, int turn) {
-  if constexpr (G == 16) {
-    return make_float2(sum16(v.x), sum16(v.y));
+  if constexpr (G < 64) {
+    return make_float2(sum_lanes<G>(v.x), sum_lanes<G>(v.y));
   } else {
     v = make_float2(sum64(v.x), sum64(v.y));
     if constexpr (G > 64) {
@@ -108,6 +112,10 @@ __device__ __forceinline__ float2 group_sum(float2 v, float2 *smem, int turn) {
       float2 *p = smem + turn * W;
       if ((threadIdx.x & 63) == 0) p[threadIdx.x % G / 64] = v;
       __syncthreads();
+      if constexpr (W == 16) {                           // a read by each lane, and a sum inside the registers
+        const float2 s = p[threadIdx.x & 15];
+        return make_float2(sum16(s.x), sum16(s.y));
+      }
       float2 s = p[0];
 #pragma unroll
       for (int w = 1; w < W; ++w) {

@@ -10,7 +10,7 @@ from rows_util import DT, HALF, U, bwd_bounds, close, matrix, norm_bounds, round
 pytestmark = pytest.mark.gpu
 SEED, OFFSET, SITE = 0x1234567890ABCDEF, 41, 3
 SHAPES = [(1, 1), (3, 2), (5, 7), (1, 100), (130, 64), (33, 100), (7, 129), (2, 650), (70, 1000), (9, 2049), (5, 4096), (3, 5003), (2, 8200), (3, 16400),
-          (2, 40007)]
+          (2, 40007), (300, 19), (530, 33), (77, 300), (40, 1030), (33, 1100), (40, 2300), (9, 6000), (5, 8191)]
 
 
 def rng_state(seed=SEED, offset=OFFSET):
