@@ -9,7 +9,7 @@
 // All sums and statistics are fp32; the mean is corrected by the mean of what is left after its subtraction, so that rows whose mean
 // is far larger than their spread keep their digits.
 //
-// Bound by memory: every element is read once and written once.  A row is held in the registers of 16, 64, 256 or 1024 lanes between the
+// Bound by memory: every element is read once and written once.  A row is held in the registers of 4 to 1024 lanes between the
 // passes that its statistics need (rows.h); only rows that no block can hold are read again.
 #include "philox.h"
 #include "rows.h"
@@ -785,7 +785,7 @@ size_t bwd_workspace(int64_t N, int64_t C) { return bwd_sums_bytes(N, C) + (size
 
 template <typename TX, typename TY, typename TS, bool RES, int G, int KE, int THREADS>
 int64_t launch_bwd_rows(const TY *dy, const TS *s, const TS *ds, TS *dres, TX *dx, const NormBwdArgs &a, hipStream_t st) {
-  const int64_t blocks = (a.N + THREADS / G - 1) / (THREADS / G), n = blocks < kStrips ? (blocks > 0 ? blocks : 1) : kStrips;
+  const int64_t blocks = (a.N + THREADS / G - 1) / (THREADS / G), n = blocks > 0 && blocks < a.strips ? blocks : a.strips;   // (a strip of the workspace each)
   hipLaunchKernelGGL((norm_bwd_rows_kernel<TX, TY, TS, RES, G, KE, THREADS>), dim3((unsigned)n), dim3(THREADS), 0, st, dy, s, ds, dres, dx, a);
   return n;
 }
