@@ -33,10 +33,6 @@ struct Unit {
 #pragma unroll
     for (int i = 0; i < E / Vec16<T>::N; ++i) q[i] = load16_any(p + i * Vec16<T>::N);
   }
-  __device__ __forceinline__ void load_nt(const T *p) {
-#pragma unroll
-    for (int i = 0; i < E / Vec16<T>::N; ++i) q[i] = load16_any_nt(p + i * Vec16<T>::N);
-  }
   __device__ __forceinline__ void store_nt(T *p) const {
 #pragma unroll
     for (int i = 0; i < E / Vec16<T>::N; ++i) store16_any_nt(p + i * Vec16<T>::N, q[i]);
