@@ -1123,12 +1123,13 @@ __global__ __launch_bounds__(kThreads) void sample_draw_kernel(const T *logits, 
 
 // Chunks that a row is cut in; 1: a block has it whole.  Measured in us, whole rows / chunks (fp32, rows of each with parameters of its own: top-k, top-p,
 // none, and top-k in half of the rows with top-p and min-p in all; several batches in turn):
-//   1 x 65536 18 55 25 19 / 14 25 15 16       64 x 65536 22 58 29 53 / 20 51 26 44    96 x 65536 22 59 29 53 / 22 64 32 51    128 x 65536 25 61 32 55 / 25 76 37 60
+//   1 x 16384 11 21 10 20 / 14 25 15 26       1 x 32768 14 33 17 31 / 14 25 15 26     32 x 32768 15 34 17 32 / 15 29 17 29    64 x 32768 14 34 17 32 / 16 36 19 34
+//   1 x 65536 18 54 25 19 / 14 25 15 16       64 x 65536 22 58 29 53 / 20 51 26 44    96 x 65536 22 59 29 53 / 22 64 32 51    128 x 65536 25 61 32 55 / 25 76 37 60
 //   1 x 131072 27 98 45 28 / 14 26 16 17      128 x 131072 38 113 55 97 / 31 100 52 79    256 x 131072 54 139 73 115 / 49 151 84 107
 //   256 x 262144 88 245 125 204 / 79 241 139 178
 // So chunks win where blocks of whole rows leave compute units idle, or where rows that ask for more than others would keep the launch waiting.
 int chunks_of(int64_t N, int64_t V) {
-  if (V < 65536 || V < (V < 131072 ? 768 : 512) * N || V > (int64_t)kMaxParts * 64 * 4) return 1;   // (a unit has four elements at the least)
+  if (V < 32768 || V < (V < 131072 ? 768 : 512) * N || V > (int64_t)kMaxParts * 64 * 4) return 1;   // (a unit has four elements at the least)
   int64_t n = V / 4096;                                  // a unit or two for each thread
   const int64_t most = (2048 + N - 1) / N;               // and about eight blocks for each compute unit
   if (n > most) n = most;

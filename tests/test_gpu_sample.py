@@ -55,7 +55,7 @@ def test_sample(v, pad, dtype, which):
     check(z, u, **params)
 
 
-@pytest.mark.parametrize("v", [65536, 131072, 262145])
+@pytest.mark.parametrize("v", [32768, 50001, 65536, 131072, 262145])
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_sample_of_large_vocabularies(v, dtype):
     n = 6
@@ -173,7 +173,7 @@ def test_sample_on_a_stream_and_in_a_graph(v):
         B.sample(torch.zeros(2, 9, device="cuda"), torch.rand(2, device="cuda"), torch.empty(2, dtype=torch.int64, device="cuda"))
 
 
-@pytest.mark.parametrize("v", [65536, 70003, 131072])
+@pytest.mark.parametrize("v", [32769, 65536, 70003, 131072])
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_rows_of_every_kind_in_one_batch(v, dtype):
     """Long rows are cut in chunks where the call brings a workspace: every way a row can go, beside all the others, and the same tokens without."""
