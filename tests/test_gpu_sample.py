@@ -36,7 +36,7 @@ def logits(n, v, dtype, seed, spread=2.0, pad=0):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-@pytest.mark.parametrize("v,pad", [(1, 0), (2, 1), (7, 0), (64, 3), (100, 0), (1000, 8), (1025, 0), (4099, 5), (10000, 0)])
+@pytest.mark.parametrize("v,pad", [(1, 0), (2, 1), (7, 0), (64, 3), (100, 0), (255, 1), (256, 0), (257, 0), (500, 3), (513, 0), (1000, 8), (1025, 0), (4099, 5), (10000, 0)])
 @pytest.mark.parametrize("which", ["", "t", "k", "p", "m", "tkpm"])
 def test_sample(v, pad, dtype, which):
     n = 13
@@ -255,3 +255,65 @@ def test_more_tokens_in_the_bin_of_a_border_than_are_ordered_by_comparing(v):
         check(z, u, temperature=t, top_k=k, top_p=p)
         check(z, u, temperature=t, top_k=k, top_p=p, min_p=[0.999] * 5 + [1e-5] * 5)
         u, k, p = np.roll(u, 1), np.roll(k, 1), np.roll(p, 1)
+
+
+@pytest.mark.parametrize("v", [5, 61, 255, 256, 257, 300, 512])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_short_rows_of_every_kind_in_one_batch(v, dtype):
+    n = 31
+    rng = np.random.default_rng(v)
+    z = logits(n, v, dtype, v + 5, 2.0, 1)
+    z[0] = -np.inf                                       # nothing to choose from
+    z[1] = 0.25                                          # all equal
+    z[2, 2:] = float("nan")
+    z[3, ::3] = np.inf                                   # equal infinities
+    z[4] = torch.finfo(z.dtype).min
+    z[5, :-1] = -np.inf                                  # one token, the last
+    z[6] = torch.round(z[6])                             # ties at every border
+    z[7] = torch.round(z[7])
+    z[8] = z[8] * 1e-3                                   # nearly flat
+    z[9] = z[9] * 1e4
+    z[10, v // 2] = np.inf                               # one infinity
+    z[11, ::2] = -0.0                                    # equal to zero
+    z[11, 1::2] = 0.0
+    u = rng.random(n, dtype=np.float32)
+    u[12], u[13] = 0.0, np.nextafter(np.float32(1), np.float32(0))
+    for _ in range(4):
+        params = dict(temperature=rng.choice([0.0, 0.5, 1.0, 1.7], n), top_k=rng.choice([0, 0, 1, 2, 5, v // 2, v - 1, v, v + 7], n),
+                      top_p=rng.choice([1.0, 0.0, 0.3, 0.9, 0.999], n), min_p=rng.choice([0.0, 0.0, 0.01, 0.3, 1.0], n))
+        params["temperature"][:12] = 0.9
+        for names in ((), ("top_k",), ("top_p",), ("min_p",), ("top_k", "top_p"), ("temperature", "top_p", "min_p"), ("temperature", "top_k", "top_p", "min_p")):
+            check(z, u, **{k: params[k] for k in names})
+        u = rng.random(n, dtype=np.float32)
+
+
+@pytest.mark.parametrize("v", [9, 200, 400])
+def test_the_ends_of_the_range_in_short_rows(v):
+    z = logits(12, v, "f32", v + 6)
+    z[0, 0] = z[1, v - 1] = -150.0                       # weights that are zero in sums, and the lightest token all the same
+    z[2] = -np.inf
+    z[3, 1] = np.inf
+    u = np.array([-1.0, 2.0, 1.0, 1.0, 1.0, np.nan, 0.0, np.inf, -np.inf, 1.5, 1.0, -3.0], np.float32)
+    got = draw(z, torch.from_numpy(u).cuda())
+    host = z.double().cpu().numpy()
+    for n, t in enumerate(got):
+        some = np.flatnonzero(host[n] == np.inf) if n == 3 else np.flatnonzero(host[n] > -np.inf)
+        assert t == (-1 if n == 2 else some[-1] if u[n] >= 1 else some[0]), n
+    k = torch.full((12,), 3, device="cuda", dtype=torch.int32)
+    got = draw(z, torch.from_numpy(u).cuda(), top_k=k)
+    for n, t in enumerate(got):
+        if n in (2, 3):
+            assert t == (-1 if n == 2 else 1), n
+        else:
+            best = sorted(sorted(range(v), key=lambda i: (-host[n, i], i))[:3])
+            assert t == (best[-1] if u[n] >= 1 else best[0]), n
+
+
+@pytest.mark.parametrize("n,v", [(2 ** 22 + 5, 3), (2 ** 20 + 3, 260)])      # four rows to a block, and a block for each
+def test_more_rows_than_a_line_of_the_grid_has_blocks(n, v):
+    z = torch.randint(-3, 4, (n, v), device="cuda", dtype=torch.int8, generator=torch.Generator(device="cuda").manual_seed(4)).to(torch.bfloat16)
+    out = torch.empty(n, dtype=torch.int32, device="cuda")
+    B.sample(z, torch.full((n,), 0.5, device="cuda"), out, temperature=torch.zeros(n, device="cuda"))
+    for a in range(0, n, 2 ** 18):                       # the first of the largest
+        part = z[a:a + 2 ** 18].float()
+        assert torch.equal(out[a:a + 2 ** 18], (part == part.max(1, keepdim=True).values).to(torch.uint8).argmax(1).int()), a
