@@ -329,3 +329,23 @@ def test_more_columns_than_a_line_of_the_grid_has_blocks():
         t = (p - mean.double()[:, None]) * rstd.double()[:, None] * q
         # a difference (the scales are powers of two), a product and a sum
         assert bool(((dgamma[a:a + 2 ** 25] - t.sum(0)).abs() <= 4 * U * (t.abs().sum(0) + 1e-30)).all()), a
+
+
+@pytest.mark.parametrize("shape", [(0, 40), (1, 7), (3, 100), (8, 1000), (9, 1000), (5, 1500), (1, 5000), (2, 5000), (4, 8200), (5, 8200), (300, 30)])
+def test_each_weight_gradient_by_itself(shape):
+    n, c = shape
+    x, dy, gamma = data(shape, "f32", 51), data(shape, "f32", 52), vec(1 + 0.3 * data((c,), "f32", 53))
+    xd, dyd = matrix(x, "f32", 1, 0), matrix(dy, "f32")
+    mean, rstd = vec(data((n,), "f32", 54)), vec(1 + 0.1 * np.abs(data((n,), "f32", 55)))
+    both = [torch.full((c,), 9.0, device="cuda") for _ in range(2)]
+    dx = matrix(x * 0, "f32")
+    B.layer_norm_bwd(dyd, xd, mean, rstd, dx, gamma, *both, ws=workspace(xd))
+    wdx, wdg, wdb = R.layer_norm_bwd(dy, x, values(mean), values(rstd), values(gamma))
+    bdx, bdg, bdb = bwd_bounds(dy.astype(np.float64), x.astype(np.float64), values(mean), values(rstd), values(gamma), "f32")
+    close(values(both[0]), wdg, bdg + U * np.abs(wdg), "dgamma")
+    close(values(both[1]), wdb, bdb + U * np.abs(wdb), "dbeta")
+    for k in range(2):
+        one, around, dx1 = [None, None], torch.full((c + 8,), 9.0, device="cuda"), matrix(x * 0, "f32")
+        one[k] = around[4:4 + c]
+        B.layer_norm_bwd(dyd, xd, mean, rstd, dx1, gamma, *one, ws=workspace(xd))
+        assert torch.equal(one[k], both[k]) and torch.equal(dx1, dx) and bool((around[:4] == 9.0).all()) and bool((around[4 + c:] == 9.0).all())
