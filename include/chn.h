@@ -444,10 +444,12 @@ chn_status chn_rng_advance(const chn_array *rng, int64_t steps, chn_stream strea
 /* ---- layer normalisation -----------------------------------------------------------------------------------
  * Every row of x (N,C), F32 or BF16, row-major with unit inner stride and any pitch:
  *   mean = sum x / C      rstd = 1 / sqrt(sum (x - mean)^2 / C + eps)      y = (x - mean) * rstd * gamma + beta
- * gamma, beta: (C,) F32 or NULL (1 and 0).  y: F32 or BF16.  mean, rstd: (N,) F32, for the backward pass, or NULL.
+ * gamma, beta: (C,) F32 or NULL (1 and 0).  y: F32 or BF16.  mean, rstd: (N,) F32, for the backward pass, or NULL.  mean may be (N,2),
+ * contiguous: the mean and what its rounding to fp32 left of it.
  * Statistics and sums are fp32 in a fixed order (bit-reproducible).  eps finite and not negative.  Rows without
  * elements (N > 0, C = 0) and more than 2^31 - 1 rows or columns are CHN_ERR_SHAPE.
- * Backward, from x and the retained statistics, with h = (x - mean) rstd and g = dy gamma:
+ * Backward, from x and the retained statistics, with h = (x - mean) rstd and g = dy gamma (a mean of two parts subtracted part by part: rows
+ * whose mean is far above their spread lose digits of dx and dgamma to the rounding of a mean that is given as one number):
  *   dx = rstd (g - sum g / C - h sum(g h) / C)     dgamma = sum over rows of dy h     dbeta = sum over rows of dy
  * dy: F32 or BF16; dx: x's dtype; dgamma, dbeta: (C,) F32 or NULL.  Workspace, where dgamma or dbeta is wanted or rows have more than
  * 8192 elements: chn_layer_norm_bwd_workspace_bytes(x), 256-byte aligned, the library's until the work on `stream` is done.

@@ -598,6 +598,7 @@ def rng_advance(rng, steps=1, stream=None):
 
 
 def layer_norm_fwd(x, y, gamma=None, beta=None, eps=1e-5, mean=None, rstd=None, stream=None):
+    """mean: (N,), or (N,2) with what its rounding left, which keeps the digits of the gradients of rows with a large mean."""
     dx, dg, db, dy, dm, dr = _here(x, gamma, beta, y, mean, rstd)
     _check(lib().chn_layer_norm_fwd(dx, dg, db, float(eps), dy, dm, dr, _stream() if stream is None else stream))
     return y

@@ -185,6 +185,10 @@ class GpuBackend:
     def rng_advance(self, rng, steps):
         self.B.rng_advance(rng, steps)
 
+    def mean_shape(self, n):
+        """Of the means that the normalisations of n rows keep for their backward passes: in two parts, so that no digit is lost."""
+        return (n, 2)
+
     def layer_norm_fwd(self, x, y, gamma, beta, eps, mean, rstd):
         self.B.layer_norm_fwd(x, y, gamma, beta, eps, mean, rstd)
 
@@ -1546,6 +1550,11 @@ class Dropout(FunctionNode):
         return (Dropout(self.ratio, self.masks, self.place, self.gx_dtype).apply((gys[0],))[0],)
 
 
+def _statistics(F, n):
+    """Memory for the means and the reciprocal deviations of n rows (a backend without `mean_shape` keeps a mean as one number)."""
+    return F.empty(F.mean_shape(n) if hasattr(F, "mean_shape") else (n,), "f32"), F.empty((n,), "f32")
+
+
 class LayerNormFunction(FunctionNode):
     """(x, gamma, beta) -> (x - mean) * rstd * gamma + beta over the rows of x; gamma and beta fp32.  Retains x and gamma and keeps the
     rows' statistics, so that the backward pass is one walk over x and the gradient."""
@@ -1559,7 +1568,7 @@ class LayerNormFunction(FunctionNode):
         F = backend()
         x, gamma, beta = xs
         y = F.empty(x.shape, self.out_dtype or F.dtype(x))
-        self.mean, self.rstd = F.empty((x.shape[0],), "f32"), F.empty((x.shape[0],), "f32")
+        self.mean, self.rstd = _statistics(F, x.shape[0])
         F.layer_norm_fwd(x, y, gamma, beta, self.eps, self.mean, self.rstd)
         self.retain_inputs((0, 1))
         return (y,)
@@ -1590,7 +1599,7 @@ class ResidualNorm(FunctionNode):
         F = backend()
         x, residual, gamma, beta = xs
         s, y = F.empty(residual.shape, F.dtype(residual)), F.empty(x.shape, F.dtype(x))
-        self.mean, self.rstd = F.empty((x.shape[0],), "f32"), F.empty((x.shape[0],), "f32")
+        self.mean, self.rstd = _statistics(F, x.shape[0])
         F.residual_norm_fwd(x, residual, s, y, gamma, beta, self.eps, self.mean, self.rstd, self.ratio, *_draw(self.masks, self.ratio, self.place))
         self.layer = F.dtype(x)
         self.retain_inputs((2,))
