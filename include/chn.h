@@ -489,8 +489,10 @@ chn_status chn_residual_norm_bwd(const chn_array *dy, const chn_array *dsum, con
  *     p times the sum of what is left, and always the first one; p >= 1 or NaN: all;
  *   - min_p: of what is left only tokens with w_i >= min(min_p, 1); 0, NaN: all;
  *   - the token: the first, in the order of indices, whose running sum of kept weights exceeds u times their sum.
- * Weights are summed as whole multiples of 2^-46 (of 2^-(63 - log2 V), V rounded up to a power of two, beyond 2^17 tokens), the exponential
- * in 64 bits: bit-reproducible, and no order of summation shows.  u below 0 or NaN counts as 0, from 1 on the last kept token is drawn.  V up to
+ * Weights are summed as whole multiples of 2^-46 (of 2^-(63 - log2 V), V rounded up to a power of two, beyond 2^17 tokens), of an exponential
+ * that is off by less than 2e-13 of itself: bit-reproducible, and no order of summation shows; a token lighter than half such a multiple counts for
+ * nothing in a sum.  min_p compares the exponential in 64 bits.  u of 0 and below or NaN draws the first kept token, from 1 on the last one is drawn, of
+ * those whose exponential is above 0 in 64 bits, however light.  V up to
  * 2^30; V = 0 with N > 0 is CHN_ERR_SHAPE.  Workspace: optional, chn_sample_workspace_bytes(logits), 256-byte aligned, the library's
  * until the work on `stream` is done; it lets several workgroups share a row.  Without it the same tokens, possibly later. */
 size_t chn_sample_workspace_bytes(const chn_array *logits);
