@@ -628,8 +628,9 @@ __device__ __forceinline__ void draw_small(Shared &sh, int M, const Asked &q, co
   sort_small(sh, M);
   const Rank r = (int)threadIdx.x < M && !(q.k > 0 && (int64_t)threadIdx.x >= q.k) ? sh.sorted[threadIdx.x] : 0;
   const float v = logit_of((uint32_t)(r >> 32));
-  const double e = r == 0 ? 0.0 : !q.inside() ? wt.exponential(v) : v >= wt.zero(q.t) ? wt.near(v) : 0.0;   // (the ends ask for the lightest)
+  double e = r != 0 && v >= wt.zero(q.t) ? wt.near(v) : 0.0;
   const u64 w = wt.of(e);
+  if (!q.inside()) e = r == 0 ? 0.0 : wt.exponential(v);   // (the ends ask for the lightest; top-p sums the same weights there)
   bool kept = r != 0;
   if (q.p < 1.0f) {
     u64 all;
@@ -939,8 +940,12 @@ __global__ __launch_bounds__(256) void sample_short_kernel(const T *logits, Samp
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
     kept[j] = z[j] > -INFINITY;
-    e[j] = !kept[j] ? 0.0 : !q.inside() ? wt.exponential(z[j]) : z[j] >= zero ? wt.near(z[j]) : 0.0;   // (the ends ask for the lightest)
+    e[j] = kept[j] && z[j] >= zero ? wt.near(z[j]) : 0.0;
     w[j] = wt.of(e[j]);
+  }
+  if (!q.inside()) {                                     // (the ends ask for the lightest; top-p sums the same weights there)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) e[j] = kept[j] ? wt.exponential(z[j]) : 0.0;
   }
   if (q.k > 0 || q.p < 1.0f) {
     uint32_t key[4], place[4];
