@@ -23,14 +23,14 @@ constexpr int kThreads = 1024, kWaves = kThreads / 64;
 constexpr int kBins = 2048;          // two for each thread
 constexpr int kFewBins = 256;        // for a bound: coarser, and read by every wave
 constexpr int kSmall = 1024;         // tokens that are ordered by comparing each with each
-constexpr int kMaxChunks = 32, kMaxParts = 4096;
+constexpr int kMaxChunks = 32, kMaxParts = 4096, kLeastParts = 1024;
 
 // What the launches over chunks leave for each other, of one row.
 struct RowSpace {
   u64 bins[kBins];                   // sums by bin
   u64 list[kSmall];                  // tokens of the border's bin
   u64 sums[kMaxChunks];              // kept weights of each chunk
-  float maxima[kMaxParts];           // of parts of 64 units; the tokens behind the last unit count to the last part
+  float maxima[kMaxParts];           // of parts; the tokens behind the last unit count to the last part
   float minima[kMaxParts];
   int count, pad[63];
 };
@@ -45,7 +45,9 @@ struct SampleArgs {
   void *out;
   int out64;
   RowSpace *space;
-  int chunks, chunk_units, parts;    // chunks are whole parts
+  int chunks, chunk_units;           // chunks are multiples of 64 units
+  int parts, part_bits;              // parts of a row, and the units of one: 2^2 to 2^6
+  int most_k;                        // of a top-k that the parts' maxima narrow to few tokens
 };
 
 // Monotone in the logit, -0 and 0 alike.  0: not a token that can be drawn (-inf, NaN).
@@ -1015,8 +1017,22 @@ __device__ __forceinline__ Span<T> chunk_of(const T *logits, const SampleArgs &a
   return Span<T>(logits + n * a.pitch, a.V, chunk * a.chunk_units, chunk + 1 == a.chunks ? a.V : (chunk + 1) * a.chunk_units);
 }
 
+// The largest over the PART lanes of a part, in all of these lanes.
+template <int PART>
+__device__ __forceinline__ float max_part(float v) {
+  if constexpr (PART == 64) return max64(v);
+  v = dpp_max<0x4E>(dpp_max<0xB1>(v));
+  if constexpr (PART >= 8) v = dpp_max<0x141>(v);
+  if constexpr (PART >= 16) v = dpp_max<0x140>(v);
+  if constexpr (PART >= 32) {
+    const auto row = [&](int r) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 16 * r)); };
+    v = (threadIdx.x & 63) < 32 ? fmaxf(row(0), row(1)) : fmaxf(row(2), row(3));
+  }
+  return v;
+}
+
 // Launch 1: the maxima and minima of all parts; what later launches add to is cleared.
-template <typename T>
+template <typename T, int PART>
 __global__ __launch_bounds__(kThreads) void sample_maxima_kernel(const T *logits, SampleArgs a) {
   constexpr int E = Span<T>::E, U = 4;
   const int64_t n = blockIdx.y;
@@ -1028,18 +1044,18 @@ __global__ __launch_bounds__(kThreads) void sample_maxima_kernel(const T *logits
     if (threadIdx.x == 0) space.count = 0;
   }
   const T *z = logits + n * a.pitch;
-  const int whole = a.V / E, p0 = chunk * (a.chunk_units / 64), p1 = min(a.parts, p0 + a.chunk_units / 64);
-  for (int p = p0 + wave; p < p1; p += kWaves * U) {
+  const int whole = a.V / E, u0 = chunk * a.chunk_units, u1 = min(whole, u0 + a.chunk_units);
+  for (int first = u0 + wave * 64; first < u1; first += kWaves * 64 * U) {
     Unit<T, E> t[U];
 #pragma unroll
     for (int j = 0; j < U; ++j) {
-      const int u = (p + j * kWaves) * 64 + lane;
-      if (p + j * kWaves < p1 && u < whole) t[j].load(z + u * E);
+      const int u = first + j * kWaves * 64 + lane;
+      if (first + j * kWaves * 64 < u1 && u < whole) t[j].load(z + u * E);
     }
 #pragma unroll
     for (int j = 0; j < U; ++j) {
-      const int at = p + j * kWaves, u = at * 64 + lane;
-      if (at >= p1) break;
+      const int base = first + j * kWaves * 64, u = base + lane;
+      if (base >= u1) break;
       float m = -INFINITY, l = INFINITY;
       const auto look = [&](float v) {
         m = fmaxf(m, v);
@@ -1049,10 +1065,14 @@ __global__ __launch_bounds__(kThreads) void sample_maxima_kernel(const T *logits
 #pragma unroll
         for (int i = 0; i < E; ++i) look(t[j].get(i));
       }
-      if (at == a.parts - 1 && whole * E + lane < a.V) look(Elem<T>::load(z + whole * E + lane));
-      m = max64(m);
-      l = -max64(-l);
-      if (lane == 0) {
+      const int at = base / PART + lane / PART;
+      if (base + 64 >= whole && at == a.parts - 1)       // the tokens behind the last unit, by the lanes of the last part
+#pragma unroll
+        for (int i = whole * E + lane % PART, k = 0; k < E - 1; i += PART, k += PART)
+          if (i < a.V) look(Elem<T>::load(z + i));
+      m = max_part<PART>(m);
+      l = -max_part<PART>(-l);
+      if (lane % PART == 0 && at < a.parts) {
         space.maxima[at] = m;
         space.minima[at] = l;
       }
@@ -1167,13 +1187,14 @@ __device__ __forceinline__ void parts_from(Shared &sh, const T *z, const SampleA
     for (int p = base + threadIdx.x; p < min(a.parts, base + 2 * kSmall); p += kThreads)
       if (space.maxima[p] >= least) hits[atomicAdd(&sh.slot, 1)] = p;
     __syncthreads();
-    const int n = sh.slot;
-    for (int h = wave; h < n; h += 2 * kWaves) {
+    const int n = sh.slot, per = 64 >> a.part_bits;       // parts that a wave looks at together
+    for (int h = wave * per; h < n; h += 2 * kWaves * per) {
       Unit<T, E> t[2];
       int u[2];
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
-        u[j] = h + j * kWaves < n ? __builtin_amdgcn_readfirstlane(hits[h + j * kWaves]) * 64 + lane : whole;
+        const int at = h + j * kWaves * per + (lane >> a.part_bits);
+        u[j] = at < n ? (hits[at] << a.part_bits) + (lane & ((1 << a.part_bits) - 1)) : whole;
         if (u[j] < whole) t[j].load(z + u[j] * E);
       }
 #pragma unroll
@@ -1217,7 +1238,7 @@ __global__ __launch_bounds__(kThreads) void sample_draw_kernel(const T *logits, 
   if (plan.way == kFew) {
     // the k-th largest of the parts' maxima is a bound (to the width of a bin)
     const Bins<kFewBins> few(plan.best, plan.best - plan.low);
-    const int last = bin_of_kth(sh, q.k, [&](auto add) {
+    const int last = q.k > a.most_k ? -1 : bin_of_kth(sh, q.k, [&](auto add) {
       for (int p = threadIdx.x; p < a.parts; p += kThreads) {
         const float m = space.maxima[p];
         if (m > -INFINITY) add(few.of(m));
@@ -1321,11 +1342,27 @@ void launch(const chn_array *logits, SampleArgs &a, hipStream_t st) {
     return;
   }
   const int units = a.V / Span<T>::E;
-  a.parts = (units + 63) / 64;
-  a.chunk_units = (a.parts + a.chunks - 1) / a.chunks * 64;
-  a.chunks = (a.parts * 64 + a.chunk_units - 1) / a.chunk_units;   // (none without a part)
+  // The k-th largest of the parts' maxima bounds a top-k, so as many parts as a block that has the whole row has threads: the two ways narrow the same k.
+  // (With parts of 64 units, bfloat16 rows of 32768 tokens had 64 of them, and a top-k beyond that went through the row in passes.)
+  const auto parts = [&](int bits) { return (units + (1 << bits) - 1) >> bits; };
+  a.part_bits = 6;
+  while (a.part_bits > 2 && parts(a.part_bits) < kLeastParts) --a.part_bits;
+  a.parts = parts(a.part_bits);
+  // Tokens in no order: P ln(P / (P - k)) of them reach the k-th largest of the maxima of P parts.  Beyond kSmall of them, and a bound is no
+  // finer than its bin, gathering is for nothing (1 x 131072 bf16 with a top-k of 1000: 92 us with it, 73).
+  a.most_k = (int)(a.parts * (1.0 - exp(-0.75 * kSmall / a.parts)));
+  const int blocks = (units + 63) / 64;
+  a.chunk_units = (blocks + a.chunks - 1) / a.chunks * 64;
+  a.chunks = (blocks * 64 + a.chunk_units - 1) / a.chunk_units;   // (none without a unit)
   const dim3 grid((unsigned)a.chunks, (unsigned)a.N);
-  hipLaunchKernelGGL((sample_maxima_kernel<T>), grid, threads, 0, st, z, a);
+#define CHN_MAXIMA(BITS) \
+  if (a.part_bits == BITS) hipLaunchKernelGGL((sample_maxima_kernel<T, 1 << BITS>), grid, threads, 0, st, z, a)
+  CHN_MAXIMA(2);
+  CHN_MAXIMA(3);
+  CHN_MAXIMA(4);
+  CHN_MAXIMA(5);
+  CHN_MAXIMA(6);
+#undef CHN_MAXIMA
   hipLaunchKernelGGL((sample_bins_kernel<T>), grid, threads, 0, st, z, a);
   if (a.top_p) hipLaunchKernelGGL((sample_border_kernel<T>), grid, threads, 0, st, z, a);
   hipLaunchKernelGGL((sample_draw_kernel<T>), dim3((unsigned)a.N), threads, 0, st, z, a);
