@@ -185,24 +185,32 @@ class GpuBackend:
     def rng_advance(self, rng, steps):
         self.B.rng_advance(rng, steps)
 
+    # Normalisation and sampling walk over rows that lie one after the other; other views (a transposed array, a row that is repeated) are copied first.
+    def _rows(self, a):
+        if a is None or a.is_contiguous() or (a.dim() == 2 and a.stride(1) == 1 and a.stride(0) >= a.shape[1]):
+            return a
+        return self.B.elementwise_broadcast("copy", [a], self.torch.empty(a.shape, dtype=a.dtype, device=a.device))
+
     def mean_shape(self, n):
         """Of the means that the normalisations of n rows keep for their backward passes: in two parts, so that no digit is lost."""
         return (n, 2)
 
     def layer_norm_fwd(self, x, y, gamma, beta, eps, mean, rstd):
-        self.B.layer_norm_fwd(x, y, gamma, beta, eps, mean, rstd)
+        self.B.layer_norm_fwd(self._rows(x), y, gamma, beta, eps, mean, rstd)
 
     def layer_norm_bwd(self, dy, x, mean, rstd, dx, gamma, dgamma, dbeta):
-        self.B.layer_norm_bwd(dy, x, mean, rstd, dx, gamma, dgamma, dbeta, ws=self._bytes(self.B.layer_norm_bwd_workspace_bytes(x)))
+        x = self._rows(x)
+        self.B.layer_norm_bwd(self._rows(dy), x, mean, rstd, dx, gamma, dgamma, dbeta, ws=self._bytes(self.B.layer_norm_bwd_workspace_bytes(x)))
 
     def residual_norm_fwd(self, x, residual, s, y, gamma, beta, eps, mean, rstd, ratio, rng, site):
-        self.B.residual_norm_fwd(x, residual, s, y, gamma, beta, eps, mean, rstd, ratio, rng, site)
+        self.B.residual_norm_fwd(self._rows(x), self._rows(residual), s, y, gamma, beta, eps, mean, rstd, ratio, rng, site)
 
     def residual_norm_bwd(self, dy, ds, s, mean, rstd, dresidual, dx, gamma, dgamma, dbeta, ratio, rng, site):
-        self.B.residual_norm_bwd(dy, ds, s, mean, rstd, dresidual, dx, gamma, dgamma, dbeta, ratio, rng, site,
+        self.B.residual_norm_bwd(self._rows(dy), self._rows(ds), s, mean, rstd, dresidual, dx, gamma, dgamma, dbeta, ratio, rng, site,
                                  ws=self._bytes(self.B.layer_norm_bwd_workspace_bytes(s)))
 
     def sample(self, logits, u, out, temperature=None, top_k=None, top_p=None, min_p=None):
+        logits = self._rows(logits)
         self.B.sample(logits, u, out, temperature, top_k, top_p, min_p, ws=self._bytes(self.B.sample_workspace_bytes(logits)))
 
     def sgd_update_multi(self, params, grads, lr, lowp_copies):
