@@ -1563,6 +1563,16 @@ def _statistics(F, n):
     return F.empty(F.mean_shape(n) if hasattr(F, "mean_shape") else (n,), "f32"), F.empty((n,), "f32")
 
 
+def _in_type(F, g, dtype):
+    """A gradient in the storage type of the array that it belongs to.  (A function may hand fp32 to a bfloat16 input; this rounds it as that input's
+    other gradients are rounded.)"""
+    if g is None or F.dtype(g) == dtype:
+        return g
+    out = F.empty(g.shape, dtype)
+    F.elementwise_broadcast("copy", [g], out)
+    return out
+
+
 class LayerNormFunction(FunctionNode):
     """(x, gamma, beta) -> (x - mean) * rstd * gamma + beta over the rows of x; gamma and beta fp32.  Retains x and gamma and keeps the
     rows' statistics, so that the backward pass is one walk over x and the gradient."""
@@ -1625,6 +1635,7 @@ class ResidualNorm(FunctionNode):
         if gy is None:                                   # (only the sum was used)
             gy = F.empty(s.shape, self.layer)
             F.elementwise_broadcast("fill", [], gy, (0.0,))
+        gy, gs = _in_type(F, gy, self.layer), _in_type(F, gs, F.dtype(s))
         new = lambda i, shape, dtype: F.empty(shape, dtype) if i in indexes else None
         out = {0: new(0, s.shape, self.layer), 1: new(1, s.shape, F.dtype(s)), 2: new(2, (s.shape[1],), "f32"), 3: new(3, (s.shape[1],), "f32")}
         F.residual_norm_bwd(gy, gs, s, self.mean, self.rstd, out[1], out[0], gamma, out[2], out[3], self.ratio,
