@@ -2019,15 +2019,19 @@ class LSTMLanguageModel:
 
     def generate(self, ids, n_steps, u, state=None, temperature=None, top_k=None, top_p=None, min_p=None):
         """Continues a prompt.  ids: flat (T*B,) integer array of `n_steps` steps, time-major; u: (n, B) array of fp32 numbers in [0, 1), one for
-        each token that is wanted.  temperature, top_k, top_p, min_p: a number, an array with one for each of the B sequences, or None
-        (not used).  Returns the (n, B) int64 array of tokens and the state after the last but one, which has seen everything but the
+        each token that is wanted.  temperature, top_k, top_p, min_p: a number, one for each of the B sequences (an array of the backend's, a
+        NumPy array, a list), or None (not used).  Returns the (n, B) int64 array of tokens and the state after the last but one, which has seen everything but the
         last token.  Nothing is recorded and nothing is dropped."""
         import numpy as np
         F = backend()
         if n_steps < 1 or len(u.shape) != 2 or u.shape[0] < 1 or ids.shape[0] != n_steps * u.shape[1]:
             raise ValueError("LSTMLanguageModel.generate: %d ids of %d steps for u of shape %s" % (ids.shape[0], n_steps, tuple(u.shape)))
         Bn = u.shape[1]
-        row = lambda v, dt: v if v is None or hasattr(v, "shape") else F.from_numpy(np.full((Bn,), v, dtype=dt))
+
+        def row(v, dt):
+            if v is None or (hasattr(v, "shape") and not isinstance(v, (np.generic, np.ndarray))):
+                return v
+            return F.from_numpy(np.broadcast_to(np.asarray(v, dtype=dt), (Bn,)))
         filters = (row(temperature, np.float32), row(top_k, np.int64), row(top_p, np.float32), row(min_p, np.float32))
         out = F.empty(tuple(u.shape), "i64")
         was, self.train = self.train, False
