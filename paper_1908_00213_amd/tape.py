@@ -1976,10 +1976,12 @@ class LSTMLanguageModel:
     def params(self):
         return list(self.P.values())
 
-    def _hidden(self, ids, n_steps, state):
-        """The hidden states of all steps, (T*B, H), as the output layer is to see them, and the state after the last."""
+    def _hidden(self, ids, n_steps, state, ratio=None):
+        """The hidden states of all steps, (T*B, H), as the output layer is to see them, and the state after the last.  ratio: of the dropout, None:
+        the model's while it trains."""
         P, F = self.P, backend()
-        ratio = self.ratio if self.train else 0.0
+        if ratio is None:
+            ratio = self.ratio if self.train else 0.0
         X = embed_id(ids, P["E"])
         if ratio > 0.0:
             X = dropout(X, ratio, self.masks, gx_dtype="f32")
@@ -2002,9 +2004,10 @@ class LSTMLanguageModel:
             hs = concat_rows(hs)
         return hs, (c, h)
 
-    def _logits(self, hs):
+    def _logits(self, hs, ratio=None):
         P = self.P
-        ratio = self.ratio if self.train else 0.0
+        if ratio is None:
+            ratio = self.ratio if self.train else 0.0
         if ratio > 0.0:
             hs = dropout(hs, ratio, self.masks)
         if "gamma" in P:
@@ -2034,14 +2037,10 @@ class LSTMLanguageModel:
             return F.from_numpy(np.broadcast_to(np.asarray(v, dtype=dt), (Bn,)))
         filters = (row(temperature, np.float32), row(top_k, np.int64), row(top_p, np.float32), row(min_p, np.float32))
         out = F.empty(tuple(u.shape), "i64")
-        was, self.train = self.train, False
-        try:
-            with no_backprop_mode():
-                for t in range(u.shape[0]):
-                    hs, state = self._hidden(ids, n_steps, state)
-                    last = Variable(hs.array[(n_steps - 1) * Bn:], requires_grad=False)
-                    F.sample(self._logits(last).array, u[t], out[t], *filters)
-                    ids, n_steps = out[t], 1
-        finally:
-            self.train = was
+        with no_backprop_mode():
+            for t in range(u.shape[0]):
+                hs, state = self._hidden(ids, n_steps, state, 0.0)
+                last = Variable(hs.array[(n_steps - 1) * Bn:], requires_grad=False)
+                F.sample(self._logits(last, 0.0).array, u[t], out[t], *filters)
+                ids, n_steps = out[t], 1
         return out, state
