@@ -2034,7 +2034,7 @@ class LSTMLanguageModel:
         def row(v, dt):
             if v is None or (hasattr(v, "shape") and not isinstance(v, (np.generic, np.ndarray))):
                 return v
-            return F.from_numpy(np.broadcast_to(np.asarray(v, dtype=dt), (Bn,)))
+            return F.from_numpy(np.array(np.broadcast_to(np.asarray(v, dtype=dt), (Bn,))))
         filters = (row(temperature, np.float32), row(top_k, np.int64), row(top_p, np.float32), row(min_p, np.float32))
         out = F.empty(tuple(u.shape), "i64")
         with no_backprop_mode():
