@@ -8,6 +8,7 @@ The library must have been built (``python -m paper_1908_00213_amd.build``); the
 """
 import ctypes as C
 import os
+import struct
 
 import torch
 
@@ -76,8 +77,8 @@ def lib():
         raise ImportError("libchn.so is missing: run `python -m paper_1908_00213_amd.build` "
                           "(there is no CPU fallback)")
     L = C.CDLL(LIB_PATH)
-    AP = C.POINTER(ChnArray)
-    APP = C.POINTER(AP)
+    AP = C.c_void_p                    # a reference (`_arg`): as a pointer to ChnArray by type it costs 50 ns more for each array of a call
+    APP = C.POINTER(C.POINTER(ChnArray))
     vp, st = C.c_void_p, C.c_void_p
     L.chn_elementwise_broadcast.argtypes = [C.c_int, C.c_int, APP, AP, C.POINTER(C.c_float), C.c_int, st]
     L.chn_elementwise_plan.argtypes = [C.c_int, C.c_int, APP, AP]
@@ -165,52 +166,113 @@ def lib():
     return L
 
 
+class _Kept:
+    """A tensor's descriptor, with the reference to it that calls take and what shows whether it still holds: the tensor's address, which another storage
+    changes, and its version, which every operation in place changes.  A tensor that is copied or pickled carries nothing in its place."""
+    __slots__ = ("ref", "ptr", "version", "device", "desc", "pointer", "shape", "strides")
+
+    def __reduce__(self):
+        return set, ()
+
+    def __deepcopy__(self, memo):
+        return None
+
+
+# By dtype: the descriptor's code and the element's bytes; by the number of dimensions: a descriptor's fields, which are written in one go.
+_ELEMENTS = {t: (code, torch.empty(0, dtype=t).element_size()) for t, code in _DTYPES.items()}
+_FIELDS = [struct.Struct("@Pi4x%dq%dx%dq%dxi4x" % (n, 8 * (MAX_NDIM - n), n, 8 * (MAX_NDIM - n))) for n in range(MAX_NDIM + 1)]
+assert all(f.size == C.sizeof(ChnArray) for f in _FIELDS)
+
+
+def _describe(t):
+    """The descriptor of a tensor, kept on it from here on: parameters, inputs and gradients are described thousands of times."""
+    k = _Kept()
+    k.desc = a = ChnArray()
+    k.shape = shape = t.shape
+    k.strides = strides = t.stride()
+    k.ptr = ptr = t.data_ptr()
+    code, size = _ELEMENTS[t.dtype]
+    n = len(shape)
+    _FIELDS[n].pack_into(a, 0, ptr, n, *shape, *[s * size for s in strides], code)
+    k.ref, k.pointer, k.device = C.byref(a), None, None      # (the latter two when they are asked for)
+    try:
+        k.version = t._version
+    except RuntimeError:                                 # (not counted in inference mode)
+        k.version = None
+    t._chn_kept = k
+    return k
+
+
+def _again(t):
+    """What is kept on a tensor of which nothing is known yet, or whose address or version is another one: made anew where more has changed than what it holds."""
+    k = getattr(t, "_chn_kept", None)
+    if type(k) is not _Kept or k.ptr != t.data_ptr() or k.shape != t.shape or k.strides != t.stride():
+        return _describe(t)
+    same = _Kept()                                       # (the old one may be kept on a shallow copy too)
+    same.ref, same.ptr, same.version, same.device, same.desc = k.ref, k.ptr, None if t.is_inference() else t._version, k.device, k.desc
+    same.pointer, same.shape, same.strides = k.pointer, k.shape, k.strides
+    t._chn_kept = same
+    return same
+
+
+def _kept(t):
+    """The descriptor of a tensor, as it is now: after resize_, set_, transpose_, an `out=` that resized it, an assignment to .data.  (Only an assignment to .data of
+    another view of the very same memory shows nowhere.)"""
+    try:
+        k = t._chn_kept
+        if k.ptr == t.data_ptr() and k.version == t._version:
+            return k
+    except (AttributeError, RuntimeError):               # (none yet, or what a copied tensor carries; a version that is not counted)
+        pass
+    return _again(t)
+
+
 def desc(t):
-    """chn_array descriptor of a tensor (or None).  The descriptor is kept on the tensor object: a
-    tensor's storage pointer, shape and strides do not change for the life of the object (this
-    package never calls the in-place re-shaping methods that could), and parameters, inputs and
-    gradients are described thousands of times."""
+    """chn_array descriptor of a tensor (or None).  It holds as long as the tensor is not given other memory or another shape."""
+    if t is None or type(t) is ChnArray:
+        return t
+    return _kept(t).desc
+
+
+def _arg(t):
+    """A call's argument for a tensor, a descriptor or None."""
     if t is None:
         return None
-    if isinstance(t, ChnArray):
-        return t
-    try:
-        return t._chn_desc
-    except AttributeError:
-        pass
-    a = ChnArray()
-    n = t.dim()
-    isz = t.element_size()
-    a.data = t.data_ptr()
-    a.ndim = n
-    a.shape[:n] = t.shape
-    a.strides[:n] = [s * isz for s in t.stride()]
-    a.dtype = _DTYPES[t.dtype]
-    a.device = t.get_device()
-    t._chn_desc = a
-    return a
+    return C.byref(t) if type(t) is ChnArray else _kept(t).ref
 
 
 def _here(*arrays):
-    """References to the arrays' descriptors, which have to lie on the current device, whose stream the call goes to.  (The reference is
-    kept beside the descriptor: a call with twelve arrays spends more time on these than on its launch.)"""
+    """References for `_raw` calls to the descriptors of arrays, which have to lie on the current device, whose stream the call goes to (of a descriptor that is not known).
+    (A call with twelve arrays spends more time on these than on its launch.)"""
     current = _raw_device() if _raw_device is not None else torch.cuda.current_device()
-    out = []
-    for t in arrays:
-        if t is None:
-            out.append(None)
-            continue
-        try:
-            ref, device = t._chn_here
-        except AttributeError:
-            d = desc(t)
-            ref, device = C.byref(d), getattr(d, "device", current)
-            if d is not t:
-                t._chn_here = ref, device
-        if device != current:
-            raise ValueError("an array lies on %s, the current device is cuda:%d" % ("the host" if device < 0 else "cuda:%d" % device, current))
-        out.append(ref)
-    return out
+    try:
+        return [None if t is None else k.ref if (k := t._chn_kept).ptr == t.data_ptr() and k.version == t._version and k.device == current else _look(t, current)
+                for t in arrays]
+    except (AttributeError, RuntimeError):
+        return [None if t is None else _look(t, current) for t in arrays]
+
+
+def _look(t, current):
+    if type(t) is ChnArray:
+        return C.byref(t)
+    k = _again(t)
+    if k.device is None:
+        k.device = t.get_device()
+    if k.device != current:
+        raise ValueError("an array lies on %s, the current device is cuda:%d" % ("the host" if k.device < 0 else "cuda:%d" % k.device, current))
+    return k.ref
+
+
+class _RawCalls(dict):
+    """The entry points without argument types, whose conversions cost half a microsecond a call: they are given references, ctypes numbers and None only."""
+
+    def __missing__(self, name):
+        f = self[name] = lib()[name]
+        f.restype = C.c_int32
+        return f
+
+
+_raw = _RawCalls()
 
 
 def raw_desc(ptr, shape, strides_bytes, dtype):
@@ -230,11 +292,25 @@ def _ref(a):
     return None if a is None else C.byref(a)
 
 
-def _ptrs(descs):
-    AP = C.POINTER(ChnArray)
-    arr = (AP * max(1, len(descs)))()
-    for i, d in enumerate(descs):
-        arr[i] = C.pointer(d) if d is not None else AP()
+_POINTER_ARRAYS = {}               # by length
+
+
+def _ptrs(arrays):
+    """Pointers to the descriptors of tensors, or to descriptors; NULL for None."""
+    n = len(arrays)
+    make = _POINTER_ARRAYS.get(n)
+    if make is None:
+        make = _POINTER_ARRAYS[n] = C.POINTER(ChnArray) * max(1, n)
+    arr = make()
+    for i, t in enumerate(arrays):
+        if t is not None:
+            if type(t) is ChnArray:
+                arr[i] = C.pointer(t)
+                continue
+            k = _kept(t)
+            if k.pointer is None:
+                k.pointer = C.pointer(k.desc)
+            arr[i] = k.pointer
     return arr
 
 
@@ -263,10 +339,17 @@ def _ws(t):
 
 
 def _ws_here(t):
-    """The same for calls whose arrays have to lie on the current device."""
-    if t is not None and t.get_device() != (_raw_device() if _raw_device is not None else torch.cuda.current_device()):
+    """The same for `_raw` calls whose arrays have to lie on the current device."""
+    if t is None:
+        return None, C.c_size_t(0)
+    if t.get_device() != (_raw_device() if _raw_device is not None else torch.cuda.current_device()):
         raise ValueError("the workspace does not lie on the current device")
-    return _ws(t)
+    return C.c_void_p(t.data_ptr()), C.c_size_t(t.numel() * t.element_size())
+
+
+def _on(stream):
+    """A stream's handle for a `_raw` call."""
+    return stream if isinstance(stream, C.c_void_p) else C.c_void_p(stream)
 
 
 def version():
@@ -274,15 +357,13 @@ def version():
 
 
 def elementwise_plan(op, inputs, out):
-    ds = [desc(x) for x in inputs]
-    return lib().chn_elementwise_plan(OP[op] if isinstance(op, str) else op, len(ds), _ptrs(ds), _ref(desc(out)))
+    return lib().chn_elementwise_plan(OP[op] if isinstance(op, str) else op, len(inputs), _ptrs(inputs), _arg(out))
 
 
 def elementwise_broadcast(op, inputs, out, scalars=(), stream=None):
-    ds = [desc(x) for x in inputs]
     sc = (C.c_float * max(1, len(scalars)))(*[float(s) for s in scalars])
-    _check(lib().chn_elementwise_broadcast(OP[op] if isinstance(op, str) else op, len(ds), _ptrs(ds),
-                                           _ref(desc(out)), sc, len(scalars),
+    _check(lib().chn_elementwise_broadcast(OP[op] if isinstance(op, str) else op, len(inputs), _ptrs(inputs),
+                                           _arg(out), sc, len(scalars),
                                            _stream() if stream is None else stream))
     return out
 
@@ -304,8 +385,8 @@ def reduce_axis(op, x, axis, out, keepdims=False, ws=None, stream=None):
     """axis: an int, a tuple of ints (several axes at once) or None (all of them)."""
     p, n = _ws(ws)
     axis = _axis_code(axis, desc(x).ndim)
-    _check(lib().chn_reduce_axis(REDUCE[op] if isinstance(op, str) else op, _ref(desc(x)), axis,
-                                 int(keepdims), _ref(desc(out)), p, n,
+    _check(lib().chn_reduce_axis(REDUCE[op] if isinstance(op, str) else op, _arg(x), axis,
+                                 int(keepdims), _arg(out), p, n,
                                  _stream() if stream is None else stream))
     return out
 
@@ -314,24 +395,24 @@ def reduce_axis_static(op, x, axis, out, keepdims=False, stream=None):
     """reduce_axis without a workspace argument and without any allocation (partial sums in the
     library's built-in per-device array)."""
     axis = _axis_code(axis, desc(x).ndim)
-    _check(lib().chn_reduce_axis_static(REDUCE[op] if isinstance(op, str) else op, _ref(desc(x)), axis,
-                                        int(keepdims), _ref(desc(out)), _stream() if stream is None else stream))
+    _check(lib().chn_reduce_axis_static(REDUCE[op] if isinstance(op, str) else op, _arg(x), axis,
+                                        int(keepdims), _arg(out), _stream() if stream is None else stream))
     return out
 
 
 def argmax_axis(x, axis, out, keepdims=False, stream=None):
-    _check(lib().chn_argmax_axis(_ref(desc(x)), int(axis), int(keepdims), _ref(desc(out)),
+    _check(lib().chn_argmax_axis(_arg(x), int(axis), int(keepdims), _arg(out),
                                  _stream() if stream is None else stream))
     return out
 
 
 def gemm_workspace_bytes(A, B, Cm):
-    return lib().chn_gemm_workspace_bytes(_ref(desc(A)), _ref(desc(B)), _ref(desc(Cm)))
+    return lib().chn_gemm_workspace_bytes(_arg(A), _arg(B), _arg(Cm))
 
 
 def gemm_plan(A, B, Cm, have_workspace=False):
     """(tile, direct_copy, splits) chn_gemm would use: tile 0/1/2 = 64/128/256 square, 3 = 256 x 128."""
-    code = lib().chn_gemm_plan(_ref(desc(A)), _ref(desc(B)), _ref(desc(Cm)), 1 if have_workspace else 0)
+    code = lib().chn_gemm_plan(_arg(A), _arg(B), _arg(Cm), 1 if have_workspace else 0)
     if code < 0:
         _check(code)
     return code & 3, bool(code & 4), code >> 4
@@ -340,7 +421,7 @@ def gemm_plan(A, B, Cm, have_workspace=False):
 def gemm_plan_eight_waves(A, B, Cm, have_workspace=False):
     """Whether the plain product would run on the eight-wave form of the direct-copy kernel (bf16) or on the
     three-part kernel (fp32)."""
-    code = lib().chn_gemm_plan(_ref(desc(A)), _ref(desc(B)), _ref(desc(Cm)), 1 if have_workspace else 0)
+    code = lib().chn_gemm_plan(_arg(A), _arg(B), _arg(Cm), 1 if have_workspace else 0)
     if code < 0:
         _check(code)
     return bool(code & 8)
@@ -351,7 +432,7 @@ GEMM_KERNELS = ("staged", "direct4", "direct8", "parts", "small")
 
 def gemm_plan_kernel(A, B, Cm, have_workspace=False):
     """The kernel the plain product would run on, one of GEMM_KERNELS."""
-    code = lib().chn_gemm_plan_kernel(_ref(desc(A)), _ref(desc(B)), _ref(desc(Cm)), 1 if have_workspace else 0)
+    code = lib().chn_gemm_plan_kernel(_arg(A), _arg(B), _arg(Cm), 1 if have_workspace else 0)
     if code < 0:
         _check(code)
     return GEMM_KERNELS[code]
@@ -365,20 +446,20 @@ def gemm_plan_override(tile=-1, splits=-1, direct_copy=-1):
 def gemm(A, B, Cm, alpha=1.0, beta=0.0, epilogue="none", bias=None, aux=None, preact_out=None,
          ws=None, stream=None):
     p, n = _ws(ws)
-    _check(lib().chn_gemm(_ref(desc(A)), _ref(desc(B)), _ref(desc(Cm)), float(alpha), float(beta),
+    _check(lib().chn_gemm(_arg(A), _arg(B), _arg(Cm), float(alpha), float(beta),
                           EPI[epilogue] if isinstance(epilogue, str) else epilogue,
-                          _ref(desc(bias)), _ref(desc(aux)), _ref(desc(preact_out)), p, n,
+                          _arg(bias), _arg(aux), _arg(preact_out), p, n,
                           _stream() if stream is None else stream))
     return Cm
 
 
 def linear_bwd_workspace_bytes(dv, W, x, dx, dW):
-    return lib().chn_linear_bwd_workspace_bytes(_ref(desc(dv)), _ref(desc(W)), _ref(desc(x)), _ref(desc(dx)), _ref(desc(dW)))
+    return lib().chn_linear_bwd_workspace_bytes(_arg(dv), _arg(W), _arg(x), _arg(dx), _arg(dW))
 
 
 def linear_bwd_in_one_launch(dv, W, x, dx, dW):
     """Whether linear_bwd would be one kernel (outputs apart from the other arrays)."""
-    code = lib().chn_linear_bwd_plan(_ref(desc(dv)), _ref(desc(W)), _ref(desc(x)), _ref(desc(dx)), _ref(desc(dW)))
+    code = lib().chn_linear_bwd_plan(_arg(dv), _arg(W), _arg(x), _arg(dx), _arg(dW))
     if code < 0:
         _check(code)
     return bool(code)
@@ -387,30 +468,30 @@ def linear_bwd_in_one_launch(dv, W, x, dx, dW):
 def linear_bwd(dv, W, x, dW, db=None, dx=None, epilogue="none", aux=None, ws=None, stream=None):
     """dW = dv^T x, db = column sums of dv, dx = epilogue(dv W): the backward of y = x W^T + b."""
     p, n = _ws(ws)
-    _check(lib().chn_linear_bwd(_ref(desc(dv)), _ref(desc(W)), _ref(desc(x)), EPI[epilogue] if isinstance(epilogue, str) else epilogue,
-                                _ref(desc(aux)), _ref(desc(dx)), _ref(desc(dW)), _ref(desc(db)), p, n,
+    _check(lib().chn_linear_bwd(_arg(dv), _arg(W), _arg(x), EPI[epilogue] if isinstance(epilogue, str) else epilogue,
+                                _arg(aux), _arg(dx), _arg(dW), _arg(db), p, n,
                                 _stream() if stream is None else stream))
 
 
 def lstm_fwd(z, bias, c_prev, c, h, gates=None, stream=None):
-    _check(lib().chn_lstm_fwd(_ref(desc(z)), _ref(desc(bias)), _ref(desc(c_prev)), _ref(desc(c)),
-                              _ref(desc(h)), _ref(desc(gates)), _stream() if stream is None else stream))
+    _check(lib().chn_lstm_fwd(_arg(z), _arg(bias), _arg(c_prev), _arg(c),
+                              _arg(h), _arg(gates), _stream() if stream is None else stream))
 
 
 def lstm_bwd(gates, c_prev, c, dh, dc_next, dz, dc_prev, stream=None):
-    _check(lib().chn_lstm_bwd(_ref(desc(gates)), _ref(desc(c_prev)), _ref(desc(c)), _ref(desc(dh)),
-                              _ref(desc(dc_next)), _ref(desc(dz)), _ref(desc(dc_prev)),
+    _check(lib().chn_lstm_bwd(_arg(gates), _arg(c_prev), _arg(c), _arg(dh),
+                              _arg(dc_next), _arg(dz), _arg(dc_prev),
                               _stream() if stream is None else stream))
 
 
 def lstm_step_fwd(zx, h_prev, Ut, bias, c_prev, c, h, gates=None, stream=None):
-    _check(lib().chn_lstm_step_fwd(_ref(desc(zx)), _ref(desc(h_prev)), _ref(desc(Ut)), _ref(desc(bias)), _ref(desc(c_prev)),
-                                   _ref(desc(c)), _ref(desc(h)), _ref(desc(gates)), _stream() if stream is None else stream))
+    _check(lib().chn_lstm_step_fwd(_arg(zx), _arg(h_prev), _arg(Ut), _arg(bias), _arg(c_prev),
+                                   _arg(c), _arg(h), _arg(gates), _stream() if stream is None else stream))
 
 
 def lstm_step_bwd(dz_next, U, dh, gates, c_prev, c, dc_next, dz, dc_prev, stream=None):
-    _check(lib().chn_lstm_step_bwd(_ref(desc(dz_next)), _ref(desc(U)), _ref(desc(dh)), _ref(desc(gates)), _ref(desc(c_prev)),
-                                   _ref(desc(c)), _ref(desc(dc_next)), _ref(desc(dz)), _ref(desc(dc_prev)),
+    _check(lib().chn_lstm_step_bwd(_arg(dz_next), _arg(U), _arg(dh), _arg(gates), _arg(c_prev),
+                                   _arg(c), _arg(dc_next), _arg(dz), _arg(dc_prev),
                                    _stream() if stream is None else stream))
 
 
@@ -431,8 +512,8 @@ def lstm_seq_status(ws):
 def lstm_seq_fwd(zx, Ut, bias, Hs, Cs, gates, n_steps, ws, stream=None):
     """All n_steps forward steps in one launch.  ws[0:4] reads 1 after synchronisation if a wait ran out."""
     p, n = _ws(ws)
-    _check(lib().chn_lstm_seq_fwd(_ref(desc(zx)), _ref(desc(Ut)), _ref(desc(bias)), _ref(desc(Hs)), _ref(desc(Cs)),
-                                  _ref(desc(gates)), int(n_steps), p, n, _stream() if stream is None else stream))
+    _check(lib().chn_lstm_seq_fwd(_arg(zx), _arg(Ut), _arg(bias), _arg(Hs), _arg(Cs),
+                                  _arg(gates), int(n_steps), p, n, _stream() if stream is None else stream))
 
 
 def lstm_seq_bwd_supported(batch, hidden, dtype):
@@ -452,8 +533,8 @@ def lstm_seq_bwd_workspace_bytes(batch, hidden):
 def lstm_seq_bwd(U, dHs, gates, Cs, dc_last, dZ, dc0, n_steps, ws, stream=None):
     """Back-propagation through all n_steps steps in one launch; status word in ws as for lstm_seq_fwd."""
     p, n = _ws(ws)
-    _check(lib().chn_lstm_seq_bwd(_ref(desc(U)), _ref(desc(dHs)), _ref(desc(gates)), _ref(desc(Cs)), _ref(desc(dc_last)),
-                                  _ref(desc(dZ)), _ref(desc(dc0)), int(n_steps), p, n, _stream() if stream is None else stream))
+    _check(lib().chn_lstm_seq_bwd(_arg(U), _arg(dHs), _arg(gates), _arg(Cs), _arg(dc_last),
+                                  _arg(dZ), _arg(dc0), int(n_steps), p, n, _stream() if stream is None else stream))
 
 
 def lstm_seq_spin_limit(polls):
@@ -471,8 +552,8 @@ def softmax_ce_workspace_bytes(n_rows):
 def softmax_ce_fwd(logits, labels, loss_mean, loss_rows=None, lse=None, ignore_label=-1, ws=None,
                    stream=None):
     p, n = _ws(ws)
-    _check(lib().chn_softmax_ce_fwd(_ref(desc(logits)), _ref(desc(labels)), int(ignore_label),
-                                    _ref(desc(loss_mean)), _ref(desc(loss_rows)), _ref(desc(lse)), p, n,
+    _check(lib().chn_softmax_ce_fwd(_arg(logits), _arg(labels), int(ignore_label),
+                                    _arg(loss_mean), _arg(loss_rows), _arg(lse), p, n,
                                     _stream() if stream is None else stream))
     return loss_mean
 
@@ -480,16 +561,16 @@ def softmax_ce_fwd(logits, labels, loss_mean, loss_rows=None, lse=None, ignore_l
 def softmax_ce_bwd(logits, labels, dlogits, lse=None, upstream=1.0, ignore_label=-1, ws=None,
                    stream=None):
     p, n = _ws(ws)
-    _check(lib().chn_softmax_ce_bwd(_ref(desc(logits)), _ref(desc(labels)), int(ignore_label),
-                                    _ref(desc(lse)), float(upstream), _ref(desc(dlogits)), p, n,
+    _check(lib().chn_softmax_ce_bwd(_arg(logits), _arg(labels), int(ignore_label),
+                                    _arg(lse), float(upstream), _arg(dlogits), p, n,
                                     _stream() if stream is None else stream))
     return dlogits
 
 
 def softmax_ce_bwd2(logits, labels, gg, dlogits, dupstream=None, lse=None, upstream=1.0, ignore_label=-1, ws=None, stream=None):
     p, n = _ws(ws)
-    _check(lib().chn_softmax_ce_bwd2(_ref(desc(logits)), _ref(desc(labels)), int(ignore_label), _ref(desc(lse)), float(upstream),
-                                     _ref(desc(gg)), _ref(desc(dlogits)), _ref(desc(dupstream)), p, n,
+    _check(lib().chn_softmax_ce_bwd2(_arg(logits), _arg(labels), int(ignore_label), _arg(lse), float(upstream),
+                                     _arg(gg), _arg(dlogits), _arg(dupstream), p, n,
                                      _stream() if stream is None else stream))
     return dlogits
 
@@ -497,22 +578,20 @@ def softmax_ce_bwd2(logits, labels, gg, dlogits, dupstream=None, lse=None, upstr
 def softmax_ce_fwd_bwd(logits, labels, loss_mean, dlogits, lse=None, upstream=1.0, ignore_label=-1, ws=None,
                        stream=None):
     p, n = _ws(ws)
-    _check(lib().chn_softmax_ce_fwd_bwd(_ref(desc(logits)), _ref(desc(labels)), int(ignore_label), _ref(desc(loss_mean)),
-                                        _ref(desc(lse)), float(upstream), _ref(desc(dlogits)), p, n,
+    _check(lib().chn_softmax_ce_fwd_bwd(_arg(logits), _arg(labels), int(ignore_label), _arg(loss_mean),
+                                        _arg(lse), float(upstream), _arg(dlogits), p, n,
                                         _stream() if stream is None else stream))
     return loss_mean
 
 
 def sgd_update(param, grad, lr, lowp_copy=None, stream=None):
-    _check(lib().chn_sgd_update(_ref(desc(param)), _ref(desc(grad)), float(lr), _ref(desc(lowp_copy)),
+    _check(lib().chn_sgd_update(_arg(param), _arg(grad), float(lr), _arg(lowp_copy),
                                 _stream() if stream is None else stream))
 
 
 def sgd_update_multi(params, grads, lr, lowp_copies=None, stream=None):
-    ps, gs = [desc(p) for p in params], [desc(g) for g in grads]
-    ls = None if lowp_copies is None else [desc(l) for l in lowp_copies]
-    _check(lib().chn_sgd_update_multi(len(ps), _ptrs(ps), _ptrs(gs), float(lr),
-                                      None if ls is None else _ptrs(ls),
+    _check(lib().chn_sgd_update_multi(len(params), _ptrs(params), _ptrs(grads), float(lr),
+                                      None if lowp_copies is None else _ptrs(lowp_copies),
                                       _stream() if stream is None else stream))
 
 
@@ -535,7 +614,7 @@ def lstm_step_fwd_seq(zx, Hs, Ut, bias, Cs, gates, n_steps, stream=None):
     (hn, _), (cn, _) = _row_block(Hs, Bn), _row_block(Cs, Bn)
     hn.data += hs
     cn.data += cs
-    ut, bd = _ref(desc(Ut)), _ref(desc(bias))
+    ut, bd = _arg(Ut), _arg(bias)
     for _ in range(n_steps):
         _check(L.chn_lstm_step_fwd(C.byref(zd), C.byref(hp), ut, bd, C.byref(cp), C.byref(cn), C.byref(hn), C.byref(gd), st))
         zd.data += zs; hp.data += hs; hn.data += hs; cp.data += cs; cn.data += cs; gd.data += gs
@@ -554,9 +633,9 @@ def lstm_step_bwd_seq(dZ, U, dHs, gates, Cs, dc_last, dc, n_steps, stream=None):
                                                              _row_block(gates, Bn), _row_block(Cs, Bn), _row_block(Cs, Bn))
     last = n_steps - 1
     zd.data += last * zs; zn.data += (last + 1) * zs; hd.data += last * hs; gd.data += last * gs; cp.data += last * cs; cn.data += (last + 1) * cs
-    ud = _ref(desc(U))
+    ud = _arg(U)
     dcd = [C.byref(desc(dc[0])), C.byref(desc(dc[1]))]
-    dc_next = _ref(desc(dc_last))
+    dc_next = _arg(dc_last)
     for t in range(last, -1, -1):
         _check(L.chn_lstm_step_bwd(None if t == last else C.byref(zn), ud, C.byref(hd), C.byref(gd), C.byref(cp), C.byref(cn),
                                    dc_next, C.byref(zd), dcd[t & 1], st))
@@ -565,21 +644,19 @@ def lstm_step_bwd_seq(dZ, U, dHs, gates, Cs, dc_last, dc, n_steps, stream=None):
 
 
 def adam_update_multi(params, grads, ms, vs, lr, step, beta1=0.9, beta2=0.999, eps=1e-8, lowp_copies=None, stream=None):
-    ps, gs, m_, v_ = ([desc(t) for t in ts] for ts in (params, grads, ms, vs))
-    ls = None if lowp_copies is None else [desc(l) for l in lowp_copies]
-    _check(lib().chn_adam_update_multi(len(ps), _ptrs(ps), _ptrs(gs), _ptrs(m_), _ptrs(v_), float(lr), float(beta1),
-                                       float(beta2), float(eps), int(step), None if ls is None else _ptrs(ls),
+    _check(lib().chn_adam_update_multi(len(params), _ptrs(params), _ptrs(grads), _ptrs(ms), _ptrs(vs), float(lr), float(beta1),
+                                       float(beta2), float(eps), int(step), None if lowp_copies is None else _ptrs(lowp_copies),
                                        _stream() if stream is None else stream))
 
 
 def embed_fwd(table, ids, out, stream=None):
-    _check(lib().chn_embed_fwd(_ref(desc(table)), _ref(desc(ids)), _ref(desc(out)),
+    _check(lib().chn_embed_fwd(_arg(table), _arg(ids), _arg(out),
                                _stream() if stream is None else stream))
     return out
 
 
 def embed_bwd(ids, dout, dtable, accumulate=False, stream=None):
-    _check(lib().chn_embed_bwd(_ref(desc(ids)), _ref(desc(dout)), _ref(desc(dtable)), int(accumulate),
+    _check(lib().chn_embed_bwd(_arg(ids), _arg(dout), _arg(dtable), int(accumulate),
                                _stream() if stream is None else stream))
     return dtable
 
@@ -587,38 +664,37 @@ def embed_bwd(ids, dout, dtable, accumulate=False, stream=None):
 def dropout(x, y, ratio, rng=None, site=0, residual=None, stream=None):
     """y = (residual +) dropout(x); rng: int64 tensor (seed, offset).  The gradient of x is the same call on the gradient of y."""
     dx, dr, dg, dy = _here(x, residual, rng, y)
-    _check(lib().chn_dropout(dx, dr, float(ratio), dg, int(site), dy, _stream() if stream is None else stream))
+    _check(_raw["chn_dropout"](dx, dr, C.c_double(ratio), dg, C.c_int64(int(site)), dy, _stream() if stream is None else _on(stream)))
     return y
 
 
 def rng_advance(rng, steps=1, stream=None):
     """rng[1] += steps on the stream: later draws (a replayed graph's too) use other masks."""
-    _check(lib().chn_rng_advance(_here(rng)[0], int(steps), _stream() if stream is None else stream))
+    _check(_raw["chn_rng_advance"](*_here(rng), C.c_int64(int(steps)), _stream() if stream is None else _on(stream)))
     return rng
 
 
 def layer_norm_fwd(x, y, gamma=None, beta=None, eps=1e-5, mean=None, rstd=None, stream=None):
     """mean: (N,), or (N,2) with what its rounding left, which keeps the digits of the gradients of rows with a large mean."""
     dx, dg, db, dy, dm, dr = _here(x, gamma, beta, y, mean, rstd)
-    _check(lib().chn_layer_norm_fwd(dx, dg, db, float(eps), dy, dm, dr, _stream() if stream is None else stream))
+    _check(_raw["chn_layer_norm_fwd"](dx, dg, db, C.c_double(eps), dy, dm, dr, _stream() if stream is None else _on(stream)))
     return y
 
 
 def layer_norm_bwd_workspace_bytes(x):
-    return lib().chn_layer_norm_bwd_workspace_bytes(_ref(desc(x)))
+    return lib().chn_layer_norm_bwd_workspace_bytes(_arg(x))
 
 
 def layer_norm_bwd(dy, x, mean, rstd, dx, gamma=None, dgamma=None, dbeta=None, ws=None, stream=None):
     p, n = _ws_here(ws)
-    _check(lib().chn_layer_norm_bwd(*_here(dy, x, mean, rstd, gamma, dx, dgamma, dbeta), p, n, _stream() if stream is None else stream))
+    _check(_raw["chn_layer_norm_bwd"](*_here(dy, x, mean, rstd, gamma, dx, dgamma, dbeta), p, n, _stream() if stream is None else _on(stream)))
     return dx
 
 
 def residual_norm_fwd(x, residual, s, y, gamma=None, beta=None, eps=1e-5, mean=None, rstd=None, ratio=0.0, rng=None, site=0, stream=None):
     """s = residual + dropout(x), y = layer_norm(s)."""
     dx, dres, ds, dy, dg, db, dm, dr, drng = _here(x, residual, s, y, gamma, beta, mean, rstd, rng)
-    _check(lib().chn_residual_norm_fwd(dx, dres, float(ratio), drng, int(site), dg, db, float(eps), ds, dy, dm, dr,
-                                       _stream() if stream is None else stream))
+    _check(_raw["chn_residual_norm_fwd"](dx, dres, C.c_double(ratio), drng, C.c_int64(int(site)), dg, db, C.c_double(eps), ds, dy, dm, dr, _stream() if stream is None else _on(stream)))
     return y
 
 
@@ -626,18 +702,18 @@ def residual_norm_bwd(dy, ds, s, mean, rstd, dresidual, dx, gamma=None, dgamma=N
     """dresidual and dx from the gradients dy of y and ds of s (or None)."""
     p, n = _ws_here(ws)
     a = _here(dy, ds, s, mean, rstd, gamma, rng, dresidual, dx, dgamma, dbeta)
-    _check(lib().chn_residual_norm_bwd(*a[:6], float(ratio), a[6], int(site), *a[7:], p, n, _stream() if stream is None else stream))
+    _check(_raw["chn_residual_norm_bwd"](*a[:6], C.c_double(ratio), a[6], C.c_int64(int(site)), *a[7:], p, n, _stream() if stream is None else _on(stream)))
     return dx
 
 
 def sample_workspace_bytes(logits):
-    return lib().chn_sample_workspace_bytes(_ref(desc(logits)))
+    return lib().chn_sample_workspace_bytes(_arg(logits))
 
 
 def sample(logits, u, out, temperature=None, top_k=None, top_p=None, min_p=None, ws=None, stream=None):
     """out[n]: a token of row n, drawn by u[n]; parameters are tensors of one value for each row (stride 0: one for all), None: not used."""
     p, n = _ws_here(ws)
-    _check(lib().chn_sample(*_here(logits, u, temperature, top_k, top_p, min_p, out), p, n, _stream() if stream is None else stream))
+    _check(_raw["chn_sample"](*_here(logits, u, temperature, top_k, top_p, min_p, out), p, n, _stream() if stream is None else _on(stream)))
     return out
 
 
