@@ -338,13 +338,16 @@ def _ws(t):
     return C.c_void_p(t.data_ptr()), t.numel() * t.element_size()
 
 
+_NO_BYTES = C.c_size_t(0)
+
+
 def _ws_here(t):
     """The same for `_raw` calls whose arrays have to lie on the current device."""
     if t is None:
-        return None, C.c_size_t(0)
+        return None, _NO_BYTES
     if t.get_device() != (_raw_device() if _raw_device is not None else torch.cuda.current_device()):
         raise ValueError("the workspace does not lie on the current device")
-    return C.c_void_p(t.data_ptr()), C.c_size_t(t.numel() * t.element_size())
+    return C.c_void_p(t.data_ptr()), C.c_size_t(t.nbytes)
 
 
 def _on(stream):
@@ -701,8 +704,9 @@ def residual_norm_fwd(x, residual, s, y, gamma=None, beta=None, eps=1e-5, mean=N
 def residual_norm_bwd(dy, ds, s, mean, rstd, dresidual, dx, gamma=None, dgamma=None, dbeta=None, ratio=0.0, rng=None, site=0, ws=None, stream=None):
     """dresidual and dx from the gradients dy of y and ds of s (or None)."""
     p, n = _ws_here(ws)
-    a = _here(dy, ds, s, mean, rstd, gamma, rng, dresidual, dx, dgamma, dbeta)
-    _check(_raw["chn_residual_norm_bwd"](*a[:6], C.c_double(ratio), a[6], C.c_int64(int(site)), *a[7:], p, n, _stream() if stream is None else _on(stream)))
+    ddy, dds, d_s, dm, dr, dg, drng, ddres, ddx, ddg, ddb = _here(dy, ds, s, mean, rstd, gamma, rng, dresidual, dx, dgamma, dbeta)
+    _check(_raw["chn_residual_norm_bwd"](ddy, dds, d_s, dm, dr, dg, C.c_double(ratio), drng, C.c_int64(int(site)), ddres, ddx, ddg, ddb, p, n,
+                                         _stream() if stream is None else _on(stream)))
     return dx
 
 
