@@ -23,6 +23,7 @@ constexpr int kThreads = 1024, kWaves = kThreads / 64;
 constexpr int kBins = 2048;          // two for each thread
 constexpr int kFewBins = 256;        // for a bound: coarser, and read by every wave
 constexpr int kSmall = 1024;         // tokens that are ordered by comparing each with each
+constexpr int kHeldUnits = 4;         // of a row that a thread keeps in registers
 constexpr int kMaxChunks = 32, kMaxParts = 4096, kLeastParts = 1024;
 
 // What the launches over chunks leave for each other, of one row.
@@ -768,7 +769,7 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(const T *logits, Sampl
   const int lane = threadIdx.x & 63;
   const Put put{a, n};
   // the largest logit, the threads' own, and the smallest of those; the units of rows of up to four a thread stay in registers
-  constexpr int E = Span<T>::E, U = 4;
+  constexpr int E = Span<T>::E, U = kHeldUnits;
   Unit<T, E> held[U];
   const bool holds = row.per <= 64 * U;
   float mine = -INFINITY, least = INFINITY;
@@ -1299,20 +1300,26 @@ __global__ __launch_bounds__(kThreads) void sample_draw_kernel(const T *logits, 
                          [&](float v, uint32_t i) -> u64 { return wt.of(limit.keeps(v, i) ? wt.near(v) : 0.0); }, put);
 }
 
-// Chunks that a row is cut in; 1: a block has it whole.  Measured in us, whole rows / chunks (fp32, rows of each with parameters of its own: top-k, top-p,
-// none, and top-k in half of the rows with top-p and min-p in all; several batches in turn):
-//   1 x 16384 11 21 10 20 / 14 25 15 26       1 x 32768 14 33 17 31 / 14 25 15 26     32 x 32768 15 34 17 32 / 15 29 17 29    64 x 32768 14 34 17 32 / 16 36 19 34
-//   1 x 65536 18 54 25 19 / 14 25 15 16       64 x 65536 22 58 29 53 / 20 51 26 44    96 x 65536 22 59 29 53 / 22 64 32 51    128 x 65536 25 61 32 55 / 25 76 37 60
-//   1 x 131072 27 98 45 28 / 14 26 16 17      128 x 131072 38 113 55 97 / 31 100 52 79    256 x 131072 54 139 73 115 / 49 151 84 107
-//   256 x 262144 88 245 125 204 / 79 241 139 178
-// So chunks win where blocks of whole rows leave compute units idle, or where rows that ask for more than others would keep the launch waiting.
-int chunks_of(int64_t N, int64_t V) {
-  if (V < 32768 || V < (V < 131072 ? 768 : 512) * N || V > (int64_t)kMaxParts * 64 * 4) return 1;   // (a unit has four elements at the least)
+// Chunks that a row is cut in; 1: a block has it whole.  `unit`: tokens of a unit.  Measured in us, whole rows / chunks (rows of each with parameters of its own: top-k, top-p,
+// none, min-p, and top-k in half of the rows with top-p and min-p in all; several batches in turn):
+//   fp32   1 x 32768   13 34 16 13 15 / 14 26 15 15 16     32 x 32768  15 34 17 16 33 / 15 30 17 17 29      64 x 50257   20 50 25 23 46 / 18 51 27 25 41
+//          1 x 65536   18 55 25 18 19 / 14 26 15 15 17     64 x 65536  22 58 28 25 53 / 19 52 26 26 42      1 x 131072   27 100 44 29 29 / 14 30 15 15 17
+//          128 x 131072  38 115 56 47 101 / 31 105 52 49 80     256 x 131072  52 140 74 68 121 / 51 153 88 79 121      256 x 262144  86 252 126 109 218 / 82 245 140 125 178
+//   bf16   1 x 32768   12 31 14 10 13 / 14 29 18 16 17     1 x 36000   14 39 19 14 15 / 14 29 17 16 17      32 x 44000   17 45 22 19 42 / 16 40 22 20 38
+//          64 x 50257  20 55 26 24 50 / 18 52 27 25 41     64 x 65536  19 56 26 23 51 / 18 60 30 27 45      128 x 131072  32 103 47 38 92 / 25 100 47 43 74
+//          256 x 131072  35 112 53 46 100 / 32 133 66 56 103     256 x 262144  63 224 104 87 193 / 53 220 112 88 151
+// So chunks win where blocks of whole rows leave compute units idle and a block cannot hold the row in its registers, and in large batches with top-k, or whose rows
+// ask for different things and keep the launch waiting; with top-p alone, min-p alone or no filter they lose up to a quarter there, which this rule, that knows
+// the sizes only, takes into the bargain.
+int chunks_of(int64_t N, int64_t V, int unit) {
+  if (V < 32768 || V / unit <= kHeldUnits * kThreads || V < (V < 131072 ? 768 : 512) * N || V > (int64_t)kMaxParts * 64 * 4) return 1;   // (a unit has four elements at the least)
   int64_t n = V / 4096;                                  // a unit or two for each thread
   const int64_t most = (2048 + N - 1) / N;               // and about eight blocks for each compute unit
   if (n > most) n = most;
   return n > kMaxChunks ? kMaxChunks : (int)n;
 }
+
+int unit_of(const chn_array *logits) { return logits->dtype == CHN_F32 ? Span<float>::E : Span<bf16_raw>::E; }
 
 chn_status check_row_parameter(const chn_array *v, const char *name, int64_t n, int64_t *stride) {
   CHN_TRY(validate(v, name, false));
@@ -1375,7 +1382,7 @@ extern "C" {
 
 size_t chn_sample_workspace_bytes(const chn_array *logits) {
   if (!logits || logits->ndim != 2 || logits->shape[0] <= 0 || logits->shape[1] <= 0) return 0;
-  return chn::chunks_of(logits->shape[0], logits->shape[1]) > 1 ? (size_t)logits->shape[0] * sizeof(chn::RowSpace) : 0;
+  return chn::chunks_of(logits->shape[0], logits->shape[1], chn::unit_of(logits)) > 1 ? (size_t)logits->shape[0] * sizeof(chn::RowSpace) : 0;
 }
 
 chn_status chn_sample(const chn_array *logits, const chn_array *u, const chn_array *temperature, const chn_array *top_k, const chn_array *top_p,
@@ -1412,7 +1419,7 @@ chn_status chn_sample(const chn_array *logits, const chn_array *u, const chn_arr
   a.out64 = out->dtype == CHN_I64;
   hipStream_t st = as_stream(stream);
   const size_t need = chn_sample_workspace_bytes(logits);
-  a.chunks = need > 0 && ws && ws_bytes >= need && reinterpret_cast<uintptr_t>(ws) % 256 == 0 ? chunks_of(a.N, V) : 1;
+  a.chunks = need > 0 && ws && ws_bytes >= need && reinterpret_cast<uintptr_t>(ws) % 256 == 0 ? chunks_of(a.N, V, unit_of(logits)) : 1;
   a.space = static_cast<RowSpace *>(ws);
   if (logits->dtype == CHN_F32) launch<float>(logits, a, st);
   else launch<bf16_raw>(logits, a, st);

@@ -20,7 +20,7 @@ def draw(z, u, ws=True, **params):
     return out.cpu().numpy()
 
 
-@pytest.mark.parametrize("v", [32768, 32770, 50257, 70001, 131072, 262144])
+@pytest.mark.parametrize("v", [32776, 32783, 50257, 70001, 131072, 262144])
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 def test_rows_in_chunks_have_as_many_bounds_as_a_block_has_threads(v, dtype):
     """The k-th largest of the extremes that the first launch leaves of a row's parts is what spares a top-k the passes over its row: there are 1024 of
@@ -38,7 +38,7 @@ def test_rows_in_chunks_have_as_many_bounds_as_a_block_has_threads(v, dtype):
         assert np.isin(part, row).sum() >= 2 * 1024
 
 
-@pytest.mark.parametrize("v", [32768, 32771, 50257, 65541])
+@pytest.mark.parametrize("v", [32768, 32771, 32776, 50257, 65541])
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 def test_top_k_of_rows_in_chunks(v, dtype):
     """Any k, also where most of a row's parts hold nothing and where the best tokens are neighbours."""
@@ -85,3 +85,10 @@ def test_rows_of_more_parts_than_are_looked_at_together(v):
         want = R.sample(host, u.numpy(), **params)
         for ws in (True, False):
             assert np.array_equal(draw(dev, u.cuda(), ws, **{q: torch.from_numpy(a).cuda() for q, a in params.items()}), want), (sorted(params), ws)
+
+
+def test_a_row_that_a_block_holds_in_its_registers_is_not_cut():
+    """bfloat16 rows of 32768 tokens are four pieces of 16 bytes a thread, with up to seven tokens behind them; fp32 rows of as many are eight."""
+    for v, cut in ((32768, False), (32775, False), (32776, True)):
+        assert (B.sample_workspace_bytes(torch.empty(1, v, dtype=torch.bfloat16)) > 0) == cut
+        assert B.sample_workspace_bytes(torch.empty(1, v)) > 0
