@@ -7,7 +7,10 @@
 // 5.8 TB/s; without a mask 21).  The mask is what comes closest to costing time: with two instructions for a three-way exclusive or the gradient
 // took 26.
 //
-// The leading dimensions of the arrays are merged where all of them allow it; what is left are rows with a list of strides.
+// The leading dimensions of the arrays are merged where all of them allow it; what is left are rows with a list of strides.  Rows of unit stride with one pitch go
+// in 16-byte pieces; the others element by element, four columns a thread behind a division for each dimension that is left.  4096 x 4096, us (a plain copy):
+// fp32 / bf16 22 (24) / 13.5 (13); rows of a 3-d slice 30 (19) / 26 (12); a repeated row 15 (12) / 13 (8); every second column 43 (42) / 26 (43); transposed 83 (26) / 71 (13), where
+// neighbouring threads read lines apart.  No model here drops out anything but rows of unit stride.
 #include "philox.h"
 #include "rows.h"
 

@@ -1496,7 +1496,11 @@ class Masks:
     each place that draws.  A mask is a function of these, so none is kept: the backward pass draws it again.
 
     ``advance()`` begins another step: the offset moves on the stream (in a captured step: at every replay) and places are numbered from
-    0 again.  Not between a forward and its backward pass: the backward pass would draw other masks, and says so instead."""
+    0 again.  Not between a forward and its backward pass: the backward pass would draw other masks, and says so instead.
+
+    What Python does not see it cannot say.  A captured step that advances has Masks of its own, or is not replayed between the forward and the backward pass of
+    another step that draws from the same ones: the replay moves the offset, and that backward pass would draw the new masks.  And Masks belong to one
+    stream: a step on another one waits for it, or has its own, since `advance()` writes what the other's kernels read."""
 
     def __init__(self, seed, offset=0):
         import numpy as np
