@@ -241,21 +241,35 @@ def _arg(t):
     return C.byref(t) if type(t) is ChnArray else _kept(t).ref
 
 
-def _here(*arrays):
-    """References for `_raw` calls to the descriptors of arrays, which have to lie on the current device, whose stream the call goes to (of a descriptor that is not known).
-    (A call with twelve arrays spends more time on these than on its launch.)"""
+_HANDLES = {}                      # streams' handles as calls take them
+
+
+def _here(stream, *arrays):
+    """For `_raw` calls: references to the descriptors of arrays, which have to lie on the current device (of a descriptor that is not known), and behind them the handle of
+    the stream, None: torch's current one.  (A call with twelve arrays spends more time on these than on its launch.)"""
     current = _raw_device() if _raw_device is not None else torch.cuda.current_device()
     try:
-        return [None if t is None else k.ref if (k := t._chn_kept).ptr == t.data_ptr() and k.version == t._version and k.device == current else _look(t, current)
-                for t in arrays]
+        out = [None if t is None else k.ref if (k := t._chn_kept).ptr == t.data_ptr() and k.version == t._version and k.device == current else _look(t, current)
+               for t in arrays]
     except (AttributeError, RuntimeError):
-        return [None if t is None else _look(t, current) for t in arrays]
+        out = [None if t is None else _look(t, current) for t in arrays]
+    if stream is None:
+        raw = _raw_stream(current) if _raw_stream is not None else torch.cuda.current_stream().cuda_stream
+        stream = _HANDLES.get(raw)
+        if stream is None:
+            if len(_HANDLES) >= 256:
+                _HANDLES.clear()
+            stream = _HANDLES[raw] = C.c_void_p(raw)
+    elif not isinstance(stream, C.c_void_p):
+        stream = C.c_void_p(stream)
+    out.append(stream)
+    return out
 
 
 def _look(t, current):
     if type(t) is ChnArray:
         return C.byref(t)
-    k = _again(t)
+    k = _kept(t)
     if k.device is None:
         k.device = t.get_device()
     if k.device != current:
@@ -348,11 +362,6 @@ def _ws_here(t):
     if t.get_device() != (_raw_device() if _raw_device is not None else torch.cuda.current_device()):
         raise ValueError("the workspace does not lie on the current device")
     return C.c_void_p(t.data_ptr()), C.c_size_t(t.nbytes)
-
-
-def _on(stream):
-    """A stream's handle for a `_raw` call."""
-    return stream if isinstance(stream, C.c_void_p) else C.c_void_p(stream)
 
 
 def version():
@@ -666,21 +675,26 @@ def embed_bwd(ids, dout, dtable, accumulate=False, stream=None):
 
 def dropout(x, y, ratio, rng=None, site=0, residual=None, stream=None):
     """y = (residual +) dropout(x); rng: int64 tensor (seed, offset).  The gradient of x is the same call on the gradient of y."""
-    dx, dr, dg, dy = _here(x, residual, rng, y)
-    _check(_raw["chn_dropout"](dx, dr, C.c_double(ratio), dg, C.c_int64(int(site)), dy, _stream() if stream is None else _on(stream)))
+    dx, dr, dg, dy, st = _here(stream, x, residual, rng, y)
+    status = _raw["chn_dropout"](dx, dr, C.c_double(ratio), dg, C.c_int64(int(site)), dy, st)
+    if status:
+        _check(status)
     return y
 
 
 def rng_advance(rng, steps=1, stream=None):
     """rng[1] += steps on the stream: later draws (a replayed graph's too) use other masks."""
-    _check(_raw["chn_rng_advance"](*_here(rng), C.c_int64(int(steps)), _stream() if stream is None else _on(stream)))
+    dg, st = _here(stream, rng)
+    _check(_raw["chn_rng_advance"](dg, C.c_int64(int(steps)), st))
     return rng
 
 
 def layer_norm_fwd(x, y, gamma=None, beta=None, eps=1e-5, mean=None, rstd=None, stream=None):
     """mean: (N,), or (N,2) with what its rounding left, which keeps the digits of the gradients of rows with a large mean."""
-    dx, dg, db, dy, dm, dr = _here(x, gamma, beta, y, mean, rstd)
-    _check(_raw["chn_layer_norm_fwd"](dx, dg, db, C.c_double(eps), dy, dm, dr, _stream() if stream is None else _on(stream)))
+    dx, dg, db, dy, dm, dr, st = _here(stream, x, gamma, beta, y, mean, rstd)
+    status = _raw["chn_layer_norm_fwd"](dx, dg, db, C.c_double(eps), dy, dm, dr, st)
+    if status:
+        _check(status)
     return y
 
 
@@ -690,23 +704,29 @@ def layer_norm_bwd_workspace_bytes(x):
 
 def layer_norm_bwd(dy, x, mean, rstd, dx, gamma=None, dgamma=None, dbeta=None, ws=None, stream=None):
     p, n = _ws_here(ws)
-    _check(_raw["chn_layer_norm_bwd"](*_here(dy, x, mean, rstd, gamma, dx, dgamma, dbeta), p, n, _stream() if stream is None else _on(stream)))
+    ddy, d_x, dm, dr, dg, ddx, ddg, ddb, st = _here(stream, dy, x, mean, rstd, gamma, dx, dgamma, dbeta)
+    status = _raw["chn_layer_norm_bwd"](ddy, d_x, dm, dr, dg, ddx, ddg, ddb, p, n, st)
+    if status:
+        _check(status)
     return dx
 
 
 def residual_norm_fwd(x, residual, s, y, gamma=None, beta=None, eps=1e-5, mean=None, rstd=None, ratio=0.0, rng=None, site=0, stream=None):
     """s = residual + dropout(x), y = layer_norm(s)."""
-    dx, dres, ds, dy, dg, db, dm, dr, drng = _here(x, residual, s, y, gamma, beta, mean, rstd, rng)
-    _check(_raw["chn_residual_norm_fwd"](dx, dres, C.c_double(ratio), drng, C.c_int64(int(site)), dg, db, C.c_double(eps), ds, dy, dm, dr, _stream() if stream is None else _on(stream)))
+    dx, dres, ds, dy, dg, db, dm, dr, drng, st = _here(stream, x, residual, s, y, gamma, beta, mean, rstd, rng)
+    status = _raw["chn_residual_norm_fwd"](dx, dres, C.c_double(ratio), drng, C.c_int64(int(site)), dg, db, C.c_double(eps), ds, dy, dm, dr, st)
+    if status:
+        _check(status)
     return y
 
 
 def residual_norm_bwd(dy, ds, s, mean, rstd, dresidual, dx, gamma=None, dgamma=None, dbeta=None, ratio=0.0, rng=None, site=0, ws=None, stream=None):
     """dresidual and dx from the gradients dy of y and ds of s (or None)."""
     p, n = _ws_here(ws)
-    ddy, dds, d_s, dm, dr, dg, drng, ddres, ddx, ddg, ddb = _here(dy, ds, s, mean, rstd, gamma, rng, dresidual, dx, dgamma, dbeta)
-    _check(_raw["chn_residual_norm_bwd"](ddy, dds, d_s, dm, dr, dg, C.c_double(ratio), drng, C.c_int64(int(site)), ddres, ddx, ddg, ddb, p, n,
-                                         _stream() if stream is None else _on(stream)))
+    ddy, dds, d_s, dm, dr, dg, drng, ddres, ddx, ddg, ddb, st = _here(stream, dy, ds, s, mean, rstd, gamma, rng, dresidual, dx, dgamma, dbeta)
+    status = _raw["chn_residual_norm_bwd"](ddy, dds, d_s, dm, dr, dg, C.c_double(ratio), drng, C.c_int64(int(site)), ddres, ddx, ddg, ddb, p, n, st)
+    if status:
+        _check(status)
     return dx
 
 
@@ -717,7 +737,10 @@ def sample_workspace_bytes(logits):
 def sample(logits, u, out, temperature=None, top_k=None, top_p=None, min_p=None, ws=None, stream=None):
     """out[n]: a token of row n, drawn by u[n]; parameters are tensors of one value for each row (stride 0: one for all), None: not used."""
     p, n = _ws_here(ws)
-    _check(_raw["chn_sample"](*_here(logits, u, temperature, top_k, top_p, min_p, out), p, n, _stream() if stream is None else _on(stream)))
+    dz, du, dt, dk, dp, dm, do, st = _here(stream, logits, u, temperature, top_k, top_p, min_p, out)
+    status = _raw["chn_sample"](dz, du, dt, dk, dp, dm, do, p, n, st)
+    if status:
+        _check(status)
     return out
 
 

@@ -13,7 +13,7 @@ def described(t):
     """What a call would be told of a tensor: by both ways that a call takes."""
     a = B.desc(t)
     out = (a.data, tuple(a.shape[:a.ndim]), tuple(a.strides[:a.ndim]), a.dtype)
-    for ref in (B._arg(t), B._here(t)[0]):
+    for ref in (B._arg(t), B._here(0, t)[0]):
         b = ref._obj
         assert out == (b.data, tuple(b.shape[:b.ndim]), tuple(b.strides[:b.ndim]), b.dtype)
     return out
@@ -104,4 +104,4 @@ def test_arrays_elsewhere_are_refused():
     B._raw_device = lambda: 0                            # (undone by the fixture)
     for _ in range(2):
         with pytest.raises(ValueError):
-            B._here(t)
+            B._here(0, t)
