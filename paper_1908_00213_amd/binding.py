@@ -208,8 +208,11 @@ def _again(t):
     k = getattr(t, "_chn_kept", None)
     if type(k) is not _Kept or k.ptr != t.data_ptr() or k.shape != t.shape or k.strides != t.stride():
         return _describe(t)
+    version = None if t.is_inference() else t._version
+    if version == k.version:
+        return k
     same = _Kept()                                       # (the old one may be kept on a shallow copy too)
-    same.ref, same.ptr, same.version, same.device, same.desc = k.ref, k.ptr, None if t.is_inference() else t._version, k.device, k.desc
+    same.ref, same.ptr, same.version, same.device, same.desc = k.ref, k.ptr, version, k.device, k.desc
     same.pointer, same.shape, same.strides = k.pointer, k.shape, k.strides
     t._chn_kept = same
     return same

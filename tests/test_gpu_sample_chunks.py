@@ -92,3 +92,15 @@ def test_a_row_that_a_block_holds_in_its_registers_is_not_cut():
     for v, cut in ((32768, False), (32775, False), (32776, True)):
         assert (B.sample_workspace_bytes(torch.empty(1, v, dtype=torch.bfloat16)) > 0) == cut
         assert B.sample_workspace_bytes(torch.empty(1, v)) > 0
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_the_longest_row(dtype):
+    """2^30 equal logits: the token is u times their number, and one that stands out."""
+    v = 2 ** 30
+    z = torch.zeros(1, v, device="cuda", dtype=dtype)
+    for u in (0.3, 1.0 - 2.0 ** -24):
+        assert draw(z, vec([u]))[0] == int(float(np.float32(u)) * v), u
+    z[0, v - 3] = z[0, v - 1] = 40.0                     # two that outweigh all others together
+    assert draw(z, vec([0.5]), temperature=vec([0.0]))[0] == v - 3
+    assert draw(z, vec([0.6]))[0] == v - 1 and draw(z, vec([0.9]), top_k=vec([1], np.int32))[0] == v - 3
