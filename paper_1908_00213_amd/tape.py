@@ -1504,7 +1504,7 @@ class Masks:
 
     def __init__(self, seed, offset=0):
         import numpy as np
-        self.rng = backend().from_numpy(np.array([(seed + 2 ** 63) % 2 ** 64 - 2 ** 63, offset], dtype=np.int64))
+        self.rng = backend().from_numpy(np.array([(int(seed) + 2 ** 63) % 2 ** 64 - 2 ** 63, int(offset)], dtype=np.int64))
         self.steps = self.sites = 0
 
     def advance(self):
