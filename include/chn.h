@@ -500,6 +500,63 @@ chn_status chn_sample(const chn_array *logits, const chn_array *u, const chn_arr
                       const chn_array *top_p, const chn_array *min_p, const chn_array *out, void *ws, size_t ws_bytes,
                       chn_stream stream);
 
+/* ---- logits before a token is drawn ----------------------------------------------------------------------------
+ * out = the logits (N,V), F32 or BF16, row-major with any pitch, with what a row's text, its caller and its grammar say about them (chn_sample
+ * draws from the result).  In a row, z the logit of token i:
+ *   tokens (N,L) I32 or I64, any pitch: the row's text so far, of which the first lengths[n] count (lengths, prompt: (N,) I32 or I64; NULL: all L,
+ *   and no prompt), the first prompt[n] of them being the prompt.  With c the number of times i stands behind the prompt:
+ *     repetition (N,) F32: z / repetition where z > 0, else z * repetition, if i is anywhere in the text;
+ *     frequency (N,) F32:  then z - frequency * c;      presence (N,) F32: then z - presence, if c > 0;
+ *   bias_ids (N,M) I32 or I64 and bias (N,M) F32: then z + the biases whose id is i, added up in the order of the list;
+ *   allowed (N, ceil(V/32)) I32: then -inf unless bit i % 32 of word i / 32 is set.  A mask may leave nothing.
+ * Every parameter NULL where it is not used (penalties without tokens are CHN_ERR_NULL, biases without ids too); stride 0: one row for all.  lengths and prompt are cut to 0 .. L,
+ * ids outside [0, V) are passed over.  out: (N,V) F32 or BF16, which may be the array of logits.  fp32 arithmetic in a fixed order, rounded once at the
+ * end; L below 2^30, V below 2^31 (CHN_ERR_SHAPE).  No workspace. */
+chn_status chn_logits_adjust(const chn_array *logits, const chn_array *tokens, const chn_array *lengths, const chn_array *prompt,
+                             const chn_array *repetition, const chn_array *frequency, const chn_array *presence, const chn_array *bias_ids,
+                             const chn_array *bias, const chn_array *allowed, const chn_array *out, chn_stream stream);
+
+/* ---- gated linear recurrence -----------------------------------------------------------------------------------
+ * A recurrence without a product from step to step, over gate and x (T,B,D), both F32 or both BF16, from a first state h0 (B,D) F32 (NULL: zeros):
+ *   CHN_SCAN_SIGMOID  a = 1 / (1 + exp(-gate_t))     h_t = a h_{t-1} + (1 - a) x_t
+ *   CHN_SCAN_DECAY                                   h_t = gate_t h_{t-1} + x_t
+ *   y_t = h_t, (T,B,D) F32 or BF16      h_last = h_T, (B,D) F32 or NULL
+ * lengths (B,) I32 or I64, cut to 0 .. T, or NULL: sequence b ends after lengths[b] steps.  Behind its end whatever gate and x hold is not looked at, y is 0 and the state stays.
+ * The three-dimensional arrays have unit inner stride and any others (time or batch outermost, halves of one product's result); h0 and h_last are row-major with any pitch.
+ * states: (chn_gated_scan_states(T), B, D) F32, contiguous, or NULL: what the backward pass needs, the state before every CHN_SCAN_STRIDE-th step.
+ * Backward, with G_t the gradient of h_t: G_T = dh_last (B,D) F32 (NULL: zeros), G_t = dy_t + a_{t+1} G_{t+1} (dh_last enters where the sequence ends):
+ *   CHN_SCAN_SIGMOID  dx_t = (1 - a) G_t     dgate_t = (h_{t-1} - x_t) a (1 - a) G_t
+ *   CHN_SCAN_DECAY    dx_t = G_t             dgate_t = h_{t-1} G_t
+ *   dh0 = a_1 G_1, (B,D) F32 or NULL
+ * dy: F32 or BF16; dgate, dx: the type of gate; behind a sequence's end they are 0.
+ * States and gradients are fp32, results the same bits from run to run.  Sequences of more than 128 steps are cut in pieces of as many, whose effect is
+ * (the product of the decays, the state from zero): where that product leaves fp32's range (decays above 1), so does the result.
+ * An output may be the very array of an input (h_last of h0, y of x, dgate of gate, dx of x or dy).
+ * T = 0 copies the state.  T, B, D below 2^31, B * D below 2^40 (CHN_ERR_SHAPE).
+ * ws: chn_gated_scan_workspace_bytes(gate) bytes, 256-byte aligned, the library's until the work on `stream` is done; the backward pass may use the same. */
+enum { CHN_SCAN_SIGMOID = 0, CHN_SCAN_DECAY = 1 };
+#define CHN_SCAN_STRIDE 16
+int64_t chn_gated_scan_states(int64_t steps);
+size_t chn_gated_scan_workspace_bytes(const chn_array *gate);
+chn_status chn_gated_scan_fwd(int kind, const chn_array *gate, const chn_array *x, const chn_array *h0, const chn_array *lengths, const chn_array *y,
+                              const chn_array *h_last, const chn_array *states, void *ws, size_t ws_bytes, chn_stream stream);
+chn_status chn_gated_scan_bwd(int kind, const chn_array *gate, const chn_array *x, const chn_array *states, const chn_array *lengths, const chn_array *dy,
+                              const chn_array *dh_last, const chn_array *dgate, const chn_array *dx, const chn_array *dh0, void *ws, size_t ws_bytes,
+                              chn_stream stream);
+
+/* ---- embeddings with a scale, their gradient by tokens ------------------------------------------------------------
+ * out[n] = scale * table[ids[n]]; table (V,D) and out (N,D) F32 or BF16, each of its own, row-major with any pitch; ids (N,) I32 or I64, any stride.
+ * One product in fp32 and one rounding.
+ * Backward: dtable[v] = (dtable[v] +) scale * (the sum of the rows n of dout with ids[n] = v); dout (N,D) F32 or BF16, dtable (V,D) F32.  Unlike
+ * chn_embed_bwd, which looks through all ids for every few rows of the table, it sorts the ids first: work grows with N + V, not with their product.
+ * Sums are fp32 in a fixed order (the same bits from run to run): the rows of a token one after the other, of a token that stands often in pieces of 64 in
+ * the order of n, then the pieces.  N and V below 2^31 (CHN_ERR_SHAPE).
+ * ws: chn_embed_sorted_workspace_bytes(ids, dtable) bytes, 256-byte aligned, the library's until the work on `stream` is done. */
+chn_status chn_embed_scaled_fwd(const chn_array *table, const chn_array *ids, double scale, const chn_array *out, chn_stream stream);
+size_t chn_embed_sorted_workspace_bytes(const chn_array *ids, const chn_array *dtable);
+chn_status chn_embed_sorted_bwd(const chn_array *ids, const chn_array *dout, double scale, const chn_array *dtable, int accumulate, void *ws,
+                                size_t ws_bytes, chn_stream stream);
+
 /* ---- user-defined kernels ----------------------------------------------------------------------------
  * Section "Custom CUDA Kernels" and the figure "Example of a user-defined kernel": a kernel is
  * declared by a list of input parameters, a list of output parameters ("<type> <name>", comma

@@ -25,6 +25,8 @@ OP = {n: i for i, n in enumerate(OPS)}
 REDUCE = {"sum": 0, "max": 1}
 EPILOGUES = ["none", "bias", "bias_relu", "bias_gelu", "relu_bwd", "gelu_bwd", "bf16_copy"]
 EPI = {n: i for i, n in enumerate(EPILOGUES)}
+SCAN_KINDS = ["sigmoid", "decay"]
+SCAN = {n: i for i, n in enumerate(SCAN_KINDS)}
 
 EXPORTS = ["chn_elementwise_broadcast", "chn_reduce_axis_workspace_bytes", "chn_reduce_axis", "chn_reduce_axis_static", "chn_argmax_axis",
            "chn_gemm_workspace_bytes", "chn_gemm", "chn_linear_bwd_workspace_bytes", "chn_linear_bwd", "chn_linear_bwd_plan", "chn_lstm_fwd", "chn_lstm_bwd", "chn_lstm_step_fwd", "chn_lstm_step_bwd",
@@ -33,7 +35,9 @@ EXPORTS = ["chn_elementwise_broadcast", "chn_reduce_axis_workspace_bytes", "chn_
            "chn_softmax_ce_workspace_bytes", "chn_softmax_ce_fwd", "chn_softmax_ce_bwd", "chn_softmax_ce_bwd2", "chn_softmax_ce_fwd_bwd",
            "chn_sgd_update", "chn_sgd_update_multi", "chn_adam_update_multi", "chn_embed_fwd", "chn_embed_bwd",
            "chn_dropout", "chn_rng_advance", "chn_layer_norm_fwd", "chn_layer_norm_bwd_workspace_bytes", "chn_layer_norm_bwd",
-           "chn_residual_norm_fwd", "chn_residual_norm_bwd", "chn_sample_workspace_bytes", "chn_sample",
+           "chn_residual_norm_fwd", "chn_residual_norm_bwd", "chn_sample_workspace_bytes", "chn_sample", "chn_logits_adjust",
+           "chn_gated_scan_states", "chn_gated_scan_workspace_bytes", "chn_gated_scan_fwd", "chn_gated_scan_bwd",
+           "chn_embed_scaled_fwd", "chn_embed_sorted_workspace_bytes", "chn_embed_sorted_bwd",
            "chn_status_string", "chn_last_error", "chn_version", "chn_elementwise_plan", "chn_gemm_plan", "chn_gemm_plan_kernel", "chn_gemm_plan_override",
            "chn_user_kernel_config", "chn_user_kernel_stats", "chn_user_kernel_destroy",
            "chn_elementwise_kernel_create", "chn_elementwise_kernel_prepare", "chn_elementwise_kernel_launch",
@@ -137,6 +141,17 @@ def lib():
     L.chn_sample_workspace_bytes.argtypes = [AP]
     L.chn_sample_workspace_bytes.restype = C.c_size_t
     L.chn_sample.argtypes = [AP] * 7 + [vp, C.c_size_t, st]
+    L.chn_logits_adjust.argtypes = [AP] * 11 + [st]
+    L.chn_gated_scan_states.argtypes = [C.c_int64]
+    L.chn_gated_scan_states.restype = C.c_int64
+    L.chn_gated_scan_workspace_bytes.argtypes = [AP]
+    L.chn_gated_scan_workspace_bytes.restype = C.c_size_t
+    L.chn_gated_scan_fwd.argtypes = [C.c_int] + [AP] * 7 + [vp, C.c_size_t, st]
+    L.chn_gated_scan_bwd.argtypes = [C.c_int] + [AP] * 9 + [vp, C.c_size_t, st]
+    L.chn_embed_scaled_fwd.argtypes = [AP, AP, C.c_double, AP, st]
+    L.chn_embed_sorted_workspace_bytes.argtypes = [AP, AP]
+    L.chn_embed_sorted_workspace_bytes.restype = C.c_size_t
+    L.chn_embed_sorted_bwd.argtypes = [AP, AP, C.c_double, AP, C.c_int, vp, C.c_size_t, st]
     L.chn_status_string.argtypes = [C.c_int32]
     L.chn_status_string.restype = C.c_char_p
     L.chn_last_error.argtypes = []
@@ -745,6 +760,72 @@ def sample(logits, u, out, temperature=None, top_k=None, top_p=None, min_p=None,
     if status:
         _check(status)
     return out
+
+
+def logits_adjust(logits, out, tokens=None, lengths=None, prompt=None, repetition=None, frequency=None, presence=None, bias_ids=None, bias=None,
+                  allowed=None, stream=None):
+    """out = logits with penalties for a row's tokens, biases and a mask of allowed tokens (out may be logits); None: not used."""
+    dz, dt, dl, dp, dr, df, ds, di, db, da, do, st = _here(stream, logits, tokens, lengths, prompt, repetition, frequency, presence, bias_ids, bias, allowed, out)
+    status = _raw["chn_logits_adjust"](dz, dt, dl, dp, dr, df, ds, di, db, da, do, st)
+    if status:
+        _check(status)
+    return out
+
+
+def gated_scan_states_shape(steps, batch, cols):
+    """Of the fp32 states that a forward pass keeps for its backward pass."""
+    return lib().chn_gated_scan_states(int(steps)), int(batch), int(cols)
+
+
+def gated_scan_workspace_bytes(gate):
+    return lib().chn_gated_scan_workspace_bytes(_arg(gate))
+
+
+def _scan_kind(kind):
+    return C.c_int(SCAN[kind] if isinstance(kind, str) else kind)
+
+
+def gated_scan_fwd(gate, x, y, h0=None, h_last=None, states=None, lengths=None, kind="sigmoid", ws=None, stream=None):
+    """y[t] = h_t = a h_{t-1} + (1 - a) x[t], a = sigmoid(gate[t]) ("sigmoid"), or gate[t] h_{t-1} + x[t] ("decay"); (T, B, D).  states: for the backward pass."""
+    p, n = _ws_here(ws)
+    dg, dx, d0, dl, dy, dh, ds, st = _here(stream, gate, x, h0, lengths, y, h_last, states)
+    status = _raw["chn_gated_scan_fwd"](_scan_kind(kind), dg, dx, d0, dl, dy, dh, ds, p, n, st)
+    if status:
+        _check(status)
+    return y
+
+
+def gated_scan_bwd(gate, x, states, dy, dgate, dx, dh_last=None, dh0=None, lengths=None, kind="sigmoid", ws=None, stream=None):
+    """Gradients of gate, x and h0 from those of y and h_last, with the states that the forward pass kept."""
+    p, n = _ws_here(ws)
+    dg, d_x, ds, dl, ddy, ddh, ddg, ddx, dd0, st = _here(stream, gate, x, states, lengths, dy, dh_last, dgate, dx, dh0)
+    status = _raw["chn_gated_scan_bwd"](_scan_kind(kind), dg, d_x, ds, dl, ddy, ddh, ddg, ddx, dd0, p, n, st)
+    if status:
+        _check(status)
+    return dx
+
+
+def embed_scaled_fwd(table, ids, out, scale=1.0, stream=None):
+    """out[n] = scale * table[ids[n]]"""
+    dt, di, do, st = _here(stream, table, ids, out)
+    status = _raw["chn_embed_scaled_fwd"](dt, di, C.c_double(scale), do, st)
+    if status:
+        _check(status)
+    return out
+
+
+def embed_sorted_workspace_bytes(ids, dtable):
+    return lib().chn_embed_sorted_workspace_bytes(_arg(ids), _arg(dtable))
+
+
+def embed_sorted_bwd(ids, dout, dtable, scale=1.0, accumulate=False, ws=None, stream=None):
+    """dtable[v] = (dtable[v] +) scale * sum of the rows of dout whose id is v, by sorting the ids."""
+    p, n = _ws_here(ws)
+    di, do, dt, st = _here(stream, ids, dout, dtable)
+    status = _raw["chn_embed_sorted_bwd"](di, do, C.c_double(scale), dt, C.c_int(int(accumulate)), p, n, st)
+    if status:
+        _check(status)
+    return dtable
 
 
 # ---- user-defined kernels ---------------------------------------------------------------------------------

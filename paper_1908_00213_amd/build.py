@@ -16,7 +16,7 @@ OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libchn.so")
 
 SOURCES = ["host.cpp", "user_kernel.cpp", "elementwise.hip", "reduce.hip", "argmax.hip", "gemm.hip", "linear_bwd.hip", "lstm.hip", "lstm_step.hip", "lstm_seq.hip", "lstm_xcd.hip", "softmax_ce.hip",
-           "sgd.hip", "adam.hip", "embed.hip", "norm.hip", "dropout.hip", "sample.hip"]
+           "sgd.hip", "adam.hip", "embed.hip", "embed_sorted.hip", "norm.hip", "dropout.hip", "sample.hip", "adjust.hip", "scan.hip"]
 
 # gemm_inst.hip is compiled once per (dtype, A layout, B layout): k = unit stride along K, m = along M/N
 GEMM_FAMILIES = [("%s_%s%s" % (tn, "k" if a else "m", "k" if b else "m"), t, a, b)

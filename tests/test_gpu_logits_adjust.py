@@ -1,0 +1,204 @@
+"""Adjusted logits against the definition in 64 bits."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import recurrent as R
+from oracle import rows
+from paper_1908_00213_amd import binding as B
+from rows_util import HALF, close, matrix, rounded, untouched, values
+
+pytestmark = pytest.mark.gpu
+IDS = {"i32": torch.int32, "i64": torch.int64}
+
+
+def dev(a, ids):
+    a = np.asarray(a)
+    if a.dtype.kind in "iu" and a.dtype != np.int32:
+        return torch.from_numpy(a).to(IDS[ids]).cuda()
+    return torch.from_numpy(np.ascontiguousarray(a)).cuda()
+
+
+def check(z, dtype="f32", out="f32", pad=0, ids="i64", in_place=False, **p):
+    z = rounded(z, dtype)
+    want, bound = R.adjust(z, **p)
+    zd = matrix(z, dtype, pad, pad)
+    o = zd if in_place else matrix(np.zeros(z.shape), out, pad, 2 * pad)
+    B.logits_adjust(zd, o, **{k: dev(v, ids) for k, v in p.items()})
+    half = HALF[dtype if in_place else out]
+    got = values(o)
+    gone = np.isneginf(want)
+    assert np.array_equal(np.isneginf(got), gone)
+    close(np.where(gone, 0, got), np.where(gone, 0, want), np.where(gone, 0, bound + half * (np.abs(np.where(gone, 0, want)) + bound)))
+    assert untouched(o, pad, pad if in_place else 2 * pad)
+    return got
+
+
+def masks(n, v, share, rng):
+    words = np.zeros((n, (v + 31) // 32), np.uint32)
+    for i in range(n):
+        bits = np.zeros(words.shape[1] * 32, np.uint8)
+        bits[:v] = rng.random(v) >= share
+        words[i] = np.packbits(bits, bitorder="little").view(np.uint32)
+    return words.view(np.int32)
+
+
+def parameters(n, v, length, m, which, rng):
+    p = {}
+    if "l" in which or "r" in which or "f" in which or "p" in which:
+        p["tokens"] = rng.integers(0, max(1, v // 3), (n, length)) * rng.choice([1, 3], (n, length))
+        p["tokens"][rng.random((n, length)) < 0.05] = rng.choice([-1, v, v + 7])
+    if "l" in which:
+        p["lengths"] = rng.integers(-1, length + 2, n)
+        p["prompt"] = rng.integers(-1, length + 2, n)
+    if "r" in which:
+        p["repetition"] = (1 + rng.random(n)).astype(np.float32)
+    if "f" in which:
+        p["frequency"] = rng.standard_normal(n).astype(np.float32)
+    if "p" in which:
+        p["presence"] = rng.standard_normal(n).astype(np.float32)
+    if "b" in which:
+        p["bias_ids"] = np.stack([rng.permutation(v + 2)[:m] - 1 for _ in range(n)])
+        p["bias"] = (rng.standard_normal((n, p["bias_ids"].shape[1])) * 3).astype(np.float32)
+    if "a" in which:
+        p["allowed"] = masks(n, v, 0.6, rng)
+    return p
+
+
+@pytest.mark.parametrize("dtype,out", [("f32", "f32"), ("bf16", "bf16"), ("bf16", "f32"), ("f32", "bf16")])
+@pytest.mark.parametrize("v,length,m,pad", [(1, 1, 1, 0), (2, 3, 2, 1), (31, 7, 5, 0), (33, 64, 20, 3), (257, 100, 30, 0), (1000, 35, 8, 8), (1023, 300, 64, 1), (1025, 257, 300, 0),
+                                            (10000, 1000, 100, 0), (10001, 35, 16, 5)])
+@pytest.mark.parametrize("which", ["", "r", "lf", "p", "b", "a", "lrfpba"])
+def test_adjust(v, length, m, pad, dtype, out, which):
+    n = 5
+    rng = np.random.default_rng(v + length)
+    z = rng.standard_normal((n, v)) * 2.5
+    p = parameters(n, v, length, m, which, rng)
+    got = check(z, dtype, out, pad, "i64", **p)
+    assert np.array_equal(check(z, dtype, out, pad, "i32", **p), got, equal_nan=True)
+    if dtype == out:
+        assert np.array_equal(check(z, dtype, out, pad, "i64", in_place=True, **p), got)
+
+
+@pytest.mark.parametrize("n,v,length", [(1, 131072, 2000), (3, 50001, 9000), (300, 2049, 40), (40, 40000, 200)])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_adjust_of_many_rows_and_large_vocabularies(n, v, length, dtype):
+    rng = np.random.default_rng(n)
+    check(rng.standard_normal((n, v)) * 3, dtype, "f32", 3, "i32", **parameters(n, v, length, 100, "lrfpba", rng))
+
+
+def test_biases_of_one_token_are_added_in_the_lists_order():
+    n, v, m = 4, 3000, 700
+    rng = np.random.default_rng(1)
+    z = rng.standard_normal((n, v)).astype(np.float32)
+    ids = rng.integers(0, 40, (n, m)) * 75
+    b = (rng.standard_normal((n, m)) * 10.0 ** rng.integers(-3, 4, (n, m))).astype(np.float32)
+    got = check(z, bias_ids=ids, bias=b, tokens=ids, repetition=np.full(n, 1.5, np.float32))
+    want = np.where(z > 0, z / np.float32(1.5), z * np.float32(1.5)).astype(np.float32)
+    for r in range(n):
+        for t in np.unique(ids[r]):
+            total = np.float32(0)
+            for x in b[r][ids[r] == t]:
+                total = np.float32(total + x)
+            assert got[r, t] == np.float32(want[r, t] + total)
+    check(z, bias_ids=np.full((n, m), 2999), bias=b)
+
+
+def test_counts_of_long_texts():
+    """One token 300000 times, half of it the prompt's."""
+    v, length = 100, 300000
+    z = np.zeros((2, v), np.float32)
+    t = np.full((2, length), 7)
+    got = check(z, tokens=t, frequency=np.array([1.0, 0.5], np.float32), prompt=np.array([150000, 0]), lengths=np.array([300000, 299999]))
+    assert got[0, 7] == -150000.0 and got[1, 7] == -149999.5
+
+
+def test_infinities_and_rows_that_nothing_is_left_of():
+    v = 100
+    z = np.zeros((3, v), np.float32)
+    z[0, 3], z[0, 4], z[1, 5] = np.inf, -np.inf, np.nan
+    none = np.zeros((3, 4), np.int32)
+    some = none.copy()
+    some[:, 0] = 0b111000
+    t = np.tile(np.array([3, 4, 5]), (3, 1))
+    params = dict(tokens=t, repetition=np.full(3, 2, np.float32), frequency=np.full(3, 1, np.float32))
+    o = torch.empty(3, v, device="cuda")
+    zd = torch.from_numpy(z).cuda()
+    B.logits_adjust(zd, o, **{k: dev(p, "i64") for k, p in params.items()})
+    got = values(o)
+    assert got[0, 3] == np.inf and got[0, 4] == -np.inf and np.isnan(got[1, 5]) and got[2, 5] == -1.0
+    z[1, 6] = np.nan                                     # a NaN that the mask leaves out is gone
+    B.logits_adjust(torch.from_numpy(z).cuda(), o, allowed=dev(some, "i64"), **{k: dev(p, "i64") for k, p in params.items()})
+    got = values(o)
+    assert np.isnan(got[1, 5]) and np.isneginf(np.delete(got, [3, 4, 5], 1)).all()
+    B.logits_adjust(zd, o, allowed=dev(none, "i64"))
+    assert np.isneginf(values(o)).all()
+    # and no token is drawn of such rows
+    out = torch.zeros(3, dtype=torch.int64, device="cuda")
+    B.sample(o, torch.full((3,), 0.5, device="cuda"), out)
+    assert out.tolist() == [-1] * 3
+
+
+def test_one_list_for_all_rows():
+    n, v = 6, 500
+    rng = np.random.default_rng(8)
+    z = rng.standard_normal((n, v)).astype(np.float32)
+    t, ids, b, a = rng.integers(0, v, (1, 30)), rng.permutation(v)[None, :9], rng.standard_normal((1, 9)).astype(np.float32), masks(1, v, 0.5, rng)
+    r, ln = np.array([1.3], np.float32), np.array([20])
+    rep = lambda x: np.repeat(x, n, 0)
+    want, bound = R.adjust(z, rep(t), rep(ln), None, rep(r), None, None, rep(ids), rep(b), rep(a))
+    o = torch.empty(n, v, device="cuda")
+    ex = lambda x: dev(x, "i64").expand(n, *x.shape[1:])
+    B.logits_adjust(torch.from_numpy(z).cuda(), o, tokens=ex(t), lengths=ex(ln), repetition=ex(r), bias_ids=ex(ids), bias=ex(b), allowed=ex(a))
+    got = values(o)
+    assert np.array_equal(np.isneginf(got), np.isneginf(want))
+    ok = ~np.isneginf(want)
+    close(got[ok], want[ok], bound[ok] + R.U * np.abs(want[ok]))
+
+
+def test_no_rows_no_tokens():
+    z = torch.empty(0, 5, device="cuda")
+    B.logits_adjust(z, torch.empty_like(z))
+    z = torch.randn(2, 5, device="cuda")
+    e = torch.empty(2, 0, device="cuda")
+    o = torch.empty_like(z)
+    ones = torch.full((2,), 3.0, device="cuda")
+    B.logits_adjust(z, o, tokens=e.long(), repetition=ones, frequency=ones, presence=ones, bias_ids=e.long(), bias=e)
+    assert torch.equal(o, z)
+
+
+def test_the_way_to_a_token_in_a_captured_graph():
+    """Adjusted and drawn, replayed while the text grows: the tokens are those of the definitions."""
+    n, v, cap = 7, 5000, 64
+    rng = np.random.default_rng(6)
+    z = torch.empty(n, v, device="cuda")
+    o = torch.empty_like(z)
+    u, out = torch.empty(n, device="cuda"), torch.zeros(n, dtype=torch.int64, device="cuda")
+    text = torch.full((n, cap), -1, device="cuda", dtype=torch.int64)
+    length = torch.full((n,), 5, device="cuda", dtype=torch.int64)
+    rep, freq, pres = (torch.full((n,), x, device="cuda") for x in (1.5, 0.5, 0.25))
+    allowed = masks(n, v, 0.3, rng)
+    al = torch.from_numpy(allowed).cuda()
+    text[:, :5] = torch.from_numpy(rng.integers(0, v, (n, 5))).cuda()
+    prompt = torch.full((n,), 2, device="cuda", dtype=torch.int64)
+
+    def call():
+        B.logits_adjust(z, o, tokens=text, lengths=length, prompt=prompt, repetition=rep, frequency=freq, presence=pres, allowed=al)
+        B.sample(o, u, out)
+    call()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+    for k in range(5):
+        zz, uu = np.float32(rng.standard_normal((n, v)) * 3), rng.random(n, dtype=np.float32)
+        z.copy_(torch.from_numpy(zz)), u.copy_(torch.from_numpy(uu))
+        graph.replay()
+        torch.cuda.synchronize()
+        want, bound = R.adjust(zz, text.cpu().numpy(), length.cpu().numpy(), prompt.cpu().numpy(), rep.cpu().numpy(), freq.cpu().numpy(), pres.cpu().numpy(), None, None, allowed)
+        got = values(o)
+        ok = ~np.isneginf(want)
+        assert np.array_equal(np.isneginf(got), ~ok)
+        close(got[ok], want[ok], bound[ok] + R.U * np.abs(want[ok]))
+        assert np.array_equal(out.cpu().numpy(), rows.sample(o.cpu().numpy(), uu))
+        text[torch.arange(n, device="cuda"), length] = out
+        length += 1
