@@ -509,7 +509,7 @@ chn_status chn_sample(const chn_array *logits, const chn_array *u, const chn_arr
  *     frequency (N,) F32:  then z - frequency * c;      presence (N,) F32: then z - presence, if c > 0;
  *   bias_ids (N,M) I32 or I64 and bias (N,M) F32: then z + the biases whose id is i, added up in the order of the list;
  *   allowed (N, ceil(V/32)) I32: then -inf unless bit i % 32 of word i / 32 is set.  A mask may leave nothing.
- * Every parameter NULL where it is not used (penalties without tokens are CHN_ERR_NULL, biases without ids too); stride 0: one row for all.  lengths and prompt are cut to 0 .. L,
+ * Every parameter NULL where it is not used (no tokens: empty lists; biases without ids are CHN_ERR_NULL); stride 0: one row for all.  lengths and prompt are cut to 0 .. L,
  * ids outside [0, V) are passed over.  out: (N,V) F32 or BF16, which may be the array of logits.  fp32 arithmetic in a fixed order, rounded once at the
  * end; L below 2^30, V below 2^31 (CHN_ERR_SHAPE).  No workspace. */
 chn_status chn_logits_adjust(const chn_array *logits, const chn_array *tokens, const chn_array *lengths, const chn_array *prompt,
@@ -532,7 +532,7 @@ chn_status chn_logits_adjust(const chn_array *logits, const chn_array *tokens, c
  * States and gradients are fp32, results the same bits from run to run.  Sequences of more than 128 steps are cut in pieces of as many, whose effect is
  * (the product of the decays, the state from zero): where that product leaves fp32's range (decays above 1), so does the result.
  * An output may be the very array of an input (h_last of h0, y of x, dgate of gate, dx of x or dy).
- * T = 0 copies the state.  T, B, D below 2^31, B * D below 2^40 (CHN_ERR_SHAPE).
+ * T = 0 copies the state.  T and B below 2^31, D below 2^30, B * D up to 2^40 (CHN_ERR_SHAPE).
  * ws: chn_gated_scan_workspace_bytes(gate) bytes, 256-byte aligned, the library's until the work on `stream` is done; the backward pass may use the same. */
 enum { CHN_SCAN_SIGMOID = 0, CHN_SCAN_DECAY = 1 };
 #define CHN_SCAN_STRIDE 16

@@ -176,8 +176,6 @@ chn_status chn_logits_adjust(const chn_array *logits, const chn_array *tokens, c
   const int64_t N = a.N;
   if (on != N || ov != a.V) return fail(CHN_ERR_SHAPE, "logits_adjust: out must have shape (%lld,%lld)", (long long)N, (long long)a.V);
   if (a.V > 0x7fffffff || N > 0x7fffffff) return fail(CHN_ERR_SHAPE, "logits_adjust: (%lld,%lld) logits", (long long)N, (long long)a.V);
-  if (!tokens && (lengths || prompt || repetition || frequency || presence))
-    return fail(CHN_ERR_NULL, "logits_adjust: lengths, prompt, repetition, frequency and presence need tokens");
   if (!bias != !bias_ids) return fail(CHN_ERR_NULL, "logits_adjust: bias and bias_ids come together");
   CHN_TRY(row_param(lengths, "lengths", true, N, &a.sl));
   CHN_TRY(row_param(prompt, "prompt", true, N, &a.sp));

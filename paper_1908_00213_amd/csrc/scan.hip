@@ -1,8 +1,17 @@
 // chn_gated_scan_fwd / _bwd: a gated linear recurrence over time and its gradient.
 #include "rows.h"
 
+#include <initializer_list>
+#include <type_traits>
+
 namespace chn {
 namespace {
+
+constexpr int kSteps = CHN_SCAN_STRIDE;        // steps of a wave
+constexpr int kWaves = 8;                      // waves of a block, at most
+constexpr int kPiece = kSteps * kWaves;        // steps of a block
+constexpr int kGroup = 2 * kWaves;             // pieces of a group
+constexpr int kPolls = 1 << 18;                // (a large part of a second: what is waited for is under way already)
 
 struct ScanArgs {
   const void *gate, *x, *dy;
@@ -11,10 +20,15 @@ struct ScanArgs {
   float *h_last, *states, *dh0;
   const void *lengths;
   int64_t T, B, D;
-  int64_t gt, gb, xt, xb, yt, yb, ht, hb;   // strides in elements: gate (dgate: ht, hb), x, y or dy
+  int64_t gt, gb, xt, xb, yt, yb, ht, hb;   // strides in elements: gate, x, y or dy, dgate
   int64_t ut, ub, p0, pl;                   // dx; rows of h0 or dh0, of h_last or dh_last
   int64_t len_stride;
   int len64;
+  // the launch
+  int64_t subs, pieces, upr, tiles;         // waves' shares of the steps, blocks' shares; units of V columns in a row, blocks next to each other
+  unsigned long long *effects;              // (piece, B, D): what a piece does to the state, the product of the decays and the state from zero
+  unsigned *starts;                         // (group, B, D): the state before a group of pieces
+  unsigned *ticket;
 };
 
 // a and 1 - a of the sigmoid gate, both to about an ulp: exp(-|g|) from the hardware's 2^t, t in two parts, and a reciprocal with a Newton step.
@@ -39,73 +53,427 @@ __device__ __forceinline__ int64_t sequence_end(const ScanArgs &s, int64_t b) {
   return n < 0 ? 0 : n > s.T ? s.T : n;
 }
 
-template <typename TI, typename TO, bool SIGMOID>
-__global__ __launch_bounds__(256) void scan_fwd_kernel(ScanArgs s) {
-  const int64_t c = block_number() * 256 + threadIdx.x;
-  if (c >= s.B * s.D) return;
-  const int64_t b = c / s.D, d = c - b * s.D;
-  const TI *g = static_cast<const TI *>(s.gate) + b * s.gb + d, *x = static_cast<const TI *>(s.x) + b * s.xb + d;
-  TO *y = static_cast<TO *>(s.y) + b * s.yb + d;
-  const int64_t end = sequence_end(s, b);
-  float h = s.h0 ? s.h0[b * s.p0 + d] : 0.0f;
-  for (int64_t t = 0; t < s.T; ++t) {
-    if (s.states && t % CHN_SCAN_STRIDE == 0) s.states[t / CHN_SCAN_STRIDE * s.B * s.D + c] = h;
-    float out = 0.0f;
-    if (t < end) {
-      float a = Elem<TI>::load(g + t * s.gt), u = Elem<TI>::load(x + t * s.xt);
-      if constexpr (SIGMOID) {
-        float rest;
-        gate_parts(a, a, rest);
-        u *= rest;
-      }
-      out = h = fmaf(a, h, u);
-    }
-    Elem<TO>::store(y + t * s.yt, out);
+template <int V> using Vals = float __attribute__((ext_vector_type(V)));
+
+// V neighbouring values as they lie in memory, at any element address.
+template <typename T, int V> struct Few;
+template <> struct Few<float, 1> {
+  float r;
+  __device__ __forceinline__ void load(const float *p) { r = *p; }
+  __device__ __forceinline__ float get(int) const { return r; }
+  static __device__ __forceinline__ void store(float *p, Vals<1> v) { *p = v[0]; }
+};
+template <> struct Few<bf16_raw, 1> {
+  uint32_t r;
+  __device__ __forceinline__ void load(const bf16_raw *p) { r = *p; }
+  __device__ __forceinline__ float get(int) const { return __uint_as_float(r << 16); }
+  static __device__ __forceinline__ void store(bf16_raw *p, Vals<1> v) { *p = f32_to_bf16(v[0]); }
+};
+typedef uint32_t u32_any __attribute__((aligned(2)));
+typedef float f32x2_any __attribute__((ext_vector_type(2), aligned(4)));
+template <> struct Few<bf16_raw, 2> {
+  uint32_t r;
+  __device__ __forceinline__ void load(const bf16_raw *p) { r = *reinterpret_cast<const u32_any *>(p); }
+  __device__ __forceinline__ float get(int i) const { return __uint_as_float(i ? r & 0xffff0000u : r << 16); }
+  static __device__ __forceinline__ void store(bf16_raw *p, Vals<2> v) {
+    *reinterpret_cast<u32_any *>(p) = (uint32_t)f32_to_bf16(v[0]) | (uint32_t)f32_to_bf16(v[1]) << 16;
   }
-  if (s.h_last) s.h_last[b * s.pl + d] = h;
+};
+template <> struct Few<float, 2> {
+  f32x2_any r;
+  __device__ __forceinline__ void load(const float *p) { r = *reinterpret_cast<const f32x2_any *>(p); }
+  __device__ __forceinline__ float get(int i) const { return r[i]; }
+  static __device__ __forceinline__ void store(float *p, Vals<2> v) { *reinterpret_cast<f32x2_any *>(p) = f32x2_any{v[0], v[1]}; }
+};
+
+// Where a lane works: V columns of one sequence.  The last unit of a row of odd length begins one column early and stores its last column alone.
+// A wave's rows are addressed from that of its first lane: a pointer for the wave and 32 bits for a lane, whose reach the host has looked at.
+template <int V>
+struct Place {
+  int64_t b, d, end;
+  int b0;                                                    // of the first lane
+  bool live, whole;
+  __device__ __forceinline__ Place(const ScanArgs &s, int64_t tile) {
+    const int64_t u = tile * 64 + (threadIdx.x & 63);
+    b = u / s.upr;
+    const int64_t j = u - b * s.upr;
+    live = b < s.B && j * V < s.D;
+    b = min(b, s.B - 1);
+    b0 = __builtin_amdgcn_readfirstlane((int)b);
+    d = j * V;
+    whole = d + V <= s.D;
+    d = whole ? d : s.D - V;
+    end = sequence_end(s, b);
+  }
+  template <typename T>
+  __device__ __forceinline__ unsigned offset(int64_t sb) const { return (unsigned)(((b - b0) * sb + d) * (int64_t)sizeof(T)); }
+  __device__ __forceinline__ bool owns(int v) const { return live && (whole || v == V - 1); }
+  template <typename T>
+  __device__ __forceinline__ void store(T *p, Vals<V> v) const {
+    if (live) {
+      if (whole) Few<T, V>::store(p, v);
+      else Elem<T>::store(p + V - 1, v[V - 1]);
+    }
+  }
+};
+
+template <typename T>
+__device__ __forceinline__ T *moved(T *p, unsigned bytes) {
+  return reinterpret_cast<T *>(reinterpret_cast<char *>(const_cast<std::remove_const_t<T> *>(p)) + (uint64_t)bytes);
 }
 
-template <typename TI, typename TO, bool SIGMOID>
-__global__ __launch_bounds__(256) void scan_bwd_kernel(ScanArgs s) {
-  const int64_t c = block_number() * 256 + threadIdx.x;
-  if (c >= s.B * s.D) return;
-  const int64_t b = c / s.D, d = c - b * s.D;
-  const TI *g = static_cast<const TI *>(s.gate) + b * s.gb + d, *x = static_cast<const TI *>(s.x) + b * s.xb + d;
-  const TO *dy = static_cast<const TO *>(s.dy) + b * s.yb + d;
-  TI *dg = static_cast<TI *>(s.dgate) + b * s.hb + d, *dx = static_cast<TI *>(s.dx) + b * s.ub + d;
-  const int64_t end = sequence_end(s, b);
-  float G = s.dh_last ? s.dh_last[b * s.pl + d] : 0.0f;
-  for (int64_t k = (s.T + CHN_SCAN_STRIDE - 1) / CHN_SCAN_STRIDE - 1; k >= 0; --k) {
-    float h = s.states[k * s.B * s.D + c], before[CHN_SCAN_STRIDE], av[CHN_SCAN_STRIDE], rv[CHN_SCAN_STRIDE], xv[CHN_SCAN_STRIDE];
+__device__ __forceinline__ unsigned long long together(float a, float u) {
+  const unsigned long long w = (unsigned long long)__float_as_uint(u) << 32 | __float_as_uint(a);
+  return w == ~0ull ? 0x7fc000007fc00000ull : w;             // (all bits set: not there yet)
+}
+
+template <int V>
+struct Shared {
+  float2 mine[kWaves][V][64];                                // what each wave does to the state
+  float2 theirs[kWaves][V][64];                              // what the pieces before this one do, two at a time
+  float start[V][64];
+  unsigned ticket;
+};
+
+// The state (forward: h, backward: the gradient that flows into a step from the next one) that a wave begins with, from what the waves do to it.
+// An effect is an affine map: state -> a state + u.  `first`: the state that the walk begins with.  Waves, pieces and groups are joined in one fixed
+// order, so results do not depend on which block runs when.  A piece waits for those before it in its group and for the group's start; all
+// of them have drawn their tickets before, so their blocks run already and wait for nothing behind them.
+template <int V>
+__device__ __forceinline__ void begin_with(const ScanArgs &s, Shared<V> &sh, const Place<V> &at, int64_t piece, int waves, Vals<V> a, Vals<V> u, Vals<V> first,
+                                           Vals<V> &state) {
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 #pragma unroll
-    for (int i = 0; i < CHN_SCAN_STRIDE; ++i) {
-      const int64_t t = k * CHN_SCAN_STRIDE + i;
-      before[i] = h;
-      av[i] = rv[i] = xv[i] = 0.0f;
-      if (t < end) {
-        av[i] = Elem<TI>::load(g + t * s.gt);
-        xv[i] = Elem<TI>::load(x + t * s.xt);
-        rv[i] = 1.0f;
-        if constexpr (SIGMOID) gate_parts(av[i], av[i], rv[i]);
-        h = fmaf(av[i], h, rv[i] * xv[i]);
+  for (int v = 0; v < V; ++v) {
+    float f = first[v];
+    asm volatile("" : "+v"(f));                              // (has been read when the others hear of this piece: its memory may be where the walk's last state goes)
+    sh.mine[wave][v][lane] = make_float2(a[v], u[v]);
+    state[v] = f;
+  }
+  __syncthreads();
+  if (s.pieces > 1) {
+    const int64_t group = piece / kGroup;
+    const int before = (int)(piece - group * kGroup);
+    const int64_t row = s.B * s.D, column = at.b * s.D + at.d;
+    if (wave == 0 && before < kGroup - 1 && piece < s.pieces - 1) {
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        float2 e = sh.mine[0][v][lane];
+        for (int w = 1; w < waves; ++w) {
+          const float2 f = sh.mine[w][v][lane];
+          e = make_float2(f.x * e.x, fmaf(f.x, e.y, f.y));
+        }
+        if (at.owns(v)) __hip_atomic_store(s.effects + piece * row + column + v, together(e.x, e.y), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
       }
     }
+    if (2 * wave < before) {
+      const int64_t p0 = (group * kGroup + 2 * wave) * row + column, p1 = 2 * wave + 1 < before ? p0 + row : p0;
+      unsigned long long e0[V], e1[V];
+      bool missing = true;
+      for (int polls = 0; polls < kPolls && missing; ++polls) {
+        missing = false;
 #pragma unroll
-    for (int i = CHN_SCAN_STRIDE - 1; i >= 0; --i) {
-      const int64_t t = k * CHN_SCAN_STRIDE + i;
-      if (t >= s.T) continue;
-      float vg = 0.0f, vx = 0.0f;
-      if (t < end) {
-        G += Elem<TO>::load(dy + t * s.yt);
-        vx = rv[i] * G;
-        vg = SIGMOID ? vx * av[i] * (before[i] - xv[i]) : before[i] * G;
-        G *= av[i];
+        for (int v = 0; v < V; ++v) {
+          e0[v] = __hip_atomic_load(s.effects + p0 + v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+          e1[v] = __hip_atomic_load(s.effects + p1 + v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        }
+#pragma unroll
+        for (int v = 0; v < V; ++v) missing |= e0[v] == ~0ull || e1[v] == ~0ull;
+        missing = __any(missing);
       }
-      Elem<TI>::store(dg + t * s.ht, vg);
-      Elem<TI>::store(dx + t * s.ut, vx);
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        // (one that never came is NaN, all of its bits set)
+        float2 e = make_float2(__uint_as_float((unsigned)e0[v]), __uint_as_float((unsigned)(e0[v] >> 32)));
+        if (p1 != p0) {
+          const float2 f = make_float2(__uint_as_float((unsigned)e1[v]), __uint_as_float((unsigned)(e1[v] >> 32)));
+          e = make_float2(f.x * e.x, fmaf(f.x, e.y, f.y));
+        }
+        sh.theirs[wave][v][lane] = e;
+      }
+    }
+    if (wave == kWaves - 1 && group > 0) {
+      const int64_t p = group * row + column;
+      unsigned e[V];
+      bool missing = true;
+      for (int polls = 0; polls < kPolls && missing; ++polls) {
+        missing = false;
+#pragma unroll
+        for (int v = 0; v < V; ++v) e[v] = __hip_atomic_load(s.starts + p + v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+#pragma unroll
+        for (int v = 0; v < V; ++v) missing |= e[v] == ~0u;
+        missing = __any(missing);
+      }
+#pragma unroll
+      for (int v = 0; v < V; ++v) sh.start[v][lane] = __uint_as_float(e[v]);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      if (group > 0) state[v] = sh.start[v][lane];
+      for (int w = 0; 2 * w < before; ++w) state[v] = fmaf(sh.theirs[w][v][lane].x, state[v], sh.theirs[w][v][lane].y);
+    }
+    if (wave == kWaves - 1 && before == kGroup - 1 && piece < s.pieces - 1) {
+      const int64_t p = (group + 1) * row + column;
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        float h = state[v];
+        for (int w = 0; w < waves; ++w) h = fmaf(sh.mine[w][v][lane].x, h, sh.mine[w][v][lane].y);
+        const unsigned bits = __float_as_uint(h);
+        if (at.owns(v)) __hip_atomic_store(s.starts + p + v, bits == ~0u ? 0x7fc00000u : bits, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      }
     }
   }
-  if (s.dh0) s.dh0[b * s.p0 + d] = G;
+#pragma unroll
+  for (int v = 0; v < V; ++v)
+    for (int w = 0; w < wave; ++w) state[v] = fmaf(sh.mine[w][v][lane].x, state[v], sh.mine[w][v][lane].y);
+}
+
+// The block's piece and tile, the pieces of all tiles in the order of the walk.
+template <int V>
+__device__ __forceinline__ void next_job(const ScanArgs &s, Shared<V> &sh, int64_t &piece, int64_t &tile) {
+  int64_t job = block_number();
+  if (s.pieces > 1) {
+    if (threadIdx.x == 0) sh.ticket = __hip_atomic_fetch_add(s.ticket, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    __syncthreads();
+    job = __builtin_amdgcn_readfirstlane((int)sh.ticket);    // (fewer than 2^31 jobs and blocks)
+  }
+  piece = job / s.tiles;
+  tile = job - piece * s.tiles;
+}
+
+template <typename TI, typename TO, int V, bool SIGMOID>
+__global__ __launch_bounds__(64 * kWaves, 4) void scan_fwd_kernel(ScanArgs s) {
+  __shared__ Shared<V> sh;
+  int64_t piece, tile;
+  next_job(s, sh, piece, tile);
+  if (piece >= s.pieces) return;                             // (the grid's last line may be longer than the jobs)
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
+  const Place<V> at(s, tile);
+  const int64_t sub = piece * kWaves + wave, t0 = sub * kSteps;
+  const TI *g = static_cast<const TI *>(s.gate) + at.b0 * s.gb, *x = static_cast<const TI *>(s.x) + at.b0 * s.xb;
+  const unsigned go = at.template offset<TI>(s.gb), xo = at.template offset<TI>(s.xb);
+  Few<TI, V> gr[kSteps], xr[kSteps];
+#pragma unroll
+  for (int i = 0; i < kSteps; ++i) {
+    const int64_t t = min(t0 + i, s.T - 1);
+    gr[i].load(moved(g + t * s.gt, go));
+    xr[i].load(moved(x + t * s.xt, xo));
+  }
+  __builtin_amdgcn_sched_barrier(0);                         // (all loads first)
+  const int n = (int)min(max(at.end - t0, (int64_t)0), (int64_t)kSteps), nt = (int)min(s.T - t0, (int64_t)kSteps);
+  Vals<V> h, first, A, U, a[kSteps], u[kSteps];
+#pragma unroll
+  for (int v = 0; v < V; ++v) {
+    first[v] = s.h0 ? s.h0[at.b * s.p0 + at.d + v] : 0.0f;
+    A[v] = 1.0f;
+    U[v] = 0.0f;
+  }
+#pragma unroll
+  for (int i = 0; i < kSteps; ++i) {
+    const bool on = i < n;
+    if (i % 2 == 0) __builtin_amdgcn_sched_barrier(0);       // (two steps at a time: more of them at once take registers that two blocks do not have)
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      float av = gr[i].get(v), uv = xr[i].get(v);
+      if constexpr (SIGMOID) {
+        float rest;
+        gate_parts(av, av, rest);
+        uv *= rest;
+      }
+      a[i][v] = on ? av : 1.0f;
+      u[i][v] = on ? uv : 0.0f;
+      A[v] *= a[i][v];
+      U[v] = fmaf(a[i][v], U[v], u[i][v]);
+    }
+  }
+  begin_with<V>(s, sh, at, piece, waves, A, U, first, h);
+  if (t0 >= s.T) return;
+  if (s.states) at.store(s.states + (sub * s.B + at.b) * s.D + at.d, h);
+  TO *y = static_cast<TO *>(s.y) + at.b0 * s.yb + t0 * s.yt;
+  const unsigned yo = at.template offset<TO>(s.yb);
+#pragma unroll
+  for (int i = 0; i < kSteps; ++i) {
+    if (i >= nt) continue;
+    Vals<V> out;
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      h[v] = fmaf(a[i][v], h[v], u[i][v]);
+      out[v] = i < n ? h[v] : 0.0f;
+    }
+    at.store(moved(y + i * s.yt, yo), out);
+  }
+  if (s.h_last && t0 + kSteps >= s.T) at.store(s.h_last + at.b * s.pl + at.d, h);
+}
+
+// Backwards: the wave whose steps are the last ones begins.  The state before each step is computed again from the one that the forward pass kept.  Of a
+// step stay three numbers and dy: the smaller of a and 1 - a (with its sign saying which one it is: the other one is 1 minus it, to half a step),
+// and what dgate has G multiplied with.
+template <typename TI, typename TO, int V, bool SIGMOID>
+__global__ __launch_bounds__(64 * kWaves, 4) void scan_bwd_kernel(ScanArgs s) {
+  __shared__ Shared<V> sh;
+  int64_t piece, tile;
+  next_job(s, sh, piece, tile);
+  if (piece >= s.pieces) return;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
+  const Place<V> at(s, tile);
+  const int64_t walk = piece * kWaves + wave, sub = s.subs - 1 - walk, t0 = max(sub, (int64_t)0) * kSteps;
+  const bool any = sub >= 0;                                 // (the last block's last waves may have no steps)
+  const TI *g = static_cast<const TI *>(s.gate) + at.b0 * s.gb, *x = static_cast<const TI *>(s.x) + at.b0 * s.xb;
+  const TO *dy = static_cast<const TO *>(s.dy) + at.b0 * s.yb;
+  const unsigned go = at.template offset<TI>(s.gb), xo = at.template offset<TI>(s.xb), yo = at.template offset<TO>(s.yb);
+  Few<TI, V> gr[kSteps], xr[kSteps];
+  Few<TO, V> yr[kSteps];
+  Vals<V> h, first, A, U, part[kSteps], coef[kSteps];
+#pragma unroll
+  for (int i = 0; i < kSteps; ++i) {
+    const int64_t t = min(t0 + i, s.T - 1);
+    gr[i].load(moved(g + t * s.gt, go));
+    xr[i].load(moved(x + t * s.xt, xo));
+    yr[i].load(moved(dy + t * s.yt, yo));
+  }
+  const int n = any ? (int)min(max(at.end - t0, (int64_t)0), (int64_t)kSteps) : 0, nt = (int)min(s.T - t0, (int64_t)kSteps);
+#pragma unroll
+  for (int v = 0; v < V; ++v) {
+    first[v] = s.dh_last ? s.dh_last[at.b * s.pl + at.d + v] : 0.0f;
+    h[v] = s.states[((t0 / kSteps) * s.B + at.b) * s.D + at.d + v];
+  }
+  __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+  for (int i = 0; i < kSteps; ++i) {
+    const bool on = i < n;
+    if (i % 2 == 0) __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      const float xv = xr[i].get(v);
+      float a = gr[i].get(v);
+      if constexpr (SIGMOID) {
+        float rest;
+        const bool upper = a >= 0.0f;
+        gate_parts(a, a, rest);
+        float c = on ? (h[v] - xv) * (a * rest) : 0.0f;
+        asm volatile("" : "+v"(c));                          // (worked out here: where it is used it would keep four numbers alive until then)
+        coef[i][v] = c;
+        part[i][v] = on ? (upper ? -rest : a) : -0.0f;
+        h[v] = fmaf(a, h[v], rest * xv);
+      } else {
+        coef[i][v] = on ? h[v] : 0.0f;
+        part[i][v] = on ? a : 1.0f;
+        h[v] = fmaf(a, h[v], xv);
+      }
+    }
+  }
+  auto decay = [](float q) {
+    return !SIGMOID ? q : __float_as_int(q) < 0 ? 1.0f + q : q;
+  };
+#pragma unroll
+  for (int v = 0; v < V; ++v) {
+    A[v] = 1.0f;
+    U[v] = 0.0f;
+  }
+#pragma unroll
+  for (int i = kSteps - 1; i >= 0; --i) {
+    if (i % 2) __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      const float a = decay(part[i][v]), d = i < n ? yr[i].get(v) : 0.0f;
+      A[v] *= a;
+      U[v] = a * (U[v] + d);
+    }
+  }
+  __builtin_amdgcn_sched_barrier(0);
+  Vals<V> G;
+  begin_with<V>(s, sh, at, piece, waves, A, U, first, G);
+  if (!any) return;
+  TI *dg = static_cast<TI *>(s.dgate) + at.b0 * s.hb + t0 * s.ht, *dx = static_cast<TI *>(s.dx) + at.b0 * s.ub + t0 * s.ut;
+  const unsigned dgo = at.template offset<TI>(s.hb), dxo = at.template offset<TI>(s.ub);
+#pragma unroll
+  for (int i = kSteps - 1; i >= 0; --i) {
+    if (i >= nt) continue;
+    const bool on = i < n;
+    Vals<V> vg, vx;
+    if constexpr (sizeof(TO) == 2) asm volatile("" : "+v"(yr[i].r));   // (taken apart again, not kept apart)
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      float q = part[i][v];
+      asm volatile("" : "+v"(q));                            // (what is worked out from it is neither kept from above nor begun early, in registers that are not there)
+      const float a = decay(q);
+      if (on) G[v] += yr[i].get(v);
+      vg[v] = on ? coef[i][v] * G[v] : 0.0f;
+      const float rest = !SIGMOID ? 1.0f : __float_as_int(q) < 0 ? -q : 1.0f - q;
+      vx[v] = on ? rest * G[v] : 0.0f;
+      G[v] *= a;
+    }
+    at.store(moved(dg + i * s.ht, dgo), vg);
+    at.store(moved(dx + i * s.ut, dxo), vx);
+  }
+  if (s.dh0 && sub == 0) at.store(s.dh0 + at.b * s.p0 + at.d, G);
+}
+
+// Nothing is there yet, no ticket drawn.
+__global__ __launch_bounds__(256) void scan_clear_kernel(chn_u32x4 *words, int64_t n, unsigned *ticket) {
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) words[i] = chn_u32x4{~0u, ~0u, ~0u, ~0u};
+  if (blockIdx.x == 0 && threadIdx.x == 0) *ticket = 0;
+}
+
+// Without steps the state stays.
+__global__ __launch_bounds__(256) void scan_keep_kernel(const float *from, int64_t pf, float *to, int64_t pt, int64_t B, int64_t D) {
+  const int64_t c = block_number() * 256 + threadIdx.x;
+  if (c >= B * D) return;
+  const int64_t b = c / D, d = c - b * D;
+  to[b * pt + d] = from ? from[b * pf + d] : 0.0f;
+}
+
+// Columns of a lane: what fills four bytes.  (Backward, fp32 gradients of bfloat16 arrays would take more registers than two blocks have.)
+int columns(int dtype, int dy, int64_t D) { return dtype == CHN_BF16 && dy == CHN_BF16 && D > 1 ? 2 : 1; }
+
+// `apart`: every row of units begins with a wave of its own, so that a wave's lanes lie in one sequence.
+struct Sizes {
+  int64_t subs, pieces, upr, tiles, jobs;
+  size_t effects, starts, bytes;
+  Sizes(int64_t T, int64_t B, int64_t D, int V, bool apart) {
+    subs = (T + kSteps - 1) / kSteps;
+    pieces = (subs + kWaves - 1) / kWaves;
+    upr = (D + V - 1) / V;
+    if (apart) upr = (upr + 63) / 64 * 64;
+    tiles = (B * upr + 63) / 64;
+    jobs = pieces * tiles;
+    effects = ((size_t)pieces * B * D * 8 + 15) / 16 * 16;
+    starts = ((size_t)((pieces + kGroup - 1) / kGroup) * B * D * 4 + 15) / 16 * 16;
+    bytes = pieces > 1 ? 256 + effects + starts : 0;
+  }
+};
+
+// Whether the rows of a wave's lanes lie further apart than 32 bits reach.
+bool far_apart(int64_t B, int64_t D, int V, std::initializer_list<int64_t> strides) {
+  const int64_t upr = (D + V - 1) / V, rows = (63 + upr - 1) / upr < B - 1 ? (63 + upr - 1) / upr : B - 1;
+  for (int64_t sb : strides)
+    if (rows > 0 && sb > ((1ll << 30) - D) / rows) return true;      // elements of four bytes at most
+  return false;
+}
+
+// The launch that both directions share: clears the workspace where pieces wait for each other.
+chn_status lay_out(const Sizes &z, void *ws, hipStream_t st, ScanArgs *s, dim3 *grid, dim3 *block) {
+  s->subs = z.subs; s->pieces = z.pieces; s->upr = z.upr; s->tiles = z.tiles;
+  *grid = grid_of(z.jobs);
+  *block = dim3(64 * (unsigned)(z.subs < kWaves ? z.subs : kWaves));
+  if (z.pieces > 1) {
+    char *p = static_cast<char *>(ws);
+    s->ticket = reinterpret_cast<unsigned *>(p);
+    s->effects = reinterpret_cast<unsigned long long *>(p + 256);
+    s->starts = reinterpret_cast<unsigned *>(p + 256 + z.effects);
+    const int64_t n = (int64_t)(z.effects + z.starts) / 16;
+    const int64_t blocks = (n + 1023) / 1024;
+    hipLaunchKernelGGL(scan_clear_kernel, dim3((unsigned)(blocks < 2048 ? blocks : 2048)), dim3(256), 0, st, reinterpret_cast<chn_u32x4 *>(p + 256), n, s->ticket);
+    return check_launch("gated_scan");
+  }
+  return CHN_OK;
+}
+
+chn_status keep(const float *from, int64_t pf, float *to, int64_t pt, int64_t B, int64_t D, hipStream_t st) {
+  if (!to) return CHN_OK;
+  hipLaunchKernelGGL(scan_keep_kernel, grid_of((B * D + 255) / 256), dim3(256), 0, st, from, pf, to, pt, B, D);
+  return check_launch("gated_scan");
 }
 
 // (T,B,D) with unit inner stride; the strides of the others in elements.
@@ -145,7 +513,7 @@ chn_status common_args(int kind, const chn_array *gate, const chn_array *x, cons
   CHN_TRY(validate(gate, "gate", false));
   if (gate->ndim != 3) return fail(CHN_ERR_NDIM, "gated_scan: gate must have 3 dimensions, got %d", gate->ndim);
   s->T = gate->shape[0]; s->B = gate->shape[1]; s->D = gate->shape[2];
-  if (s->T > 0x7fffffff || s->B > 0x7fffffff || s->D > 0x7fffffff || s->B * s->D > (1ll << 40))
+  if (s->T > 0x7fffffff || s->B > 0x7fffffff || s->D >= (1 << 30) || s->B * s->D > (1ll << 40))
     return fail(CHN_ERR_SHAPE, "gated_scan: sizes of (%lld,%lld,%lld)", (long long)s->T, (long long)s->B, (long long)s->D);
   CHN_TRY(steps_of(gate, "gate", false, s->T, s->B, s->D, &s->gt, &s->gb));
   CHN_TRY(steps_of(x, "x", false, s->T, s->B, s->D, &s->xt, &s->xb));
@@ -177,7 +545,13 @@ extern "C" {
 
 int64_t chn_gated_scan_states(int64_t steps) { return steps <= 0 ? 0 : (steps - 1) / CHN_SCAN_STRIDE + 1; }
 
-size_t chn_gated_scan_workspace_bytes(const chn_array *gate) { return 0; }
+size_t chn_gated_scan_workspace_bytes(const chn_array *gate) {
+  using namespace chn;
+  if (!gate || gate->ndim != 3 || !is_float(gate->dtype)) return 0;
+  for (int k = 0; k < 3; ++k)
+    if (gate->shape[k] <= 0 || gate->shape[k] > 0x7fffffff) return 0;
+  return Sizes(gate->shape[0], gate->shape[1], gate->shape[2], 1, false).bytes;
+}
 
 chn_status chn_gated_scan_fwd(int kind, const chn_array *gate, const chn_array *x, const chn_array *h0, const chn_array *lengths, const chn_array *y,
                               const chn_array *h_last, const chn_array *states, void *ws, size_t ws_bytes, chn_stream stream) {
@@ -192,15 +566,21 @@ chn_status chn_gated_scan_fwd(int kind, const chn_array *gate, const chn_array *
   s.y = y->data;
   if (h0) s.h0 = static_cast<const float *>(h0->data);
   if (h_last) s.h_last = static_cast<float *>(h_last->data);
-  const dim3 grid = grid_of((s.B * s.D + 255) / 256);
   hipStream_t st = as_stream(stream);
-#define CHN_GO(TI, TO)                                                                                                                     \
-  do {                                                                                                                                     \
-    if (kind == CHN_SCAN_SIGMOID) hipLaunchKernelGGL((scan_fwd_kernel<TI, TO, true>), grid, dim3(256), 0, st, s);                          \
-    else hipLaunchKernelGGL((scan_fwd_kernel<TI, TO, false>), grid, dim3(256), 0, st, s);                                                  \
+  if (s.T == 0) return keep(s.h0, s.p0, s.h_last, s.pl, s.B, s.D, st);
+  const int V = columns(gate->dtype, CHN_BF16, s.D);
+  const Sizes z(s.T, s.B, s.D, V, far_apart(s.B, s.D, V, {s.gb, s.xb, s.yb}));
+  if (z.jobs > 0x7fffffffll) return fail(CHN_ERR_SHAPE, "gated_scan: %lld pieces of work", (long long)z.jobs);
+  dim3 grid, block;
+  CHN_TRY(lay_out(z, ws, st, &s, &grid, &block));
+#define CHN_GO(TI, TO, V_)                                                                                                      \
+  do {                                                                                                                          \
+    if (kind == CHN_SCAN_SIGMOID) hipLaunchKernelGGL((scan_fwd_kernel<TI, TO, V_, true>), grid, block, 0, st, s);                 \
+    else hipLaunchKernelGGL((scan_fwd_kernel<TI, TO, V_, false>), grid, block, 0, st, s);                                         \
   } while (0)
-  if (gate->dtype == CHN_F32) { if (y->dtype == CHN_F32) CHN_GO(float, float); else CHN_GO(float, bf16_raw); }
-  else { if (y->dtype == CHN_F32) CHN_GO(bf16_raw, float); else CHN_GO(bf16_raw, bf16_raw); }
+  if (gate->dtype == CHN_F32) { if (y->dtype == CHN_F32) CHN_GO(float, float, 1); else CHN_GO(float, bf16_raw, 1); }
+  else if (V == 2) { if (y->dtype == CHN_F32) CHN_GO(bf16_raw, float, 2); else CHN_GO(bf16_raw, bf16_raw, 2); }
+  else { if (y->dtype == CHN_F32) CHN_GO(bf16_raw, float, 1); else CHN_GO(bf16_raw, bf16_raw, 1); }
 #undef CHN_GO
   return check_launch("gated_scan_fwd");
 }
@@ -223,15 +603,21 @@ chn_status chn_gated_scan_bwd(int kind, const chn_array *gate, const chn_array *
   s.dy = dy->data; s.dgate = dgate->data; s.dx = dx->data;
   if (dh_last) s.dh_last = static_cast<const float *>(dh_last->data);
   if (dh0) s.dh0 = static_cast<float *>(dh0->data);
-  const dim3 grid = grid_of((s.B * s.D + 255) / 256);
   hipStream_t st = as_stream(stream);
-#define CHN_GO(TI, TO)                                                                                                                     \
-  do {                                                                                                                                     \
-    if (kind == CHN_SCAN_SIGMOID) hipLaunchKernelGGL((scan_bwd_kernel<TI, TO, true>), grid, dim3(256), 0, st, s);                          \
-    else hipLaunchKernelGGL((scan_bwd_kernel<TI, TO, false>), grid, dim3(256), 0, st, s);                                                  \
+  if (s.T == 0) return keep(s.dh_last, s.pl, s.dh0, s.p0, s.B, s.D, st);
+  const int V = columns(gate->dtype, dy->dtype, s.D);
+  const Sizes z(s.T, s.B, s.D, V, far_apart(s.B, s.D, V, {s.gb, s.xb, s.yb, s.hb, s.ub}));
+  if (z.jobs > 0x7fffffffll) return fail(CHN_ERR_SHAPE, "gated_scan: %lld pieces of work", (long long)z.jobs);
+  dim3 grid, block;
+  CHN_TRY(lay_out(z, ws, st, &s, &grid, &block));
+#define CHN_GO(TI, TO, V_)                                                                                                      \
+  do {                                                                                                                          \
+    if (kind == CHN_SCAN_SIGMOID) hipLaunchKernelGGL((scan_bwd_kernel<TI, TO, V_, true>), grid, block, 0, st, s);                 \
+    else hipLaunchKernelGGL((scan_bwd_kernel<TI, TO, V_, false>), grid, block, 0, st, s);                                         \
   } while (0)
-  if (gate->dtype == CHN_F32) { if (dy->dtype == CHN_F32) CHN_GO(float, float); else CHN_GO(float, bf16_raw); }
-  else { if (dy->dtype == CHN_F32) CHN_GO(bf16_raw, float); else CHN_GO(bf16_raw, bf16_raw); }
+  if (gate->dtype == CHN_F32) { if (dy->dtype == CHN_F32) CHN_GO(float, float, 1); else CHN_GO(float, bf16_raw, 1); }
+  else if (V == 2) CHN_GO(bf16_raw, bf16_raw, 2);
+  else { if (dy->dtype == CHN_F32) CHN_GO(bf16_raw, float, 1); else CHN_GO(bf16_raw, bf16_raw, 1); }
 #undef CHN_GO
   return check_launch("gated_scan_bwd");
 }

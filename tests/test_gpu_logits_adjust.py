@@ -165,6 +165,8 @@ def test_no_rows_no_tokens():
     ones = torch.full((2,), 3.0, device="cuda")
     B.logits_adjust(z, o, tokens=e.long(), repetition=ones, frequency=ones, presence=ones, bias_ids=e.long(), bias=e)
     assert torch.equal(o, z)
+    B.logits_adjust(z, o.zero_(), repetition=ones, frequency=ones, presence=ones, lengths=torch.ones(2, dtype=torch.int64, device="cuda"))
+    assert torch.equal(o, z)
 
 
 def test_the_way_to_a_token_in_a_captured_graph():
