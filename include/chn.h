@@ -511,7 +511,7 @@ chn_status chn_sample(const chn_array *logits, const chn_array *u, const chn_arr
  *   allowed (N, ceil(V/32)) I32: then -inf unless bit i % 32 of word i / 32 is set.  A mask may leave nothing.
  * Every parameter NULL where it is not used (no tokens: empty lists; biases without ids are CHN_ERR_NULL); stride 0: one row for all.  lengths and prompt are cut to 0 .. L,
  * ids outside [0, V) are passed over.  out: (N,V) F32 or BF16, which may be the array of logits.  fp32 arithmetic in a fixed order, rounded once at the
- * end; L below 2^30, V below 2^31 (CHN_ERR_SHAPE).  No workspace. */
+ * end; L and M below 2^30, V below 2^31 (CHN_ERR_SHAPE).  No workspace. */
 chn_status chn_logits_adjust(const chn_array *logits, const chn_array *tokens, const chn_array *lengths, const chn_array *prompt,
                              const chn_array *repetition, const chn_array *frequency, const chn_array *presence, const chn_array *bias_ids,
                              const chn_array *bias, const chn_array *allowed, const chn_array *out, chn_stream stream);

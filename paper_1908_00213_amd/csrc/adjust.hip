@@ -9,6 +9,9 @@
 namespace chn {
 namespace {
 
+constexpr int kThreads = 512;                // of a block, at most
+constexpr int kHeld = 16;                    // logits that a thread of a large launch holds
+constexpr int kListed = 512;                  // biases of a piece that are put in order in LDS
 constexpr uint32_t kSeen = 0x80000000u, kBiased = 0x40000000u, kCount = 0x3fffffffu;
 
 struct AdjustArgs {
@@ -23,114 +26,195 @@ struct AdjustArgs {
   int len64, prompt64;
 };
 
-__device__ __forceinline__ int64_t cut(const void *p, int is64, int64_t at, int64_t L) {
+__device__ __forceinline__ int cut(const void *p, int is64, int64_t at, int L) {
   const int64_t n = is64 ? static_cast<const int64_t *>(p)[at] : static_cast<const int32_t *>(p)[at];
-  return n < 0 ? 0 : n > L ? L : n;
+  return n < 0 ? 0 : n > L ? L : (int)n;
 }
 
 struct Penalties {
-  float repetition, frequency, presence;
-  bool rep, freq, pres;
+  float repetition, inverse, frequency, presence;
+  bool rep;
+  // (without frequency or presence: zeros, which change nothing but the sign of a zero)
   __device__ __forceinline__ float apply(float z, uint32_t word) const {
     const uint32_t c = word & kCount;
-    if (rep && (word & (kSeen | kCount))) z = z > 0.0f ? z / repetition : z * repetition;
-    if (freq) z = fmaf(-frequency, (float)c, z);
-    if (pres && c) z -= presence;
-    return z;
+    if (rep) {
+      const float q = z * inverse, d = fmaf(fmaf(-q, repetition, z), inverse, q);   // z / repetition, its rounding made good
+      const float less = z > 0.0f ? (d == d ? d : q) : z * repetition;
+      z = word & (kSeen | kCount) ? less : z;
+    }
+    return c ? fmaf(-frequency, (float)c, z) - presence : z;
   }
 };
 
-template <typename TI, typename TO, typename ID>
-__global__ __launch_bounds__(256) void adjust_kernel(AdjustArgs a) {
+// A token's place in the piece, `len` and above where it lies outside: ids are below 2^31, whatever wraps lies above.
+__device__ __forceinline__ uint32_t place(int32_t id, int64_t v0) { return (uint32_t)id - (uint32_t)v0; }
+__device__ __forceinline__ uint32_t place(int64_t id, int64_t v0) {
+  const uint64_t at = (uint64_t)id - (uint64_t)v0;
+  return at > 0xffffffffull ? ~0u : (uint32_t)at;
+}
+
+// f(i, values[i]) for the indexes [0, n) that belong to the thread, eight loads in flight.  `v` holds the first eight already.
+constexpr int kAhead = 8;
+template <typename ID>
+__device__ __forceinline__ void ahead(const ID *values, int n, ID (&v)[kAhead], int from) {
+  const int step = blockDim.x;
+#pragma unroll
+  for (int k = 0; k < kAhead; ++k) v[k] = values[min(from + k * step, n - 1)];
+}
+template <typename ID, typename F>
+__device__ __forceinline__ void each(const ID *values, int n, ID (&v)[kAhead], F f) {
+  const int step = blockDim.x;
+  for (int i = threadIdx.x; i < n; i += kAhead * step) {
+    if (i >= kAhead * step) ahead(values, n, v, i);
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k)
+      if (i + k * step < n) f(i + k * step, v[k]);
+  }
+}
+
+// K: units of a thread, which are on their way while the list is looked through.
+template <typename TI, typename TO, typename ID, int K>
+__global__ __launch_bounds__(kThreads, 8) void adjust_kernel(AdjustArgs a) {
   extern __shared__ uint32_t words[];
-  __shared__ int twice;
+  __shared__ int twice, listed;
+  __shared__ uint32_t place_of[kListed];               // the list's entries in this piece, in its order, where an id stands more than once
+  __shared__ float bias_of[kListed];
   constexpr int E = unit_elements<TI, TO>();
   const int64_t n = block_number() / a.tiles, v0 = (block_number() - n * a.tiles) * a.tile;
   if (n >= a.N) return;                                // (the grid's last line may be longer than its blocks)
-  const int len = (int)min(a.tile, a.V - v0);
+  const int len = (int)min(a.tile, a.V - v0), step = (int)blockDim.x * E;
   const TI *z = static_cast<const TI *>(a.z) + n * a.pz + v0;
   TO *out = static_cast<TO *>(a.out) + n * a.po + v0;
+  const int32_t *allowed = a.allowed ? a.allowed + n * a.pa : nullptr;
   const bool lists = a.tokens || a.bias;
-  if (lists) {
-    for (int i = threadIdx.x; i < len; i += 256) words[i] = 0;
-    if (threadIdx.x == 0) twice = 0;
-    __syncthreads();
-    if (a.tokens) {
-      const ID *t = static_cast<const ID *>(a.tokens) + n * a.pt;
-      const int64_t end = a.lengths ? cut(a.lengths, a.len64, n * a.sl, a.L) : a.L, mine = a.prompt ? cut(a.prompt, a.prompt64, n * a.sp, a.L) : 0;
-      for (int64_t i = threadIdx.x; i < end; i += 256) {
-        const int64_t at = (int64_t)t[i] - v0;
-        if ((uint64_t)at < (uint64_t)len) {
-          if (i >= mine) atomicAdd(&words[at], 1u);
-          else atomicOr(&words[at], kSeen);
-        }
-      }
-    }
-    if (a.bias) {
-      const ID *t = static_cast<const ID *>(a.bias_ids) + n * a.pi;
-      for (int64_t i = threadIdx.x; i < a.M; i += 256) {
-        const int64_t at = (int64_t)t[i] - v0;
-        if ((uint64_t)at < (uint64_t)len && (atomicOr(&words[at], kBiased) & kBiased)) twice = 1;
-      }
-    }
-    __syncthreads();
+  Unit<TI, E> u[K];
+  uint32_t bits[K];
+#pragma unroll
+  for (int k = 0; k < K; ++k) {
+    const int i = (int)threadIdx.x * E + k * step;
+    if (i + E <= len) u[k].load(z + i);
+    bits[k] = allowed && i < len ? (uint32_t)allowed[(v0 + i) >> 5] >> ((v0 + i) & 31) : ~0u;
   }
   Penalties p;
-  p.rep = a.repetition != nullptr; p.freq = a.frequency != nullptr; p.pres = a.presence != nullptr;
+  p.rep = a.repetition != nullptr;
   p.repetition = p.rep ? a.repetition[n * a.sr] : 1.0f;
-  p.frequency = p.freq ? a.frequency[n * a.sf] : 0.0f;
-  p.presence = p.pres ? a.presence[n * a.ss] : 0.0f;
-  const int32_t *allowed = a.allowed ? a.allowed + n * a.pa : nullptr;
-  for (int i = (int)threadIdx.x * E; i < len; i += 256 * E) {
-    const uint32_t bits = allowed ? (uint32_t)allowed[(v0 + i) >> 5] >> ((v0 + i) & 31) : ~0u;
+  p.inverse = 1.0f / p.repetition;
+  p.frequency = a.frequency ? a.frequency[n * a.sf] : 0.0f;
+  p.presence = a.presence ? a.presence[n * a.ss] : 0.0f;
+  const ID *tokens = static_cast<const ID *>(a.tokens) + n * a.pt, *named = static_cast<const ID *>(a.bias_ids) + n * a.pi;
+  ID name = -1;                                        // of the thread's first bias
+  if (lists) {
+    // (the barriers wait for every load: the list's first part is fetched together with the logits)
+    ID first[kAhead];
+    int end = 0, mine = 0;
+    if (a.tokens) {
+      ahead(tokens, (int)a.L, first, threadIdx.x);
+      end = a.lengths ? cut(a.lengths, a.len64, n * a.sl, (int)a.L) : (int)a.L;
+      mine = a.prompt ? cut(a.prompt, a.prompt64, n * a.sp, (int)a.L) : 0;
+    }
+    if (a.bias && (int)threadIdx.x < (int)a.M) name = named[threadIdx.x];
+    for (int i = (int)threadIdx.x * 4; i < len; i += (int)blockDim.x * 4) *reinterpret_cast<uint4 *>(words + i) = make_uint4(0, 0, 0, 0);
+    if (threadIdx.x == 0) twice = 0;
+    __syncthreads();
+    each(tokens, end, first, [&](int i, ID id) {
+      const uint32_t at = place(id, v0);
+      if (at < (uint32_t)len) {
+        if (i >= mine) atomicAdd(&words[at], 1u);
+        else atomicOr(&words[at], kSeen);
+      }
+    });
+    if (a.bias) {
+      for (int i = threadIdx.x; i < (int)a.M; i += blockDim.x) {
+        const uint32_t at = place(i < (int)blockDim.x ? name : named[i], v0);
+        if (at < (uint32_t)len && (atomicOr(&words[at], kBiased) & kBiased)) twice = 1;
+      }
+    }
+    __syncthreads();
+    if (a.bias && twice) {
+      if (threadIdx.x < 64) {
+        int count = 0;
+        for (int i0 = 0; i0 < (int)a.M; i0 += 64) {
+          const int i = i0 + (int)threadIdx.x;
+          const uint32_t at = i < (int)a.M ? place(named[i], v0) : ~0u;
+          const bool in = at < (uint32_t)len;
+          const unsigned long long m = __ballot(in);
+          const int to = count + __popcll(m & ((1ull << threadIdx.x) - 1));
+          if (in && to < kListed) {
+            place_of[to] = at;
+            bias_of[to] = a.bias[n * a.pb + i];
+          }
+          count += __popcll(m);
+        }
+        if (threadIdx.x == 0) listed = count;
+      }
+      __syncthreads();
+    }
+  }
+#pragma unroll
+  for (int k = 0; k < K; ++k) {
+    const int i = (int)threadIdx.x * E + k * step;
     if (i + E <= len) {
-      Unit<TI, E> u;
+      uint32_t w[E], any = 0;
       Unit<TO, E> o;
-      u.load(z + i);
-      uint32_t any = 0;
+#pragma unroll
+      for (int e = 0; e < E; e += 4) {
+        const uint4 q = lists ? *reinterpret_cast<const uint4 *>(words + i + e) : make_uint4(0, 0, 0, 0);
+        w[e] = q.x; w[e + 1] = q.y; w[e + 2] = q.z; w[e + 3] = q.w;
+        any |= q.x | q.y | q.z | q.w;
+      }
 #pragma unroll
       for (int e = 0; e < E; ++e) {
-        const uint32_t w = lists ? words[i + e] : 0u;
-        any |= w;
-        float v = u.get(e);
-        if (w) v = p.apply(v, w);
-        o.set(e, bits >> e & 1 ? v : -INFINITY);
+        const float v = p.apply(u[k].get(e), w[e]);
+        o.set(e, bits[k] >> e & 1 ? v : -INFINITY);
       }
       if (any & kBiased) {
 #pragma unroll
         for (int e = 0; e < E; ++e)
-          if (!(words[i + e] & kBiased)) Elem<TO>::store(out + i + e, o.get(e));
+          if (!(w[e] & kBiased)) Elem<TO>::store(out + i + e, o.get(e));
       } else {
         o.store(out + i);
       }
     } else {
       for (int e = 0; e < len - i; ++e) {
         const uint32_t w = lists ? words[i + e] : 0u;
-        float v = Elem<TI>::load(z + i + e);
-        if (w) v = p.apply(v, w);
-        if (!(w & kBiased)) Elem<TO>::store(out + i + e, bits >> e & 1 ? v : -INFINITY);
+        const float v = p.apply(Elem<TI>::load(z + i + e), w);
+        if (!(w & kBiased)) Elem<TO>::store(out + i + e, bits[k] >> e & 1 ? v : -INFINITY);
       }
     }
   }
   if (a.bias) {
-    const ID *t = static_cast<const ID *>(a.bias_ids) + n * a.pi;
     const float *b = a.bias + n * a.pb;
-    for (int64_t i = threadIdx.x; i < a.M; i += 256) {
-      const int64_t id = (int64_t)t[i], at = id - v0;
-      if ((uint64_t)at >= (uint64_t)len) continue;
-      float sum = b[i];
-      if (twice) {                                       // (the same id more than once, somewhere in this piece)
-        sum = 0.0f;
-        bool first = true;
-        for (int64_t j = 0; j < a.M; ++j)
-          if ((int64_t)t[j] == id) {
-            first = first && j >= i;
-            sum = j == i && first ? b[j] : sum + b[j];
-          }
-        if (!first) continue;
-      }
+    auto add = [&](uint32_t at, float sum) {
       const float v = p.apply(Elem<TI>::load(z + at), words[at]) + sum;
-      Elem<TO>::store(out + at, !allowed || ((uint32_t)allowed[id >> 5] >> (id & 31) & 1) ? v : -INFINITY);
+      Elem<TO>::store(out + at, !allowed || ((uint32_t)allowed[(v0 + at) >> 5] >> ((v0 + at) & 31) & 1) ? v : -INFINITY);
+    };
+    if (twice && listed <= kListed) {
+      // (the thread with an id's first entry adds up those behind it, in their order)
+      for (int i = threadIdx.x; i < listed; i += blockDim.x) {
+        const uint32_t at = place_of[i];
+        float sum = bias_of[i];
+        bool first = true;
+        for (int j = 0; j < listed; ++j)
+          if (j != i && place_of[j] == at) {
+            first = first && j > i;
+            sum += bias_of[j];
+          }
+        if (first) add(at, sum);
+      }
+    } else {
+      for (int i = threadIdx.x; i < (int)a.M; i += blockDim.x) {
+        const ID id = i < (int)blockDim.x ? name : named[i];
+        const uint32_t at = place(id, v0);
+        if (at >= (uint32_t)len) continue;
+        float sum = b[i];
+        bool first = true;
+        for (int j = 0; twice && j < (int)a.M; ++j)
+          if (j != i && named[j] == id) {
+            first = first && j > i;
+            sum += b[j];
+          }
+        if (first) add(at, sum);
+      }
     }
   }
 }
@@ -186,7 +270,7 @@ chn_status chn_logits_adjust(const chn_array *logits, const chn_array *tokens, c
   if (tokens) {
     CHN_TRY(row_list(tokens, "tokens", N, &a.L, &a.pt));
     if (!is_index(tokens->dtype)) return fail(CHN_ERR_DTYPE, "logits_adjust: tokens must be I32 or I64");
-    if (a.L >= (1 << 30)) return fail(CHN_ERR_SHAPE, "logits_adjust: lists of %lld tokens", (long long)a.L);
+    if (a.L >= 1 << 30) return fail(CHN_ERR_SHAPE, "logits_adjust: lists of %lld tokens", (long long)a.L);
     id64 = tokens->dtype == CHN_I64;
   }
   if (bias) {
@@ -195,6 +279,7 @@ chn_status chn_logits_adjust(const chn_array *logits, const chn_array *tokens, c
     CHN_TRY(row_list(bias, "bias", N, &m, &a.pb));
     if (!is_index(bias_ids->dtype)) return fail(CHN_ERR_DTYPE, "logits_adjust: bias_ids must be I32 or I64");
     if (bias->dtype != CHN_F32) return fail(CHN_ERR_DTYPE, "logits_adjust: bias must be F32");
+    if (a.M >= 1 << 30) return fail(CHN_ERR_SHAPE, "logits_adjust: lists of %lld biases", (long long)a.M);
     if (m != a.M) return fail(CHN_ERR_SHAPE, "logits_adjust: %lld biases for %lld ids", (long long)m, (long long)a.M);
     if (tokens && (bias_ids->dtype == CHN_I64) != id64) return fail(CHN_ERR_DTYPE, "logits_adjust: tokens and bias_ids must have one dtype");
     id64 = bias_ids->dtype == CHN_I64;
@@ -216,21 +301,23 @@ chn_status chn_logits_adjust(const chn_array *logits, const chn_array *tokens, c
     if (presence) a.presence = static_cast<const float *>(presence->data);
   }
   if (bias && a.M > 0) { a.bias = static_cast<const float *>(bias->data); a.bias_ids = bias_ids->data; }
-  // Pieces of at most 8192 tokens (32 KiB of words: four blocks on a compute unit), shorter ones while the launch has fewer than 1024 blocks.
-  int64_t tile = (a.V * N / 1024 + 1023) / 1024 * 1024;
-  tile = tile < 1024 ? 1024 : tile > 8192 ? 8192 : tile;
-  a.tile = tile;
-  a.tiles = (a.V + tile - 1) / tile;
-  const size_t lds = a.tokens || a.bias ? (size_t)tile * 4 : 0;
+  const int E = logits->dtype == CHN_F32 && out->dtype == CHN_F32 ? 4 : 8;
+  const bool large = a.V * N >= 512ll * kThreads * kHeld;
+  const int threads = large ? kThreads : 256;
+  a.tile = threads * (large ? kHeld : E);
+  a.tiles = (a.V + a.tile - 1) / a.tile;
+  const size_t lds = a.tokens || a.bias ? (size_t)(a.tile < (a.V + 3) / 4 * 4 ? a.tile : (a.V + 3) / 4 * 4) * 4 : 0;
   hipStream_t st = as_stream(stream);
-  const dim3 grid = grid_of(N * a.tiles);
-#define CHN_GO(TI, TO)                                                                                                            \
+  const dim3 grid = grid_of(N * a.tiles), block(threads);
+#define CHN_GO(TI, TO, H)                                                                                                         \
   do {                                                                                                                            \
-    if (id64) hipLaunchKernelGGL((adjust_kernel<TI, TO, int64_t>), grid, dim3(256), lds, st, a);                                  \
-    else hipLaunchKernelGGL((adjust_kernel<TI, TO, int32_t>), grid, dim3(256), lds, st, a);                                       \
+    if (id64 && large) hipLaunchKernelGGL((adjust_kernel<TI, TO, int64_t, H>), grid, block, lds, st, a);                          \
+    else if (id64) hipLaunchKernelGGL((adjust_kernel<TI, TO, int64_t, 1>), grid, block, lds, st, a);                              \
+    else if (large) hipLaunchKernelGGL((adjust_kernel<TI, TO, int32_t, H>), grid, block, lds, st, a);                             \
+    else hipLaunchKernelGGL((adjust_kernel<TI, TO, int32_t, 1>), grid, block, lds, st, a);                                        \
   } while (0)
-  if (logits->dtype == CHN_F32) { if (out->dtype == CHN_F32) CHN_GO(float, float); else CHN_GO(float, bf16_raw); }
-  else { if (out->dtype == CHN_F32) CHN_GO(bf16_raw, float); else CHN_GO(bf16_raw, bf16_raw); }
+  if (logits->dtype == CHN_F32) { if (out->dtype == CHN_F32) CHN_GO(float, float, kHeld / 4); else CHN_GO(float, bf16_raw, kHeld / 8); }
+  else { if (out->dtype == CHN_F32) CHN_GO(bf16_raw, float, kHeld / 8); else CHN_GO(bf16_raw, bf16_raw, kHeld / 8); }
 #undef CHN_GO
   return check_launch("logits_adjust");
 }

@@ -80,7 +80,7 @@ def test_adjust(v, length, m, pad, dtype, out, which):
         assert np.array_equal(check(z, dtype, out, pad, "i64", in_place=True, **p), got)
 
 
-@pytest.mark.parametrize("n,v,length", [(1, 131072, 2000), (3, 50001, 9000), (300, 2049, 40), (40, 40000, 200)])
+@pytest.mark.parametrize("n,v,length", [(1, 131072, 2000), (3, 50001, 9000), (300, 2049, 40), (40, 40000, 200), (70, 131067, 5000), (600, 16385, 500)])
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_adjust_of_many_rows_and_large_vocabularies(n, v, length, dtype):
     rng = np.random.default_rng(n)
@@ -102,6 +102,9 @@ def test_biases_of_one_token_are_added_in_the_lists_order():
                 total = np.float32(total + x)
             assert got[r, t] == np.float32(want[r, t] + total)
     check(z, bias_ids=np.full((n, m), 2999), bias=b)
+    # more of them in one piece than are put in order at once
+    z, ids = z[:, :900], np.concatenate([rng.integers(0, 900, (n, 1500)), np.full((n, 30), -1)], 1)
+    check(z, bias_ids=ids, bias=rng.standard_normal((n, 1530)).astype(np.float32), allowed=masks(n, 900, 0.5, rng))
 
 
 def test_counts_of_long_texts():
