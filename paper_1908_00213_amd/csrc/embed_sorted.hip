@@ -46,13 +46,14 @@ __global__ __launch_bounds__(256) void embed_scaled_kernel(const TI *table, int6
 
 constexpr int kMaxBits = 9, kBins = 1 << kMaxBits;           // of a digit
 constexpr int kSortWaves = 16;
+constexpr int kFew = 8192;                                    // ids that one block sorts
 
 struct SortArgs {
   const void *ids;                   // pass 0 reads these
   const uint32_t *keys, *places;     // later ones these
   uint32_t *keys_out, *places_out;
   uint32_t *counts;                  // (blocks, bins)
-  uint32_t *ends;                    // (V), which the first launch clears
+  uint32_t *starts, *ends;           // (V)
   int64_t stride, V;
   uint32_t N, share;                 // pairs of a block
   int id64, shift, bits, blocks, first;
@@ -63,10 +64,6 @@ __device__ __forceinline__ uint32_t key_of(const SortArgs &s, bool first, const 
   return (uint32_t)(s.id64 ? id_at(static_cast<const int64_t *>(s.ids), i, s.stride, s.V) : id_at(static_cast<const int32_t *>(s.ids), i, s.stride, s.V));
 }
 
-__device__ __forceinline__ void clear_ends(uint32_t *ends, int64_t V, int64_t block, int64_t blocks) {
-  for (int64_t i = block * 1024 + threadIdx.x; i < V; i += blocks * 1024) ends[i] = 0;
-}
-
 // How often a block's share has each digit.
 __global__ __launch_bounds__(1024) void embed_count_kernel(SortArgs s) {
   __shared__ uint32_t count[kBins];
@@ -74,7 +71,6 @@ __global__ __launch_bounds__(1024) void embed_count_kernel(SortArgs s) {
   __syncthreads();
   const uint32_t lo = blockIdx.x * s.share, hi = min(lo + s.share, s.N), mask = (1u << s.bits) - 1;
   for (uint32_t i = lo + threadIdx.x; i < hi; i += 1024) atomicAdd(&count[key_of(s, s.first, s.keys, i) >> s.shift & mask], 1u);
-  if (s.first) clear_ends(s.ends, s.V, blockIdx.x, gridDim.x);
   __syncthreads();
   if (threadIdx.x <= mask) s.counts[blockIdx.x * kBins + threadIdx.x] = count[threadIdx.x];
 }
@@ -84,30 +80,30 @@ struct SortShared {
   uint32_t sums[kSortWaves];
 };
 
-// One pass over the block's share [lo, hi), split over the waves.  Before it: the same digit in the blocks before, smaller digits anywhere.
-__device__ __forceinline__ void sort_pass(const SortArgs &s, SortShared &sh, bool first, const uint32_t *keys, const uint32_t *places, uint32_t *keys_out,
-                                          uint32_t *places_out, uint32_t lo, uint32_t hi, int shift, const uint32_t *counts, int block, int blocks) {
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const uint32_t mask = (1u << s.bits) - 1;
-  for (int i = tid; i < kSortWaves * kBins; i += 1024) (&sh.at[0][0])[i] = 0;
-  __syncthreads();
-  const uint32_t part = ((hi - lo + kSortWaves - 1) / kSortWaves + 63) / 64 * 64;
-  const uint32_t from = min(lo + wave * part, hi), to = min(from + part, hi);
-  for (uint32_t i = from + lane; i < to; i += 64) atomicAdd(&sh.at[wave][key_of(s, first, keys, i) >> shift & mask], 1u);
-  __syncthreads();
-  uint32_t mine = 0, all = 0;
-  if (tid < kBins) {
-    if (blocks == 1) {
-      for (int w = 0; w < kSortWaves; ++w) all += sh.at[w][tid];
-    } else if (tid <= (int)mask) {
-#pragma unroll 8
-      for (int b = 0; b < blocks; ++b) {
-        const uint32_t c = counts[b * kBins + tid];
-        mine += b < block ? c : 0;
-        all += c;
-      }
-    }
+// The lanes whose digit is this lane's.
+__device__ __forceinline__ unsigned long long equals(bool on, uint32_t digit, int bits) {
+  unsigned long long same = __ballot(on);
+  for (int b = 0; b < bits; ++b) {
+    const bool bit = digit >> b & 1;
+    const unsigned long long m = __ballot(bit);
+    same &= bit ? m : ~m;
   }
+  return same;
+}
+
+// What the wave's lanes have written to LDS is what its lanes read from here on.
+__device__ __forceinline__ void wave_order() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
+// From the number of a digit's pairs in each wave to the place of its first one there.  count(d, before, all): how many pairs of digit d the blocks
+// before this one have, and how many there are.
+template <typename F>
+__device__ __forceinline__ void bases(SortShared &sh, F count) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  uint32_t mine = 0, all = 0;
+  if (tid < kBins) count(tid, mine, all);
   uint32_t run = all;                                        // running sums over the digits: in the wave, then over the waves
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) {
@@ -117,76 +113,132 @@ __device__ __forceinline__ void sort_pass(const SortArgs &s, SortShared &sh, boo
   if (lane == 63) sh.sums[wave] = run;
   __syncthreads();
   if (tid < kBins) {
-    uint32_t base = run - all + mine;
+    uint32_t base = run - all + mine, c[kSortWaves];
     for (int w = 0; w < wave; ++w) base += sh.sums[w];
+#pragma unroll
+    for (int w = 0; w < kSortWaves; ++w) c[w] = sh.at[w][tid];
+#pragma unroll
     for (int w = 0; w < kSortWaves; ++w) {
-      const uint32_t c = sh.at[w][tid];
       sh.at[w][tid] = base;
-      base += c;
+      base += c[w];
     }
   }
   __syncthreads();
-  for (uint32_t i0 = from; i0 < to; i0 += 64) {
-    const uint32_t i = i0 + lane;
-    const bool on = i < to;
-    const uint32_t key = on ? key_of(s, first, keys, i) : 0, place = on && !first ? places[i] : i, digit = key >> shift & mask;
-    unsigned long long same = __ballot(on);
-    for (int b = 0; b < s.bits; ++b) {
-      const bool bit = digit >> b & 1;
-      const unsigned long long m = __ballot(bit);
-      same &= bit ? m : ~m;
-    }
-    if (on) {
-      const uint32_t rank = __popcll(same & ((1ull << lane) - 1)), to_ = sh.at[wave][digit] + rank;
-      keys_out[to_] = key;
-      places_out[to_] = place;
-    }
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-    if (on && same >> lane == 1) sh.at[wave][digit] += __popcll(same);   // (the digit's last lane)
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-  }
 }
 
+// One pass over the block's share, split over the waves.
 __global__ __launch_bounds__(1024) void embed_sort_kernel(SortArgs s) {
   __shared__ SortShared sh;
   const uint32_t lo = min(blockIdx.x * s.share, s.N), hi = min(lo + s.share, s.N);
-  sort_pass(s, sh, s.first, s.keys, s.places, s.keys_out, s.places_out, lo, hi, s.shift, s.counts, blockIdx.x, s.blocks);
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const uint32_t mask = (1u << s.bits) - 1;
+  for (int i = tid; i < kSortWaves * kBins; i += 1024) (&sh.at[0][0])[i] = 0;
+  __syncthreads();
+  const uint32_t part = ((hi - lo + kSortWaves - 1) / kSortWaves + 63) / 64 * 64;
+  const uint32_t from = min(lo + wave * part, hi), to = min(from + part, hi);
+  for (uint32_t i = from + lane; i < to; i += 64) atomicAdd(&sh.at[wave][key_of(s, s.first, s.keys, i) >> s.shift & mask], 1u);
+  __syncthreads();
+  bases(sh, [&](int d, uint32_t &mine, uint32_t &all) {
+    if (d > (int)mask) return;
+#pragma unroll 8
+    for (int b = 0; b < s.blocks; ++b) {
+      const uint32_t c = s.counts[b * kBins + d];
+      mine += b < (int)blockIdx.x ? c : 0;
+      all += c;
+    }
+  });
+  for (uint32_t i0 = from; i0 < to; i0 += 64) {
+    const uint32_t i = i0 + lane;
+    const bool on = i < to;
+    const uint32_t key = on ? key_of(s, s.first, s.keys, i) : 0, place = on && !s.first ? s.places[i] : i, digit = key >> s.shift & mask;
+    const unsigned long long same = equals(on, digit, s.bits);
+    if (on) {
+      const uint32_t to_ = sh.at[wave][digit] + __popcll(same & ((1ull << lane) - 1));
+      s.keys_out[to_] = key;
+      s.places_out[to_] = place;
+    }
+    wave_order();
+    if (on && same >> lane == 1) sh.at[wave][digit] += __popcll(same);   // (the digit's last lane)
+    wave_order();
+  }
 }
 
-// Few ids: one block makes all passes, the others clear.  `keys` and `places` are the memory between two passes; the last one ends in the outputs.
-__global__ __launch_bounds__(1024) void embed_sort_few_kernel(SortArgs s, int passes, uint32_t *keys_between, uint32_t *places_between) {
-  if (blockIdx.x > 0) {
-    clear_ends(s.ends, s.V, blockIdx.x - 1, gridDim.x - 1);
-    return;
-  }
+// Few ids: one block makes all passes, its pairs in registers while a pass counts, in LDS in between, and says where each token's places begin and end.
+__global__ __launch_bounds__(1024) void embed_sort_few_kernel(SortArgs s, int passes) {
   __shared__ SortShared sh;
-  const uint32_t *keys = nullptr, *places = nullptr;
+  __shared__ uint2 pairs[kFew];
+  constexpr int M = kFew / 1024;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const uint32_t mask = (1u << s.bits) - 1, part = ((s.N + kSortWaves - 1) / kSortWaves + 63) / 64 * 64;
+  const uint32_t from = min(wave * part, s.N), to = min(from + part, s.N);
+  uint32_t key[M], place[M], at[M];
+#pragma unroll
+  for (int m = 0; m < M; ++m) {
+    place[m] = from + m * 64 + lane;
+    key[m] = place[m] < to ? key_of(s, true, nullptr, place[m]) : 0;
+  }
   for (int p = 0; p < passes; ++p) {
-    const bool out = (passes - 1 - p) % 2 == 0;
-    uint32_t *ko = out ? s.keys_out : keys_between, *po = out ? s.places_out : places_between;
-    sort_pass(s, sh, p == 0, keys, places, ko, po, 0, s.N, p * s.bits, nullptr, 0, 1);
-    __threadfence_block();
+    const int shift = p * s.bits;
+    for (int i = tid; i < kSortWaves * kBins; i += 1024) (&sh.at[0][0])[i] = 0;
     __syncthreads();
-    keys = ko;
-    places = po;
+    // where a pair goes among the wave's own of its digit; behind that the digit's number in the wave
+#pragma unroll
+    for (int m = 0; m < M; ++m) {
+      if (from + m * 64 >= to) break;
+      const bool on = from + m * 64 + lane < to;
+      const uint32_t digit = key[m] >> shift & mask;
+      const unsigned long long same = equals(on, digit, s.bits);
+      at[m] = on ? sh.at[wave][digit] + __popcll(same & ((1ull << lane) - 1)) : 0;
+      wave_order();
+      if (on && same >> lane == 1) sh.at[wave][digit] += __popcll(same);
+      wave_order();
+    }
+    __syncthreads();
+    bases(sh, [&](int d, uint32_t &mine, uint32_t &all) {
+      mine = all = 0;
+#pragma unroll
+      for (int w = 0; w < kSortWaves; ++w) all += sh.at[w][d];
+    });
+#pragma unroll
+    for (int m = 0; m < M; ++m)
+      if (from + m * 64 + lane < to) pairs[sh.at[wave][key[m] >> shift & mask] + at[m]] = make_uint2(key[m], place[m]);
+    __syncthreads();
+#pragma unroll
+    for (int m = 0; m < M; ++m) {
+      const uint32_t i = from + m * 64 + lane;
+      if (i < to) {
+        key[m] = pairs[i].x;
+        place[m] = pairs[i].y;
+      }
+    }
+  }
+#pragma unroll
+  for (int m = 0; m < M; ++m) {
+    const uint32_t i = from + m * 64 + lane;
+    if (i < to) {
+      s.keys_out[i] = key[m];
+      s.places_out[i] = place[m];
+      if (key[m] < s.V) {
+        if (i == 0 || pairs[i - 1].x != key[m]) s.starts[key[m]] = i;
+        if (i == s.N - 1 || pairs[i + 1].x != key[m]) s.ends[key[m]] = i + 1;
+      }
+    }
   }
 }
 
 // ---- the sums -----------------------------------------------------------------------------------------------------
 constexpr int kPiece = 64;           // places of a piece: tokens with more of them than that are summed by pieces
-constexpr int kTogether = 8;         // rows in flight
+constexpr int kTogether = 16;        // rows in flight
 
 struct SumArgs {
   const uint32_t *keys, *places;
-  uint32_t *starts, *ends;           // (V): a token's places in the sorted list; an end of 0 where it has none
+  uint32_t *starts, *ends;           // (V): a token's places in the sorted list, anything where it has none
   const void *dout;
   float *dtable, *partial;           // (pieces, 2, pitch): of a piece's first and of its last token, where they stand often
   int64_t dp, tp, pitch, V, D, chunks, pieces;
   float scale;
   uint32_t N;
-  int accumulate;
+  int accumulate, rows;              // rows of the table for a wave
 };
 
 __global__ __launch_bounds__(256) void embed_ranges_kernel(SumArgs s) {
@@ -198,31 +250,50 @@ __global__ __launch_bounds__(256) void embed_ranges_kernel(SumArgs s) {
   if (i == s.N - 1 || s.keys[i + 1] != k) s.ends[k] = i + 1;
 }
 
-// The sum of the rows at places [lo, hi) in a lane's columns, in their order.
+template <typename T, int E, int M, typename F>
+__device__ __forceinline__ void add_rows(F row, int i, int n, int64_t at, float (&sum)[E]) {
+  Unit<T, E> u[M];
+#pragma unroll
+  for (int k = 0; k < M; ++k) u[k].load(row(min(i + k, n - 1)) + at);
+#pragma unroll
+  for (int k = 0; k < M; ++k)
+    if (i + k < n) {
+#pragma unroll
+      for (int e = 0; e < E; ++e) sum[e] += u[k].get(e);
+    }
+}
+
+// The sum of the rows at places [lo, hi), 64 of them at most, in a lane's columns, in their order.  Each lane fetches one place; from there on only
+// rows are waited for.
 template <typename T, int E>
 __device__ __forceinline__ void sum_rows(const SumArgs &s, uint32_t lo, uint32_t hi, int64_t d, float (&sum)[E]) {
-  const T *base = static_cast<const T *>(s.dout) + d;
+  const int n = __builtin_amdgcn_readfirstlane((int)(hi - lo));
+  const uint32_t place = s.places[min(lo + (threadIdx.x & 63), hi - 1)];
+  auto row = [&](int i) { return static_cast<const T *>(s.dout) + (int64_t)(uint32_t)__builtin_amdgcn_readlane((int)place, i) * s.dp; };
 #pragma unroll
   for (int e = 0; e < E; ++e) sum[e] = 0.0f;
-  if (d >= s.D) return;
-  if (d + E <= s.D) {
-    for (uint32_t i = lo; i < hi; i += kTogether) {
-      Unit<T, E> u[kTogether];
+  if (s.D >= E) {
+    const int64_t at = min(d, s.D - E);                      // (behind the last whole unit: the row's last E columns)
+    int i = 0;
+    for (; n - i > kTogether / 2; i += kTogether) add_rows<T, E, kTogether>(row, i, n, at, sum);
+    for (; i < n; i += kTogether / 4) add_rows<T, E, kTogether / 4>(row, i, n, at, sum);
+    const int off = (int)min(d - at, (int64_t)E);
+    if (__any(off > 0)) {
+      float moved[E];
 #pragma unroll
-      for (int k = 0; k < kTogether; ++k) u[k].load(base + (int64_t)s.places[min(i + k, hi - 1)] * s.dp);
+      for (int e = 0; e < E; ++e) {
+        moved[e] = 0.0f;
 #pragma unroll
-      for (int k = 0; k < kTogether; ++k)
-        if (i + k < hi) {
+        for (int f = e; f < E; ++f) moved[e] = f == e + off ? sum[f] : moved[e];
+      }
 #pragma unroll
-          for (int e = 0; e < E; ++e) sum[e] += u[k].get(e);
-        }
+      for (int e = 0; e < E; ++e) sum[e] = moved[e];
     }
   } else {
-    for (uint32_t i = lo; i < hi; ++i) {
-      const T *row = base + (int64_t)s.places[i] * s.dp;
+    for (int i = 0; i < n; ++i) {
+      const T *r = row(i);
 #pragma unroll
-      for (int e = 0; e < E; ++e)
-        if (d + e < s.D) sum[e] += Elem<T>::load(row + e);
+      for (int e = 0; e < E; ++e) sum[e] += d + e < s.D ? Elem<T>::load(r + d + e) : 0.0f;
     }
   }
 }
@@ -243,9 +314,10 @@ __device__ __forceinline__ void write_row(const SumArgs &s, int64_t v, int64_t d
   }
 }
 
+// of a token that is in the list
 __device__ __forceinline__ bool often(const SumArgs &s, uint32_t v) { return v < s.V && s.ends[v] - s.starts[v] > kPiece; }
 
-// A wave for each (piece, chunk of columns), then for each (row of the table, chunk).
+// A wave for each (piece, chunk of columns), then for every few rows of the table and each chunk.
 template <typename T>
 __global__ __launch_bounds__(256) void embed_sum_kernel(SumArgs s) {
   constexpr int E = unit_elements<T>();
@@ -269,60 +341,77 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(SumArgs s) {
     return;
   }
   job -= s.pieces * s.chunks;
-  const int64_t v = job / s.chunks, d = ((job - v * s.chunks) * 64 + lane) * E;
-  if (v >= s.V || d >= s.D) return;
-  const uint32_t hi = s.ends[v];
-  if (hi == 0) {
-    if (s.accumulate) return;
-#pragma unroll
-    for (int e = 0; e < E; ++e) sum[e] = 0.0f;
-  } else {
-    const uint32_t lo = s.starts[v];
-    if (hi - lo > kPiece) return;
-    sum_rows<T, E>(s, lo, hi, d, sum);
+  const int64_t rows = job / s.chunks, v0 = rows * s.rows, d = ((job - rows * s.chunks) * 64 + lane) * E;
+  if (v0 >= s.V) return;
+  const int n = (int)min((int64_t)s.rows, s.V - v0);
+  // A token is in the list where the list says so: at the place that is noted for it, whatever an earlier call may have left there.
+  uint32_t lo = 0, count = 0;
+  if (lane < n) {
+    lo = s.starts[v0 + lane];
+    if (lo < s.N && s.keys[lo] == v0 + lane) count = s.ends[v0 + lane] - lo;
   }
-  write_row<E>(s, v, d, sum);
+  for (int r = 0; r < n; ++r) {
+    const uint32_t from = __builtin_amdgcn_readlane(lo, r), c = __builtin_amdgcn_readlane(count, r);
+    if (c > kPiece || (c == 0 && s.accumulate)) continue;
+    if (c > 0) {
+      sum_rows<T, E>(s, from, from + c, d, sum);
+    } else {
+#pragma unroll
+      for (int e = 0; e < E; ++e) sum[e] = 0.0f;
+    }
+    if (d < s.D) write_row<E>(s, v0 + r, d, sum);
+  }
 }
 
-// The pieces of the token that stands often and begins in the block's piece, if there is one: sixteen waves take neighbouring shares of them.
+// A block looks at kLooked pieces for tokens that stand often and begin in one of them, and adds up their pieces: its waves take neighbouring shares.
+constexpr int kLooked = 4;
+
 template <int E>
-__global__ __launch_bounds__(1024) void embed_join_kernel(SumArgs s) {
+__global__ __launch_bounds__(64 * kSortWaves) void embed_join_kernel(SumArgs s) {
   __shared__ float parts[kSortWaves][E][64];
-  const int64_t job = block_number(), piece = job / s.chunks;
-  if (piece >= s.pieces) return;
-  const uint32_t lo = (uint32_t)piece * kPiece, hi = min(lo + kPiece, s.N), v = s.keys[hi - 1];
-  if (!often(s, v) || s.starts[v] < lo) return;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int64_t d = ((job - piece * s.chunks) * 64 + lane) * E;
-  const int64_t last = (s.ends[v] - 1) / kPiece, share = (last - piece + kSortWaves) / kSortWaves;
-  const int64_t from = piece + wave * share, to = min(from + share, last + 1);
-  float sum[E];
-#pragma unroll
-  for (int e = 0; e < E; ++e) sum[e] = 0.0f;
-  if (d < s.D) {
-    for (int64_t i = from; i < to; i += kTogether) {
-      Unit<float, E> u[kTogether];
-#pragma unroll
-      for (int k = 0; k < kTogether; ++k) {
-        const int64_t p = min(i + k, to - 1);
-        u[k].load(s.partial + (p * 2 + (p == piece && s.starts[v] != lo)) * s.pitch + d);   // (of the first piece the last token, of the others the first)
-      }
-#pragma unroll
-      for (int k = 0; k < kTogether; ++k)
-        if (i + k < to) {
-#pragma unroll
-          for (int e = 0; e < E; ++e) sum[e] += u[k].get(e);
-        }
-    }
+  const int64_t job = block_number(), group = job / s.chunks, d = ((job - group * s.chunks) * 64 + lane) * E;
+  bool found = false;
+  if (lane < kLooked && group * kLooked + lane < s.pieces) {
+    const uint32_t lo = (uint32_t)(group * kLooked + lane) * kPiece, hi = min(lo + kPiece, s.N), v = s.keys[hi - 1];
+    found = often(s, v) && s.starts[v] >= lo;
   }
+  for (unsigned long long left = __ballot(found); left; left &= left - 1) {
+    const int64_t piece = group * kLooked + __builtin_ctzll(left);
+    const uint32_t lo = (uint32_t)piece * kPiece, v = s.keys[min(lo + kPiece, s.N) - 1];
+    const int64_t last = (s.ends[v] - 1) / kPiece, share = (last - piece + kSortWaves) / kSortWaves;
+    const int64_t from = piece + wave * share, to = min(from + share, last + 1);
+    const int side = s.starts[v] != lo;                      // of its first piece the token is the last one, of the others the first
+    float sum[E];
 #pragma unroll
-  for (int e = 0; e < E; ++e) parts[wave][e][lane] = sum[e];
-  __syncthreads();
-  if (wave > 0 || d >= s.D) return;
+    for (int e = 0; e < E; ++e) sum[e] = 0.0f;
+    if (d < s.D) {
+      for (int64_t i = from; i < to; i += 8) {
+        Unit<float, E> u[8];
 #pragma unroll
-  for (int e = 0; e < E; ++e)
-    for (int w = 1; w < kSortWaves; ++w) sum[e] += parts[w][e][lane];
-  write_row<E>(s, v, d, sum);
+        for (int k = 0; k < 8; ++k) {
+          const int64_t p = min(i + k, to - 1);
+          u[k].load(s.partial + (p * 2 + (p == piece ? side : 0)) * s.pitch + d);
+        }
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+          if (i + k < to) {
+#pragma unroll
+            for (int e = 0; e < E; ++e) sum[e] += u[k].get(e);
+          }
+      }
+    }
+#pragma unroll
+    for (int e = 0; e < E; ++e) parts[wave][e][lane] = sum[e];
+    __syncthreads();
+    if (wave == 0 && d < s.D) {
+#pragma unroll
+      for (int e = 0; e < E; ++e)
+        for (int w = 1; w < kSortWaves; ++w) sum[e] += parts[w][e][lane];
+      write_row<E>(s, v, d, sum);
+    }
+    __syncthreads();
+  }
 }
 
 // The workspace, in the order in which its parts lie.
@@ -344,15 +433,14 @@ struct Layout {
     auto put = [&](size_t n) { const size_t here = at; at += (n + 255) / 256 * 256; return here; };
     keys = put(4 * (size_t)N);
     places = put(4 * (size_t)N);
-    between = put(passes > 1 ? 4 * (size_t)N : 0);
-    places_between = put(passes > 1 ? 4 * (size_t)N : 0);
+    between = put(blocks > 1 && passes > 1 ? 4 * (size_t)N : 0);
+    places_between = put(blocks > 1 && passes > 1 ? 4 * (size_t)N : 0);
     counts = put(blocks > 1 ? 4 * (size_t)blocks * kBins : 0);
     starts = put(4 * (size_t)V);
     ends = put(4 * (size_t)V);
     partial = put(8 * (size_t)pieces * pitch);
     bytes = at;
   }
-  static constexpr int64_t kFew = 8192;
 };
 
 chn_status ids_of(const chn_array *ids, int64_t *N, int64_t *stride) {
@@ -429,12 +517,10 @@ chn_status chn_embed_sorted_bwd(const chn_array *ids, const chn_array *dout, dou
   SortArgs o = {};
   o.ids = ids->data; o.stride = is; o.id64 = ids->dtype == CHN_I64;
   o.V = V; o.N = (uint32_t)N; o.share = z.share; o.bits = z.bits; o.blocks = z.blocks;
-  o.counts = words(z.counts); o.ends = words(z.ends);
+  o.counts = words(z.counts); o.starts = words(z.starts); o.ends = words(z.ends);
   o.keys_out = words(z.keys); o.places_out = words(z.places);
   if (z.blocks == 1) {
-    const int64_t clearing = (V + 4095) / 4096;
-    hipLaunchKernelGGL(embed_sort_few_kernel, dim3(1 + (unsigned)(clearing < 256 ? clearing : 256)), dim3(1024), 0, st, o, z.passes, words(z.between),
-                       words(z.places_between));
+    if (N > 0) hipLaunchKernelGGL(embed_sort_few_kernel, dim3(1), dim3(1024), 0, st, o, z.passes);
     CHN_TRY(check_launch("embed_sorted_bwd"));
   } else {
     for (int p = 0; p < z.passes; ++p) {
@@ -455,17 +541,19 @@ chn_status chn_embed_sorted_bwd(const chn_array *ids, const chn_array *dout, dou
   s.dout = dout->data; s.dtable = static_cast<float *>(dtable->data); s.partial = reinterpret_cast<float *>(w + z.partial);
   s.dp = dp; s.tp = tp; s.pitch = z.pitch; s.V = V; s.D = D; s.chunks = (D + 64 * E - 1) / (64 * E); s.pieces = z.pieces;
   s.scale = (float)scale; s.N = (uint32_t)N; s.accumulate = accumulate;
-  if (N > 0) {
+  if (z.blocks > 1) {
     hipLaunchKernelGGL(embed_ranges_kernel, dim3((unsigned)((N + 255) / 256)), dim3(256), 0, st, s);
     CHN_TRY(check_launch("embed_sorted_bwd"));
   }
-  const dim3 grid = grid_of(((z.pieces + V) * s.chunks + 3) / 4);
+  const int64_t each = V * s.chunks / 16384;                 // (fewer waves than that, and the chip is not full)
+  s.rows = (int)(each < 1 ? 1 : each > 16 ? 16 : each);
+  const dim3 grid = grid_of(((z.pieces + (V + s.rows - 1) / s.rows) * s.chunks + 3) / 4);
   if (dout->dtype == CHN_F32) hipLaunchKernelGGL((embed_sum_kernel<float>), grid, dim3(256), 0, st, s);
   else hipLaunchKernelGGL((embed_sum_kernel<bf16_raw>), grid, dim3(256), 0, st, s);
   CHN_TRY(check_launch("embed_sorted_bwd"));
   if (N <= kPiece) return CHN_OK;                            // (no token stands more often)
-  if (dout->dtype == CHN_F32) hipLaunchKernelGGL((embed_join_kernel<4>), grid_of(z.pieces * s.chunks), dim3(1024), 0, st, s);
-  else hipLaunchKernelGGL((embed_join_kernel<8>), grid_of(z.pieces * s.chunks), dim3(1024), 0, st, s);
+  if (dout->dtype == CHN_F32) hipLaunchKernelGGL((embed_join_kernel<4>), grid_of((z.pieces + kLooked - 1) / kLooked * s.chunks), dim3(64 * kSortWaves), 0, st, s);
+  else hipLaunchKernelGGL((embed_join_kernel<8>), grid_of((z.pieces + kLooked - 1) / kLooked * s.chunks), dim3(64 * kSortWaves), 0, st, s);
   return check_launch("embed_sorted_bwd");
 }
 
