@@ -33,7 +33,7 @@ __global__ __launch_bounds__(256) void embed_scaled_kernel(const TI *table, int6
 #pragma unroll
         for (int e = 0; e < E; ++e) o.set(e, u.get(e) * scale);
       }
-      o.store(dst + d);
+      o.store_nt(dst + d);
     } else {
       for (int64_t e = d; e < D; ++e) Elem<TO>::store(dst + e, none ? 0.0f : Elem<TI>::load(src + e) * scale);
     }
@@ -57,7 +57,28 @@ struct SortArgs {
   int64_t stride, V;
   uint32_t N, share;                 // pairs of a block
   int id64, shift, bits, blocks, first;
+  float *dtable;                     // of this launch's blocks behind the sort's: rows [row, row_end) of the table become zeros
+  int64_t tp, D, row, row_end;
 };
+
+// Sorting keeps a few blocks busy; the others meanwhile clear a table most rows of which will stay empty.
+__device__ __forceinline__ bool fills(const SortArgs &s) {
+  if ((int)blockIdx.x < s.blocks) return false;
+  const int lane = threadIdx.x & 63;
+  const int64_t waves = (int64_t)(gridDim.x - s.blocks) * kSortWaves;
+  const chn_u32x4 none = {0, 0, 0, 0};
+  for (int64_t v = s.row + ((int64_t)blockIdx.x - s.blocks) * kSortWaves + (threadIdx.x >> 6); v < s.row_end; v += waves) {
+    float *p = s.dtable + v * s.tp;
+    for (int64_t d = lane * 4; d < s.D; d += 256) {
+      if (d + 4 <= s.D) {
+        __builtin_nontemporal_store(none, reinterpret_cast<chn_u32x4_any *>(p + d));
+      } else {
+        for (int64_t e = d; e < s.D; ++e) p[e] = 0.0f;
+      }
+    }
+  }
+  return true;
+}
 
 __device__ __forceinline__ uint32_t key_of(const SortArgs &s, bool first, const uint32_t *keys, uint32_t i) {
   if (!first) return keys[i];
@@ -67,6 +88,7 @@ __device__ __forceinline__ uint32_t key_of(const SortArgs &s, bool first, const 
 // How often a block's share has each digit.
 __global__ __launch_bounds__(1024) void embed_count_kernel(SortArgs s) {
   __shared__ uint32_t count[kBins];
+  if (fills(s)) return;
   if (threadIdx.x < kBins) count[threadIdx.x] = 0;
   __syncthreads();
   const uint32_t lo = blockIdx.x * s.share, hi = min(lo + s.share, s.N), mask = (1u << s.bits) - 1;
@@ -129,6 +151,7 @@ __device__ __forceinline__ void bases(SortShared &sh, F count) {
 // One pass over the block's share, split over the waves.
 __global__ __launch_bounds__(1024) void embed_sort_kernel(SortArgs s) {
   __shared__ SortShared sh;
+  if (fills(s)) return;
   const uint32_t lo = min(blockIdx.x * s.share, s.N), hi = min(lo + s.share, s.N);
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const uint32_t mask = (1u << s.bits) - 1;
@@ -238,7 +261,7 @@ struct SumArgs {
   int64_t dp, tp, pitch, V, D, chunks, pieces;
   float scale;
   uint32_t N;
-  int accumulate, rows;              // rows of the table for a wave
+  int accumulate, leave, rows;       // whether rows without a token stay as they are; rows of the table for a wave
 };
 
 __global__ __launch_bounds__(256) void embed_ranges_kernel(SumArgs s) {
@@ -306,11 +329,27 @@ __device__ __forceinline__ void write_row(const SumArgs &s, int64_t v, int64_t d
     if (s.accumulate) u.load(p);
 #pragma unroll
     for (int e = 0; e < E; ++e) u.set(e, s.accumulate ? fmaf(s.scale, sum[e], u.get(e)) : s.scale * sum[e]);
-    u.store(p);
+    u.store_nt(p);
   } else {
 #pragma unroll
     for (int e = 0; e < E; ++e)
       if (d + e < s.D) p[e] = s.accumulate ? fmaf(s.scale, sum[e], p[e]) : s.scale * sum[e];
+  }
+}
+
+// A chunk of a row of zeros, neighbouring lanes next to each other.
+template <int E>
+__device__ __forceinline__ void zero_row(const SumArgs &s, int64_t v, int64_t d0) {
+  float *p = s.dtable + v * s.tp;
+  const chn_u32x4 none = {0, 0, 0, 0};
+#pragma unroll
+  for (int j = 0; j < E / 4; ++j) {
+    const int64_t d = d0 + j * 256 + (threadIdx.x & 63) * 4;
+    if (d + 4 <= s.D) {
+      __builtin_nontemporal_store(none, reinterpret_cast<chn_u32x4_any *>(p + d));
+    } else {
+      for (int64_t e = d; e < s.D; ++e) p[e] = 0.0f;
+    }
   }
 }
 
@@ -327,10 +366,11 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(SumArgs s) {
   if (job < s.pieces * s.chunks) {
     const int64_t piece = job / s.chunks, d = ((job - piece * s.chunks) * 64 + lane) * E;
     const uint32_t lo = (uint32_t)piece * kPiece, hi = min(lo + kPiece, s.N), f = s.keys[lo], l = s.keys[hi - 1];
+    const uint32_t fv = f < s.V ? f : 0, lv = l < s.V ? l : 0;
+    const uint32_t f0 = s.starts[fv], f1 = s.ends[fv], l0 = s.starts[lv], l1 = s.ends[lv];
     for (int side = 0; side < 2; ++side) {
-      const uint32_t v = side ? l : f;
-      if ((side && l == f) || !often(s, v)) continue;
-      sum_rows<T, E>(s, side ? s.starts[v] : lo, side ? hi : min(hi, s.ends[v]), d, sum);
+      if (side ? l == f || l >= s.V || l1 - l0 <= kPiece : f >= s.V || f1 - f0 <= kPiece) continue;
+      sum_rows<T, E>(s, side ? l0 : lo, side ? hi : min(hi, f1), d, sum);
       if (d < s.D) {
         Unit<float, E> u;
 #pragma unroll
@@ -348,27 +388,27 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(SumArgs s) {
   uint32_t lo = 0, count = 0;
   if (lane < n) {
     lo = s.starts[v0 + lane];
-    if (lo < s.N && s.keys[lo] == v0 + lane) count = s.ends[v0 + lane] - lo;
+    const uint32_t end = s.ends[v0 + lane];
+    if (lo < s.N && s.keys[lo] == v0 + lane) count = end - lo;
   }
   for (int r = 0; r < n; ++r) {
     const uint32_t from = __builtin_amdgcn_readlane(lo, r), c = __builtin_amdgcn_readlane(count, r);
-    if (c > kPiece || (c == 0 && s.accumulate)) continue;
+    if (c > kPiece || (c == 0 && s.leave)) continue;
     if (c > 0) {
       sum_rows<T, E>(s, from, from + c, d, sum);
+      if (d < s.D) write_row<E>(s, v0 + r, d, sum);
     } else {
-#pragma unroll
-      for (int e = 0; e < E; ++e) sum[e] = 0.0f;
+      zero_row<E>(s, v0 + r, d - lane * E);
     }
-    if (d < s.D) write_row<E>(s, v0 + r, d, sum);
   }
 }
 
 // A block looks at kLooked pieces for tokens that stand often and begin in one of them, and adds up their pieces: its waves take neighbouring shares.
-constexpr int kLooked = 4;
+constexpr int kLooked = 4, kJoinWaves = 8;
 
 template <int E>
-__global__ __launch_bounds__(64 * kSortWaves) void embed_join_kernel(SumArgs s) {
-  __shared__ float parts[kSortWaves][E][64];
+__global__ __launch_bounds__(64 * kJoinWaves) void embed_join_kernel(SumArgs s) {
+  __shared__ float parts[kJoinWaves][E][64];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int64_t job = block_number(), group = job / s.chunks, d = ((job - group * s.chunks) * 64 + lane) * E;
   bool found = false;
@@ -379,7 +419,7 @@ __global__ __launch_bounds__(64 * kSortWaves) void embed_join_kernel(SumArgs s) 
   for (unsigned long long left = __ballot(found); left; left &= left - 1) {
     const int64_t piece = group * kLooked + __builtin_ctzll(left);
     const uint32_t lo = (uint32_t)piece * kPiece, v = s.keys[min(lo + kPiece, s.N) - 1];
-    const int64_t last = (s.ends[v] - 1) / kPiece, share = (last - piece + kSortWaves) / kSortWaves;
+    const int64_t last = (s.ends[v] - 1) / kPiece, share = (last - piece + kJoinWaves) / kJoinWaves;
     const int64_t from = piece + wave * share, to = min(from + share, last + 1);
     const int side = s.starts[v] != lo;                      // of its first piece the token is the last one, of the others the first
     float sum[E];
@@ -407,7 +447,7 @@ __global__ __launch_bounds__(64 * kSortWaves) void embed_join_kernel(SumArgs s) 
     if (wave == 0 && d < s.D) {
 #pragma unroll
       for (int e = 0; e < E; ++e)
-        for (int w = 1; w < kSortWaves; ++w) sum[e] += parts[w][e][lane];
+        for (int w = 1; w < kJoinWaves; ++w) sum[e] += parts[w][e][lane];
       write_row<E>(s, v, d, sum);
     }
     __syncthreads();
@@ -519,6 +559,8 @@ chn_status chn_embed_sorted_bwd(const chn_array *ids, const chn_array *dout, dou
   o.V = V; o.N = (uint32_t)N; o.share = z.share; o.bits = z.bits; o.blocks = z.blocks;
   o.counts = words(z.counts); o.starts = words(z.starts); o.ends = words(z.ends);
   o.keys_out = words(z.keys); o.places_out = words(z.places);
+  const bool filled = z.blocks > 1 && !accumulate && N <= V / 2;
+  o.dtable = static_cast<float *>(dtable->data); o.tp = tp; o.D = D;
   if (z.blocks == 1) {
     if (N > 0) hipLaunchKernelGGL(embed_sort_few_kernel, dim3(1), dim3(1024), 0, st, o, z.passes);
     CHN_TRY(check_launch("embed_sorted_bwd"));
@@ -529,10 +571,17 @@ chn_status chn_embed_sorted_bwd(const chn_array *ids, const chn_array *dout, dou
       o.shift = p * z.bits;
       o.keys = words(last ? z.between : z.keys); o.places = words(last ? z.places_between : z.places);
       o.keys_out = words(last ? z.keys : z.between); o.places_out = words(last ? z.places : z.places_between);
-      hipLaunchKernelGGL(embed_count_kernel, dim3(z.blocks), dim3(1024), 0, st, o);
-      CHN_TRY(check_launch("embed_sorted_bwd"));
-      hipLaunchKernelGGL(embed_sort_kernel, dim3(z.blocks), dim3(1024), 0, st, o);
-      CHN_TRY(check_launch("embed_sorted_bwd"));
+      for (int half = 0; half < 2; ++half) {
+        if (filled) {
+          const int64_t k = p * 2 + half, parts = z.passes * 2;
+          o.row = V * k / parts;
+          o.row_end = V * (k + 1) / parts;
+        }
+        const dim3 grid(z.blocks + (filled ? 512 : 0));
+        if (half == 0) hipLaunchKernelGGL(embed_count_kernel, grid, dim3(1024), 0, st, o);
+        else hipLaunchKernelGGL(embed_sort_kernel, grid, dim3(1024), 0, st, o);
+        CHN_TRY(check_launch("embed_sorted_bwd"));
+      }
     }
   }
   const int E = dout->dtype == CHN_F32 ? 4 : 8;
@@ -540,7 +589,7 @@ chn_status chn_embed_sorted_bwd(const chn_array *ids, const chn_array *dout, dou
   s.keys = words(z.keys); s.places = words(z.places); s.starts = words(z.starts); s.ends = words(z.ends);
   s.dout = dout->data; s.dtable = static_cast<float *>(dtable->data); s.partial = reinterpret_cast<float *>(w + z.partial);
   s.dp = dp; s.tp = tp; s.pitch = z.pitch; s.V = V; s.D = D; s.chunks = (D + 64 * E - 1) / (64 * E); s.pieces = z.pieces;
-  s.scale = (float)scale; s.N = (uint32_t)N; s.accumulate = accumulate;
+  s.scale = (float)scale; s.N = (uint32_t)N; s.accumulate = accumulate; s.leave = accumulate || filled;
   if (z.blocks > 1) {
     hipLaunchKernelGGL(embed_ranges_kernel, dim3((unsigned)((N + 255) / 256)), dim3(256), 0, st, s);
     CHN_TRY(check_launch("embed_sorted_bwd"));
@@ -552,8 +601,8 @@ chn_status chn_embed_sorted_bwd(const chn_array *ids, const chn_array *dout, dou
   else hipLaunchKernelGGL((embed_sum_kernel<bf16_raw>), grid, dim3(256), 0, st, s);
   CHN_TRY(check_launch("embed_sorted_bwd"));
   if (N <= kPiece) return CHN_OK;                            // (no token stands more often)
-  if (dout->dtype == CHN_F32) hipLaunchKernelGGL((embed_join_kernel<4>), grid_of((z.pieces + kLooked - 1) / kLooked * s.chunks), dim3(64 * kSortWaves), 0, st, s);
-  else hipLaunchKernelGGL((embed_join_kernel<8>), grid_of((z.pieces + kLooked - 1) / kLooked * s.chunks), dim3(64 * kSortWaves), 0, st, s);
+  if (dout->dtype == CHN_F32) hipLaunchKernelGGL((embed_join_kernel<4>), grid_of((z.pieces + kLooked - 1) / kLooked * s.chunks), dim3(64 * kJoinWaves), 0, st, s);
+  else hipLaunchKernelGGL((embed_join_kernel<8>), grid_of((z.pieces + kLooked - 1) / kLooked * s.chunks), dim3(64 * kJoinWaves), 0, st, s);
   return check_launch("embed_sorted_bwd");
 }
 
