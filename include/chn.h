@@ -503,7 +503,7 @@ chn_status chn_sample(const chn_array *logits, const chn_array *u, const chn_arr
 /* ---- logits before a token is drawn ----------------------------------------------------------------------------
  * out = the logits (N,V), F32 or BF16, row-major with any pitch, with what a row's text, its caller and its grammar say about them (chn_sample
  * draws from the result).  In a row, z the logit of token i:
- *   tokens (N,L) I32 or I64, any pitch: the row's text so far, of which the first lengths[n] count (lengths, prompt: (N,) I32 or I64; NULL: all L,
+ *   tokens (N,L) I32 or I64, any strides: the row's text so far, of which the first lengths[n] count (lengths, prompt: (N,) I32 or I64; NULL: all L,
  *   and no prompt), the first prompt[n] of them being the prompt.  With c the number of times i stands behind the prompt:
  *     repetition (N,) F32: z / repetition where z > 0, else z * repetition, if i is anywhere in the text;
  *     frequency (N,) F32:  then z - frequency * c;      presence (N,) F32: then z - presence, if c > 0;

@@ -20,7 +20,7 @@ struct AdjustArgs {
   const void *tokens, *lengths, *prompt, *bias_ids;
   const float *repetition, *frequency, *presence, *bias;
   const int32_t *allowed;
-  int64_t N, V, L, M, pz, po, pt, pi, pb, pa;      // sizes, pitches
+  int64_t N, V, L, M, pz, po, pt, ts, pi, pb, pa;  // sizes, pitches, the step from token to token
   int64_t sl, sp, sr, sf, ss;                   // strides of lengths, prompt, repetition, frequency, presence
   int64_t tiles, tile;                          // pieces of a row, tokens of a piece
   int len64, prompt64;
@@ -56,16 +56,16 @@ __device__ __forceinline__ uint32_t place(int64_t id, int64_t v0) {
 // f(i, values[i]) for the indexes [0, n) that belong to the thread, eight loads in flight.  `v` holds the first eight already.
 constexpr int kAhead = 8;
 template <typename ID>
-__device__ __forceinline__ void ahead(const ID *values, int n, ID (&v)[kAhead], int from) {
+__device__ __forceinline__ void ahead(const ID *values, int64_t stride, int n, ID (&v)[kAhead], int from) {
   const int step = blockDim.x;
 #pragma unroll
-  for (int k = 0; k < kAhead; ++k) v[k] = values[min(from + k * step, n - 1)];
+  for (int k = 0; k < kAhead; ++k) v[k] = values[min(from + k * step, n - 1) * stride];
 }
 template <typename ID, typename F>
-__device__ __forceinline__ void each(const ID *values, int n, ID (&v)[kAhead], F f) {
+__device__ __forceinline__ void each(const ID *values, int64_t stride, int n, ID (&v)[kAhead], F f) {
   const int step = blockDim.x;
   for (int i = threadIdx.x; i < n; i += kAhead * step) {
-    if (i >= kAhead * step) ahead(values, n, v, i);
+    if (i >= kAhead * step) ahead(values, stride, n, v, i);
 #pragma unroll
     for (int k = 0; k < kAhead; ++k)
       if (i + k * step < n) f(i + k * step, v[k]);
@@ -108,7 +108,7 @@ __global__ __launch_bounds__(kThreads, 8) void adjust_kernel(AdjustArgs a) {
     ID first[kAhead];
     int end = 0, mine = 0;
     if (a.tokens) {
-      ahead(tokens, (int)a.L, first, threadIdx.x);
+      ahead(tokens, a.ts, (int)a.L, first, threadIdx.x);
       end = a.lengths ? cut(a.lengths, a.len64, n * a.sl, (int)a.L) : (int)a.L;
       mine = a.prompt ? cut(a.prompt, a.prompt64, n * a.sp, (int)a.L) : 0;
     }
@@ -116,7 +116,7 @@ __global__ __launch_bounds__(kThreads, 8) void adjust_kernel(AdjustArgs a) {
     for (int i = (int)threadIdx.x * 4; i < len; i += (int)blockDim.x * 4) *reinterpret_cast<uint4 *>(words + i) = make_uint4(0, 0, 0, 0);
     if (threadIdx.x == 0) twice = 0;
     __syncthreads();
-    each(tokens, end, first, [&](int i, ID id) {
+    each(tokens, a.ts, end, first, [&](int i, ID id) {
       const uint32_t at = place(id, v0);
       if (at < (uint32_t)len) {
         if (i >= mine) atomicAdd(&words[at], 1u);
@@ -229,13 +229,14 @@ chn_status row_param(const chn_array *p, const char *name, bool index, int64_t N
   return CHN_OK;
 }
 
-// A list for each row: (N,n), unit inner stride, any pitch, 0 for one list for all.
-chn_status row_list(const chn_array *p, const char *name, int64_t N, int64_t *n, int64_t *pitch) {
+// A list for each row: (N,n), any pitch, 0 for one list for all; unit inner stride, or any where `step` takes it.
+chn_status row_list(const chn_array *p, const char *name, int64_t N, int64_t *n, int64_t *pitch, int64_t *step = nullptr) {
   CHN_TRY(validate(p, name, false));
   if (p->ndim != 2) return fail(CHN_ERR_NDIM, "logits_adjust: %s must have 2 dimensions, got %d", name, p->ndim);
   if (p->shape[0] != N) return fail(CHN_ERR_SHAPE, "logits_adjust: %s must have %lld rows", name, (long long)N);
   const int isz = dtype_size(p->dtype);
-  if (p->shape[1] > 1 && p->strides[1] != isz) return fail(CHN_ERR_STRIDE, "logits_adjust: the last axis of %s must have unit stride", name);
+  if (step) *step = p->shape[1] > 1 ? p->strides[1] / isz : 0;
+  else if (p->shape[1] > 1 && p->strides[1] != isz) return fail(CHN_ERR_STRIDE, "logits_adjust: the last axis of %s must have unit stride", name);
   *n = p->shape[1];
   *pitch = N > 1 ? p->strides[0] / isz : 0;
   return CHN_OK;
@@ -268,7 +269,7 @@ chn_status chn_logits_adjust(const chn_array *logits, const chn_array *tokens, c
   CHN_TRY(row_param(presence, "presence", false, N, &a.ss));
   bool id64 = true;
   if (tokens) {
-    CHN_TRY(row_list(tokens, "tokens", N, &a.L, &a.pt));
+    CHN_TRY(row_list(tokens, "tokens", N, &a.L, &a.pt, &a.ts));
     if (!is_index(tokens->dtype)) return fail(CHN_ERR_DTYPE, "logits_adjust: tokens must be I32 or I64");
     if (a.L >= 1 << 30) return fail(CHN_ERR_SHAPE, "logits_adjust: lists of %lld tokens", (long long)a.L);
     id64 = tokens->dtype == CHN_I64;

@@ -13,7 +13,7 @@ __device__ __forceinline__ int64_t id_at(const L *ids, int64_t n, int64_t stride
 // A wave for each row, in units at whatever address the rows have; what is left of a row behind its last whole unit goes element by element.
 template <typename TI, typename TO, typename L>
 __global__ __launch_bounds__(256) void embed_scaled_kernel(const TI *table, int64_t tp, int64_t V, const L *ids, int64_t is, int64_t N, int64_t D, float scale,
-                                                           TO *out, int64_t op) {
+                                                           TO *out, int64_t op, bool past) {
   constexpr int E = unit_elements<TI, TO>();
   const int lane = threadIdx.x & 63;
   const int64_t n = block_number() * 4 + (threadIdx.x >> 6);
@@ -33,7 +33,8 @@ __global__ __launch_bounds__(256) void embed_scaled_kernel(const TI *table, int6
 #pragma unroll
         for (int e = 0; e < E; ++e) o.set(e, u.get(e) * scale);
       }
-      o.store_nt(dst + d);
+      if (past) o.store_nt(dst + d);
+      else o.store(dst + d);
     } else {
       for (int64_t e = d; e < D; ++e) Elem<TO>::store(dst + e, none ? 0.0f : Elem<TI>::load(src + e) * scale);
     }
@@ -512,14 +513,16 @@ chn_status chn_embed_scaled_fwd(const chn_array *table, const chn_array *ids, do
   if (N == 0 || D == 0) return CHN_OK;
   const dim3 grid = grid_of((N + 3) / 4);
   hipStream_t st = as_stream(stream);
+  const int64_t osz = dtype_size(out->dtype);
+  const bool past = D * osz % 128 == 0 && op * osz % 128 == 0 && reinterpret_cast<uintptr_t>(out->data) % 128 == 0;
 #define CHN_GO(TI, TO)                                                                                                                               \
   do {                                                                                                                                               \
     if (ids->dtype == CHN_I32)                                                                                                                       \
       hipLaunchKernelGGL((embed_scaled_kernel<TI, TO, int32_t>), grid, dim3(256), 0, st, static_cast<const TI *>(table->data), tp, V,                \
-                         static_cast<const int32_t *>(ids->data), is, N, D, (float)scale, static_cast<TO *>(out->data), op);                         \
+                         static_cast<const int32_t *>(ids->data), is, N, D, (float)scale, static_cast<TO *>(out->data), op, past);                   \
     else                                                                                                                                             \
       hipLaunchKernelGGL((embed_scaled_kernel<TI, TO, int64_t>), grid, dim3(256), 0, st, static_cast<const TI *>(table->data), tp, V,                \
-                         static_cast<const int64_t *>(ids->data), is, N, D, (float)scale, static_cast<TO *>(out->data), op);                         \
+                         static_cast<const int64_t *>(ids->data), is, N, D, (float)scale, static_cast<TO *>(out->data), op, past);                   \
   } while (0)
   if (table->dtype == CHN_F32) { if (out->dtype == CHN_F32) CHN_GO(float, float); else CHN_GO(float, bf16_raw); }
   else { if (out->dtype == CHN_F32) CHN_GO(bf16_raw, float); else CHN_GO(bf16_raw, bf16_raw); }

@@ -10,7 +10,8 @@ namespace {
 constexpr int kSteps = CHN_SCAN_STRIDE;        // steps of a wave
 constexpr int kWaves = 8;                      // waves of a block, at most
 constexpr int kPiece = kSteps * kWaves;        // steps of a block
-constexpr int kGroup = 2 * kWaves;             // pieces of a group
+constexpr int kEach = 2;                       // pieces before its own that a wave joins
+constexpr int kGroup = kEach * kWaves;         // pieces of a group
 constexpr int kPolls = 1 << 18;                // (a large part of a second: what is waited for is under way already)
 
 struct ScanArgs {
@@ -61,7 +62,7 @@ template <> struct Few<float, 1> {
   float r;
   __device__ __forceinline__ void load(const float *p) { r = *p; }
   __device__ __forceinline__ float get(int) const { return r; }
-  static __device__ __forceinline__ void store(float *p, Vals<1> v) { *p = v[0]; }
+  static __device__ __forceinline__ void store(float *p, Vals<1> v) { __builtin_nontemporal_store(v[0], p); }
 };
 template <> struct Few<bf16_raw, 1> {
   uint32_t r;
@@ -76,7 +77,7 @@ template <> struct Few<bf16_raw, 2> {
   __device__ __forceinline__ void load(const bf16_raw *p) { r = *reinterpret_cast<const u32_any *>(p); }
   __device__ __forceinline__ float get(int i) const { return __uint_as_float(i ? r & 0xffff0000u : r << 16); }
   static __device__ __forceinline__ void store(bf16_raw *p, Vals<2> v) {
-    *reinterpret_cast<u32_any *>(p) = (uint32_t)f32_to_bf16(v[0]) | (uint32_t)f32_to_bf16(v[1]) << 16;
+    __builtin_nontemporal_store((uint32_t)f32_to_bf16(v[0]) | (uint32_t)f32_to_bf16(v[1]) << 16, reinterpret_cast<u32_any *>(p));
   }
 };
 template <> struct Few<float, 2> {
@@ -166,30 +167,34 @@ __device__ __forceinline__ void begin_with(const ScanArgs &s, Shared<V> &sh, con
         if (at.owns(v)) __hip_atomic_store(s.effects + piece * row + column + v, together(e.x, e.y), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
       }
     }
-    if (2 * wave < before) {
-      const int64_t p0 = (group * kGroup + 2 * wave) * row + column, p1 = 2 * wave + 1 < before ? p0 + row : p0;
-      unsigned long long e0[V], e1[V];
+    if (kEach * wave < before) {
+      const int n = min(before - kEach * wave, kEach);
+      const int64_t p = (group * kGroup + kEach * wave) * row + column;
+      unsigned long long e[kEach][V];
       bool missing = true;
       for (int polls = 0; polls < kPolls && missing; ++polls) {
         missing = false;
 #pragma unroll
-        for (int v = 0; v < V; ++v) {
-          e0[v] = __hip_atomic_load(s.effects + p0 + v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-          e1[v] = __hip_atomic_load(s.effects + p1 + v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        }
+        for (int k = 0; k < kEach; ++k)
 #pragma unroll
-        for (int v = 0; v < V; ++v) missing |= e0[v] == ~0ull || e1[v] == ~0ull;
+          for (int v = 0; v < V; ++v) e[k][v] = __hip_atomic_load(s.effects + p + min(k, n - 1) * row + v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+#pragma unroll
+        for (int k = 0; k < kEach; ++k)
+#pragma unroll
+          for (int v = 0; v < V; ++v) missing |= e[k][v] == ~0ull;
         missing = __any(missing);
       }
 #pragma unroll
       for (int v = 0; v < V; ++v) {
         // (one that never came is NaN, all of its bits set)
-        float2 e = make_float2(__uint_as_float((unsigned)e0[v]), __uint_as_float((unsigned)(e0[v] >> 32)));
-        if (p1 != p0) {
-          const float2 f = make_float2(__uint_as_float((unsigned)e1[v]), __uint_as_float((unsigned)(e1[v] >> 32)));
-          e = make_float2(f.x * e.x, fmaf(f.x, e.y, f.y));
-        }
-        sh.theirs[wave][v][lane] = e;
+        float2 all = make_float2(1.0f, 0.0f);
+#pragma unroll
+        for (int k = 0; k < kEach; ++k)
+          if (k < n) {
+            const float f = __uint_as_float((unsigned)e[k][v]);
+            all = make_float2(f * all.x, fmaf(f, all.y, __uint_as_float((unsigned)(e[k][v] >> 32))));
+          }
+        sh.theirs[wave][v][lane] = all;
       }
     }
     if (wave == kWaves - 1 && group > 0) {
@@ -211,7 +216,7 @@ __device__ __forceinline__ void begin_with(const ScanArgs &s, Shared<V> &sh, con
 #pragma unroll
     for (int v = 0; v < V; ++v) {
       if (group > 0) state[v] = sh.start[v][lane];
-      for (int w = 0; 2 * w < before; ++w) state[v] = fmaf(sh.theirs[w][v][lane].x, state[v], sh.theirs[w][v][lane].y);
+      for (int w = 0; kEach * w < before; ++w) state[v] = fmaf(sh.theirs[w][v][lane].x, state[v], sh.theirs[w][v][lane].y);
     }
     if (wave == kWaves - 1 && before == kGroup - 1 && piece < s.pieces - 1) {
       const int64_t p = (group + 1) * row + column;

@@ -32,7 +32,8 @@ __all__ = ["Variable", "Parameter", "VariableNode", "FunctionNode", "GpuBackend"
            "grad", "mul", "sub", "scale", "tanh", "sum_all", "sum_rows", "broadcast_to", "broadcast_rows", "transpose",
            "relu_grad", "user_elementwise",
            "Masks", "dropout", "layer_norm", "residual_norm", "LayerNorm",
-           "MLP", "LSTMLanguageModel"]
+           "gated_scan", "embed_scaled",
+           "MLP", "LSTMLanguageModel", "GatedLanguageModel"]
 
 
 # ---- backend ----------------------------------------------------------------------------------------
@@ -212,6 +213,43 @@ class GpuBackend:
     def sample(self, logits, u, out, temperature=None, top_k=None, top_p=None, min_p=None):
         logits = self._rows(logits)
         self.B.sample(logits, u, out, temperature, top_k, top_p, min_p, ws=self._bytes(self.B.sample_workspace_bytes(logits)))
+
+    def logits_adjust(self, logits, out, tokens=None, lengths=None, prompt=None, repetition=None, frequency=None, presence=None, bias_ids=None, bias=None,
+                      allowed=None):
+        self.B.logits_adjust(self._rows(logits), out, tokens, lengths, prompt, repetition, frequency, presence, bias_ids, bias, allowed)
+
+    def text(self, ids, n_steps, more):
+        """Memory for n_steps steps of tokens and `more` further ones, (n_steps + more, B), the first of which are the flat time-major `ids`."""
+        t = self.torch.empty((n_steps + more, ids.shape[0] // n_steps), dtype=self.torch.int64, device=self._dev)
+        t[:n_steps].view(-1).copy_(ids)
+        return t
+
+    def _steps(self, a, n_steps):
+        """(T*B, W) rows as (T, B, W)."""
+        a = self._rows(a)
+        return a.view(n_steps, a.shape[0] // n_steps, a.shape[1])
+
+    def gated_scan_fwd(self, z, y, h0, h_last, keep, lengths, kind, n_steps):
+        """z (T*B, 2H): gates and inputs; returns what the backward pass needs, if it is to be kept."""
+        z, y = self._steps(z, n_steps), self._steps(y, n_steps)
+        T, Bn, H = y.shape
+        states = self.empty(self.B.gated_scan_states_shape(T, Bn, H)) if keep else None
+        gate, x = z[:, :, :H], z[:, :, H:]
+        self.B.gated_scan_fwd(gate, x, y, self._rows(h0), h_last, states, lengths, kind, ws=self._bytes(self.B.gated_scan_workspace_bytes(gate)))
+        return states
+
+    def gated_scan_bwd(self, z, states, dy, dz, dh_last, dh0, lengths, kind, n_steps):
+        z, dy, dz = self._steps(z, n_steps), self._steps(dy, n_steps), self._steps(dz, n_steps)
+        H = dy.shape[2]
+        gate = z[:, :, :H]
+        self.B.gated_scan_bwd(gate, z[:, :, H:], states, dy, dz[:, :, :H], dz[:, :, H:], self._rows(dh_last), dh0, lengths, kind,
+                              ws=self._bytes(self.B.gated_scan_workspace_bytes(gate)))
+
+    def embed_scaled_fwd(self, table, ids, out, scale):
+        self.B.embed_scaled_fwd(table, ids, out, scale)
+
+    def embed_sorted_bwd(self, ids, dout, dtable, scale, accumulate):
+        self.B.embed_sorted_bwd(ids, self._rows(dout), dtable, scale, accumulate, ws=self._bytes(self.B.embed_sorted_workspace_bytes(ids, dtable)))
 
     def sgd_update_multi(self, params, grads, lr, lowp_copies):
         self.B.sgd_update_multi(params, grads, lr, lowp_copies)
@@ -1308,6 +1346,106 @@ class EmbedGrad(FunctionNode):
         return (embed_id(self.ids, gys[0]),)
 
 
+class EmbedScaled(FunctionNode):
+    """out[n] = scale * table[ids[n]], in a storage type of its own; the backward sorts the tokens and sums their rows.  Retains nothing but the ids."""
+    fresh = (1,)
+
+    def __init__(self, scale=1.0, out_dtype=None):
+        super().__init__()
+        self.scale, self.out_dtype = float(scale), out_dtype
+
+    def forward(self, xs):
+        F = backend()
+        ids = xs[0]
+        var = self.in_vars[1]
+        table = var.compute_array if isinstance(var, Parameter) else var.array   # (the bf16 working copy, if any)
+        self.ids, self.table_shape = ids, tuple(table.shape)
+        out = F.empty((ids.shape[0], table.shape[1]), self.out_dtype or F.dtype(table))
+        F.embed_scaled_fwd(table, ids, out, self.scale)
+        return (out,)
+
+    def release_locals(self):
+        self.ids = None
+
+    def backward(self, indexes, gys):
+        F = backend()
+        out = []
+        for k, i in enumerate(indexes):
+            g = None
+            if i == 1:
+                g = self.grad_slots[k]
+                accumulate = g is not None
+                if g is None:
+                    g = F.empty(self.table_shape, "f32")
+                F.embed_sorted_bwd(self.ids, gys[0], g, self.scale, accumulate)
+            out.append(g)
+        return tuple(out)
+
+    def backward_vars(self, indexes, gys):
+        if not _record:
+            return FunctionNode.backward_vars(self, indexes, gys)
+        return tuple(EmbedScaledGrad(self.ids, self.table_shape, self.scale).apply((gys[0],))[0] if i == 1 else None for i in indexes)
+
+
+class EmbedScaledGrad(FunctionNode):
+    """dout (N, D) -> dtable (V, D): the backward of the scaled lookup as a function.  Linear, so its own backward is the lookup again."""
+
+    def __init__(self, ids, table_shape, scale):
+        super().__init__()
+        self.ids, self.table_shape, self.scale = ids, table_shape, scale
+
+    def forward(self, xs):
+        F = backend()
+        self.dt = F.dtype(xs[0])
+        g = F.empty(self.table_shape, "f32")
+        F.embed_sorted_bwd(self.ids, xs[0], g, self.scale, False)
+        return (g,)
+
+    def backward_vars(self, indexes, gys):
+        return (embed_scaled(self.ids, gys[0], self.scale, self.dt),)
+
+
+class GatedScan(FunctionNode):
+    """(h0, z) -> (h_T, hs): a gated linear recurrence over all steps.  z (T*B, 2H) holds gates and inputs side by side, time-major as in NStepLSTM, h0
+    (B, H) the first state, fp32; hs (T*B, H) the states of all steps in z's storage type (or `out_dtype`), h_T the last ones, fp32.  Sequences may end early
+    (`lengths`).  No product links a step to the next one, so the steps run in parallel; retained are z and the state before every few steps."""
+    fresh = (0, 1)
+
+    def __init__(self, n_steps, kind="sigmoid", lengths=None, out_dtype=None):
+        super().__init__()
+        self.T, self.kind, self.lengths, self.out_dtype = int(n_steps), kind, lengths, out_dtype
+
+    def forward(self, xs):
+        F = backend()
+        h0, z = xs
+        Bn, H = h0.shape
+        if self.T < 1 or tuple(z.shape) != (self.T * Bn, 2 * H) or (self.lengths is not None and tuple(self.lengths.shape) != (Bn,)):
+            raise ValueError("gated_scan: z %s, h0 %s do not fit %d steps" % (tuple(z.shape), tuple(h0.shape), self.T))
+        self.dt = F.dtype(z)
+        self.out_dtype = self.out_dtype or self.dt
+        hs, h = F.empty((self.T * Bn, H), self.out_dtype), F.empty((Bn, H), "f32")
+        keep = _record and any(v.node.requires_grad for v in self.in_vars)
+        self.states = F.gated_scan_fwd(z, hs, h0, h, keep, self.lengths, self.kind, self.T)
+        self.retain_inputs((1,))
+        return (h, hs)
+
+    def release_locals(self):
+        self.states = self.lengths = None
+
+    def backward(self, indexes, gys):
+        F = backend()
+        z, = self.get_retained_inputs()
+        Bn, H = z.shape[0] // self.T, z.shape[1] // 2
+        gh, ghs = gys
+        if ghs is None:                                  # (only the last state was used)
+            ghs = F.empty((z.shape[0], H), self.out_dtype)
+            F.elementwise_broadcast("fill", [], ghs, (0.0,))
+        dz = F.empty(z.shape, self.dt)
+        dh0 = F.empty((Bn, H), "f32") if 0 in indexes else None
+        F.gated_scan_bwd(z, self.states, ghs, dz, _in_type(F, gh, "f32"), dh0, self.lengths, self.kind, self.T)
+        return tuple(dh0 if i == 0 else dz for i in indexes)
+
+
 class LSTM(FunctionNode):
     """(c_prev, z[, bias]) -> (c, h): the cell of the recurrent language model; z holds the four
     gate pre-activations.  Backward works from retained outputs: the activated gates the forward
@@ -1779,6 +1917,17 @@ def embed_id(ids, table):
     return EmbedID().apply((ids, table))[0]
 
 
+def embed_scaled(ids, table, scale=1.0, out_dtype=None):
+    """scale * table[ids], in the storage type of the table's working copy or `out_dtype`; its gradient is summed by sorted tokens."""
+    return EmbedScaled(scale, out_dtype).apply((ids, table))[0]
+
+
+def gated_scan(h0, z, n_steps, kind="sigmoid", lengths=None, out_dtype=None):
+    """h_t = a h_{t-1} + (1 - a) x_t with a = sigmoid(gate_t) ("sigmoid"), or gate_t h_{t-1} + x_t ("decay"), z (n_steps*B, 2H) holding gates and inputs side by
+    side; returns (h_T, hs) with hs (n_steps*B, H).  lengths (B,): steps of each sequence, behind which hs is 0 and the state stays."""
+    return GatedScan(n_steps, kind, lengths, out_dtype).apply((h0, z))
+
+
 def lstm(c_prev, z, bias=None, twice_differentiable=False):
     """Returns (c, h)."""
     return LSTM(twice_differentiable).apply((c_prev, z) if bias is None else (c_prev, z, bias))
@@ -1947,7 +2096,56 @@ class MLP:
         return softmax_cross_entropy(self(x), t, grad_dtype="bf16" if self.lowp else None)
 
 
-class LSTMLanguageModel:
+class _Generates:
+    """What answers with a model's `_hidden` and `_logits`."""
+
+    def generate(self, ids, n_steps, u, state=None, temperature=None, top_k=None, top_p=None, min_p=None, repetition=None, frequency=None, presence=None,
+                 bias_ids=None, bias=None, allowed=None):
+        """Continues a prompt.  ids: flat (T*B,) integer array of `n_steps` steps, time-major; u: (n, B) array of fp32 numbers in [0, 1), one for
+        each token that is wanted.  temperature, top_k, top_p, min_p: a number, one for each of the B sequences (an array of the backend's, a
+        NumPy array, a list), or None (not used).  repetition, frequency, presence: the same, penalties for what a sequence holds already (the prompt counts for the first one
+        alone); bias_ids, bias (M,) or (B, M): added to the logits of those tokens; allowed (ceil(V/32),) or (B, ceil(V/32)) int32: bit masks of the tokens that
+        may be drawn.  Returns the (n, B) int64 array of tokens and the state after the last but one, which has seen everything but the
+        last token.  Nothing is recorded and nothing is dropped."""
+        import numpy as np
+        F = backend()
+        if n_steps < 1 or len(u.shape) != 2 or u.shape[0] < 1 or ids.shape[0] != n_steps * u.shape[1]:
+            raise ValueError("%s.generate: %d ids of %d steps for u of shape %s" % (type(self).__name__, ids.shape[0], n_steps, tuple(u.shape)))
+        Bn = u.shape[1]
+
+        def row(v, dt):
+            if v is None or (hasattr(v, "shape") and not isinstance(v, (np.generic, np.ndarray))):
+                return v
+            return F.from_numpy(np.array(np.broadcast_to(np.asarray(v, dtype=dt), (Bn,))))
+        filters = (row(temperature, np.float32), row(top_k, np.int64), row(top_p, np.float32), row(min_p, np.float32))
+
+        def rows(v, dt):
+            if v is None or (hasattr(v, "shape") and not isinstance(v, np.ndarray)):
+                return v
+            v = np.asarray(v, dtype=dt)
+            return F.from_numpy(np.array(np.broadcast_to(v, (Bn, v.shape[-1]))))
+        penalties = {"repetition": row(repetition, np.float32), "frequency": row(frequency, np.float32), "presence": row(presence, np.float32)}
+        adjusts = {"bias_ids": rows(bias_ids, np.int64), "bias": rows(bias, np.float32), "allowed": rows(allowed, np.int32)}
+        text, begin = None, n_steps
+        if any(p is not None for p in penalties.values()):
+            text = F.text(ids, n_steps, u.shape[0])
+            adjusts.update(penalties, prompt=F.from_numpy(np.full(Bn, n_steps, dtype=np.int64)))
+            out = text[n_steps:]
+        else:
+            out = F.empty(tuple(u.shape), "i64")
+        adjusted = any(p is not None for p in adjusts.values())
+        with no_backprop_mode():
+            for t in range(u.shape[0]):
+                hs, state = self._hidden(ids, n_steps, state, 0.0)
+                last = Variable(hs.array[(n_steps - 1) * Bn:], requires_grad=False)
+                logits = self._logits(last, 0.0).array
+                if adjusted:
+                    F.logits_adjust(logits, logits, tokens=None if text is None else text[:begin + t].T, **adjusts)
+                F.sample(logits, u[t], out[t], *filters)
+                ids, n_steps = out[t], 1
+        return out, state
+
+class LSTMLanguageModel(_Generates):
     """Embedding, one LSTM layer, output Linear layer, softmax cross-entropy over every (time,
     batch) token; time-major rows (row t*B + b).  ``P``: dict of backend arrays E (V,E), W (E,4H),
     U (H,4H), b (4H,), W_out (V,H), b_out (V,).  The forward code is ordinary Python: the number of
@@ -2024,27 +2222,62 @@ class LSTMLanguageModel:
         hs, state = self._hidden(ids, n_steps, state)
         return softmax_cross_entropy(self._logits(hs), targets, grad_dtype="bf16" if self.lowp else None), state
 
-    def generate(self, ids, n_steps, u, state=None, temperature=None, top_k=None, top_p=None, min_p=None):
-        """Continues a prompt.  ids: flat (T*B,) integer array of `n_steps` steps, time-major; u: (n, B) array of fp32 numbers in [0, 1), one for
-        each token that is wanted.  temperature, top_k, top_p, min_p: a number, one for each of the B sequences (an array of the backend's, a
-        NumPy array, a list), or None (not used).  Returns the (n, B) int64 array of tokens and the state after the last but one, which has seen everything but the
-        last token.  Nothing is recorded and nothing is dropped."""
-        import numpy as np
-        F = backend()
-        if n_steps < 1 or len(u.shape) != 2 or u.shape[0] < 1 or ids.shape[0] != n_steps * u.shape[1]:
-            raise ValueError("LSTMLanguageModel.generate: %d ids of %d steps for u of shape %s" % (ids.shape[0], n_steps, tuple(u.shape)))
-        Bn = u.shape[1]
 
-        def row(v, dt):
-            if v is None or (hasattr(v, "shape") and not isinstance(v, (np.generic, np.ndarray))):
-                return v
-            return F.from_numpy(np.array(np.broadcast_to(np.asarray(v, dtype=dt), (Bn,))))
-        filters = (row(temperature, np.float32), row(top_k, np.int64), row(top_p, np.float32), row(min_p, np.float32))
-        out = F.empty(tuple(u.shape), "i64")
-        with no_backprop_mode():
-            for t in range(u.shape[0]):
-                hs, state = self._hidden(ids, n_steps, state, 0.0)
-                last = Variable(hs.array[(n_steps - 1) * Bn:], requires_grad=False)
-                F.sample(self._logits(last, 0.0).array, u[t], out[t], *filters)
-                ids, n_steps = out[t], 1
-        return out, state
+class GatedLanguageModel(_Generates):
+    """Scaled embeddings, layers of gated linear recurrences as residual blocks, output Linear layer, softmax cross-entropy over every (time, batch) token;
+    time-major rows as in LSTMLanguageModel.  ``P``: dict of backend arrays E (V,H), W_out (V,H), b_out (V,), gamma, beta (H,) of the first normalisation,
+    and, for layer k = 0, 1, ..., W<k> (2H,H), b<k> (2H,) (gates and inputs), gamma<k>, beta<k> (H,).  Each layer reads the normalised stream, and its states are added to
+    it.  The steps of a sequence run in parallel; a token of an answer is one step from the state.
+
+    ``lowp``: bf16 working copies of E and the W feed the products, as do bf16 normalised values, gates, inputs and states of all steps; the stream, the states that are carried
+    on, logits and gradients of parameters stay fp32.  ``ratio``, ``masks``: dropout of the states on their way to the stream, and of the embeddings, while `train` is true."""
+
+    def __init__(self, P, lowp=False, ratio=0.0, masks=None):
+        if ratio > 0.0 and masks is None:
+            raise ValueError("GatedLanguageModel: dropout needs masks")
+        self.n_layers = sum(1 for k in P if k.startswith("W") and k[1:].isdigit())
+        names = {"E", "W_out", "b_out", "gamma", "beta"} | {n + str(k) for n in ("W", "b", "gamma", "beta") for k in range(self.n_layers)}
+        if set(P) != names or self.n_layers < 1:
+            raise ValueError("GatedLanguageModel: parameters %s for %d layers" % (sorted(P), self.n_layers))
+        F = backend()
+        self.P = {}
+        for k, v in P.items():
+            low = None
+            if lowp and (k == "E" or k.startswith("W")):
+                low = F.empty(tuple(v.shape), "bf16")
+                F.elementwise_broadcast("copy", [v], low)
+            self.P[k] = Parameter(v, low, k)
+        self.scale = float(P["E"].shape[1]) ** 0.5
+        self.lowp, self.ratio, self.masks, self.train = lowp, float(ratio), masks, True
+
+    def params(self):
+        return list(self.P.values())
+
+    def _hidden(self, ids, n_steps, state, ratio=None, lengths=None):
+        """What the output layer is to see of all steps, (T*B, H), and the states after the last, one for each layer."""
+        P, F = self.P, backend()
+        if ratio is None:
+            ratio = self.ratio if self.train else 0.0
+        stream = embed_scaled(ids, P["E"], self.scale, "f32")
+        if ratio > 0.0:
+            stream = dropout(stream, ratio, self.masks)
+        y = layer_norm(stream, P["gamma"], P["beta"], out_dtype="bf16" if self.lowp else None)
+        if state is None:
+            z0 = F.empty((ids.shape[0] // n_steps, P["E"].shape[1]), "f32")
+            F.elementwise_broadcast("fill", [], z0, (0.0,))
+            state = [Variable(z0, requires_grad=False)] * self.n_layers
+        after = []
+        for k in range(self.n_layers):
+            k_ = str(k)
+            h, hs = gated_scan(state[k], linear(y, P["W" + k_], P["b" + k_]), n_steps, lengths=lengths)
+            after.append(h)
+            y, stream = residual_norm(hs, stream, P["gamma" + k_], P["beta" + k_], ratio, self.masks)
+        return y, after
+
+    def _logits(self, y, ratio=None):
+        return linear(y, self.P["W_out"], self.P["b_out"], out_dtype="f32")
+
+    def loss(self, ids, targets, n_steps, state=None, lengths=None):
+        """ids, targets: flat (T*B,) integer arrays; lengths (B,): steps of each sequence (the targets behind them are to be -1).  Returns (loss, states)."""
+        y, state = self._hidden(ids, n_steps, state, lengths=lengths)
+        return softmax_cross_entropy(self._logits(y), targets, grad_dtype="bf16" if self.lowp else None), state

@@ -159,6 +159,19 @@ def test_one_list_for_all_rows():
     close(got[ok], want[ok], bound[ok] + R.U * np.abs(want[ok]))
 
 
+def test_texts_that_grow_in_time_major_memory():
+    n, v, length = 5, 700, 900
+    rng = np.random.default_rng(3)
+    z, t = rng.standard_normal((n, v)).astype(np.float32), rng.integers(0, v, (length + 1, n))
+    f = rng.random(n).astype(np.float32)
+    text = dev(t, "i64")
+    for upto in (0, 1, length):
+        want, bound = R.adjust(z, t[:upto].T, None, None, None, f)
+        o = torch.empty(n, v, device="cuda")
+        B.logits_adjust(torch.from_numpy(z).cuda(), o, tokens=text[:upto].T, frequency=dev(f, "i64"))
+        close(values(o), want, bound + R.U * np.abs(want))
+
+
 def test_no_rows_no_tokens():
     z = torch.empty(0, 5, device="cuda")
     B.logits_adjust(z, torch.empty_like(z))

@@ -106,7 +106,7 @@ def test_adjust_refuses():
     for name in ("lengths", "prompt"):
         assert adjust(tokens=t, **{name: p}) == -3 and adjust(tokens=t, **{name: d((2,), B.I64)}) == -4
     assert adjust(tokens=d((3, 9))) == -3 and adjust(tokens=d((2, 9), B.I64)) == -4 and adjust(tokens=d((27,), B.I64)) == -2
-    assert adjust(tokens=d((3, 9), B.I64, strides=[144, 16])) == -5 and adjust(tokens=d((3, 2 ** 30), B.I32)) == -4
+    assert adjust(tokens=d((3, 9), B.I64, strides=[144, -16])) == -5 and adjust(tokens=d((3, 2 ** 30), B.I32)) == -4
     b, bi = d((3, 4)), d((3, 4), B.I64)
     assert adjust(bias=b) == -1 and adjust(bias_ids=bi) == -1
     assert adjust(bias=bi, bias_ids=bi) == -3 and adjust(bias=b, bias_ids=b) == -3 and adjust(bias=d((3, 5)), bias_ids=bi) == -4
