@@ -10,33 +10,44 @@ __device__ __forceinline__ int64_t id_at(const L *ids, int64_t n, int64_t stride
   return (uint64_t)id < (uint64_t)V ? id : V;            // an id outside the table is never used as an offset
 }
 
-// A wave for each row, in units at whatever address the rows have; what is left of a row behind its last whole unit goes element by element.
-template <typename TI, typename TO, typename L>
-__global__ __launch_bounds__(256) void embed_scaled_kernel(const TI *table, int64_t tp, int64_t V, const L *ids, int64_t is, int64_t N, int64_t D, float scale,
-                                                           TO *out, int64_t op, bool past) {
+// Units of a row, whichever rows they belong to, one after the other: a thread has kUnits of them, whose ids and then whose units are on their way
+// together, at whatever address they have.  What is left of a row behind its last whole unit goes element by element.
+constexpr int kUnits = 4;
+
+template <typename TI, typename TO, typename L, bool PAST>
+__global__ __launch_bounds__(256) void embed_scaled_kernel(const TI *table, int64_t tp, int64_t V, const L *ids, int64_t is, int64_t N, int64_t D, uint32_t upr, float scale,
+                                                           TO *out, int64_t op) {
   constexpr int E = unit_elements<TI, TO>();
-  const int lane = threadIdx.x & 63;
-  const int64_t n = block_number() * 4 + (threadIdx.x >> 6);
-  if (n >= N) return;
-  const int64_t id = id_at(ids, n, is, V);
-  const TI *src = table + id * tp;
-  TO *dst = out + n * op;
-  const bool none = id == V;
-  for (int64_t d = (int64_t)lane * E; d < D; d += 64 * E) {
-    if (d + E <= D) {
-      Unit<TI, E> u;
-      Unit<TO, E> o;
-      if (none) {
-        o.zero();
-      } else {
-        u.load(src + d);
+  const int64_t total = N * upr, first = (block_number() * 4 + (threadIdx.x >> 6)) * (64 * kUnits) + (threadIdx.x & 63);
+  int64_t n[kUnits], id[kUnits];
+  uint32_t c[kUnits];
 #pragma unroll
-        for (int e = 0; e < E; ++e) o.set(e, u.get(e) * scale);
-      }
-      if (past) o.store_nt(dst + d);
-      else o.store(dst + d);
+  for (int k = 0; k < kUnits; ++k) {
+    const int64_t i = min(first + k * 64, total - 1);
+    n[k] = total <= 0xffffffffll ? (int64_t)((uint32_t)i / upr) : i / upr;
+    c[k] = (uint32_t)(i - n[k] * upr);
+    id[k] = id_at(ids, n[k], is, V);
+  }
+  Unit<TI, E> u[kUnits];
+#pragma unroll
+  for (int k = 0; k < kUnits; ++k) {
+    const int64_t d = (int64_t)c[k] * E;
+    if (id[k] == V) u[k].zero();
+    else if (d + E <= D) u[k].load(table + id[k] * tp + d);
+  }
+#pragma unroll
+  for (int k = 0; k < kUnits; ++k) {
+    if (first + k * 64 >= total) break;
+    const int64_t d = (int64_t)c[k] * E;
+    TO *dst = out + n[k] * op + d;
+    if (d + E <= D) {
+      Unit<TO, E> o;
+#pragma unroll
+      for (int e = 0; e < E; ++e) o.set(e, id[k] == V ? 0.0f : u[k].get(e) * scale);
+      if constexpr (PAST) o.store_nt(dst);
+      else o.store(dst);
     } else {
-      for (int64_t e = d; e < D; ++e) Elem<TO>::store(dst + e, none ? 0.0f : Elem<TI>::load(src + e) * scale);
+      for (int e = 0; e < D - d; ++e) Elem<TO>::store(dst + e, id[k] == V ? 0.0f : Elem<TI>::load(table + id[k] * tp + d + e) * scale);
     }
   }
 }
@@ -57,7 +68,7 @@ struct SortArgs {
   uint32_t *starts, *ends;           // (V)
   int64_t stride, V;
   uint32_t N, share;                 // pairs of a block
-  int id64, shift, bits, blocks, first;
+  int id64, shift, bits, blocks, first, only;
   float *dtable;                     // of this launch's blocks behind the sort's: rows [row, row_end) of the table become zeros
   int64_t tp, D, row, row_end;
 };
@@ -162,6 +173,7 @@ __global__ __launch_bounds__(1024) void embed_sort_kernel(SortArgs s) {
   const uint32_t from = min(lo + wave * part, hi), to = min(from + part, hi);
   for (uint32_t i = from + lane; i < to; i += 64) atomicAdd(&sh.at[wave][key_of(s, s.first, s.keys, i) >> s.shift & mask], 1u);
   __syncthreads();
+  uint32_t total = 0;                                        // of the thread's digit
   bases(sh, [&](int d, uint32_t &mine, uint32_t &all) {
     if (d > (int)mask) return;
 #pragma unroll 8
@@ -170,7 +182,13 @@ __global__ __launch_bounds__(1024) void embed_sort_kernel(SortArgs s) {
       mine += b < (int)blockIdx.x ? c : 0;
       all += c;
     }
+    total = all;
   });
+  if (s.only && blockIdx.x == 0 && tid < s.V) {              // (one pass: digits are tokens, and this block's wave 0 has their first places)
+    s.starts[tid] = sh.at[0][tid];
+    s.ends[tid] = sh.at[0][tid] + total;
+  }
+  __syncthreads();
   for (uint32_t i0 = from; i0 < to; i0 += 64) {
     const uint32_t i = i0 + lane;
     const bool on = i < to;
@@ -287,12 +305,9 @@ __device__ __forceinline__ void add_rows(F row, int i, int n, int64_t at, float 
     }
 }
 
-// The sum of the rows at places [lo, hi), 64 of them at most, in a lane's columns, in their order.  Each lane fetches one place; from there on only
-// rows are waited for.
+// The sum of n rows, 64 of them at most, in a lane's columns, in the order in which the lanes hold their numbers.
 template <typename T, int E>
-__device__ __forceinline__ void sum_rows(const SumArgs &s, uint32_t lo, uint32_t hi, int64_t d, float (&sum)[E]) {
-  const int n = __builtin_amdgcn_readfirstlane((int)(hi - lo));
-  const uint32_t place = s.places[min(lo + (threadIdx.x & 63), hi - 1)];
+__device__ __forceinline__ void sum_places(const SumArgs &s, uint32_t place, int n, int64_t d, float (&sum)[E]) {
   auto row = [&](int i) { return static_cast<const T *>(s.dout) + (int64_t)(uint32_t)__builtin_amdgcn_readlane((int)place, i) * s.dp; };
 #pragma unroll
   for (int e = 0; e < E; ++e) sum[e] = 0.0f;
@@ -320,6 +335,13 @@ __device__ __forceinline__ void sum_rows(const SumArgs &s, uint32_t lo, uint32_t
       for (int e = 0; e < E; ++e) sum[e] += d + e < s.D ? Elem<T>::load(r + d + e) : 0.0f;
     }
   }
+}
+
+// The same for places [lo, hi) of the sorted list: each lane fetches one, and from there on only rows are waited for.
+template <typename T, int E>
+__device__ __forceinline__ void sum_rows(const SumArgs &s, uint32_t lo, uint32_t hi, int64_t d, float (&sum)[E]) {
+  const int n = __builtin_amdgcn_readfirstlane((int)(hi - lo));
+  sum_places<T, E>(s, s.places[min(lo + (threadIdx.x & 63), hi - 1)], n, d, sum);
 }
 
 template <int E>
@@ -399,6 +421,55 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(SumArgs s) {
       sum_rows<T, E>(s, from, from + c, d, sum);
       if (d < s.D) write_row<E>(s, v0 + r, d, sum);
     } else {
+      zero_row<E>(s, v0 + r, d - lane * E);
+    }
+  }
+}
+
+// Few ids: nothing is sorted.  A wave looks through them for its rows' tokens, 64 at a time, and adds up the rows that it finds there, then these sums.
+constexpr int kDirect = 256;
+
+template <typename T, typename L>
+__global__ __launch_bounds__(256) void embed_direct_kernel(SumArgs s, const L *ids, int64_t stride) {
+  constexpr int E = unit_elements<T>(), M = kDirect / 64;
+  const int lane = threadIdx.x & 63;
+  const int64_t job = block_number() * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), rows = job / s.chunks, v0 = rows * s.rows;
+  const int64_t d = ((job - rows * s.chunks) * 64 + lane) * E;
+  if (v0 >= s.V) return;
+  const int n = (int)min((int64_t)s.rows, s.V - v0), N = (int)s.N;
+  uint32_t id[M];                                            // of ids outside the table V and above, which no row has
+#pragma unroll
+  for (int m = 0; m < M; ++m) {
+    id[m] = ~0u;
+    if (m * 64 < N) {
+      const int i = m * 64 + lane;
+      const int64_t v = id_at(ids, min(i, N - 1), stride, s.V);
+      id[m] = i < N ? (uint32_t)v : ~0u;
+    }
+  }
+  for (int r = 0; r < n; ++r) {
+    float total[E];
+    bool any = false;
+#pragma unroll
+    for (int e = 0; e < E; ++e) total[e] = 0.0f;
+#pragma unroll
+    for (int m = 0; m < M; ++m) {
+      if (m * 64 >= N) break;
+      unsigned long long found = __ballot(id[m] == (uint32_t)(v0 + r));
+      if (!found) continue;
+      any = true;
+      // the found places in their order, one to a lane
+      const int count = __popcll(found);
+      int place = 0;
+      for (int k = 0; k < count; ++k, found &= found - 1) place = lane == k ? m * 64 + (int)__builtin_ctzll(found) : place;
+      float sum[E];
+      sum_places<T, E>(s, (uint32_t)place, count, d, sum);
+#pragma unroll
+      for (int e = 0; e < E; ++e) total[e] += sum[e];
+    }
+    if (any) {
+      if (d < s.D) write_row<E>(s, v0 + r, d, total);
+    } else if (!s.accumulate) {
       zero_row<E>(s, v0 + r, d - lane * E);
     }
   }
@@ -511,22 +582,26 @@ chn_status chn_embed_scaled_fwd(const chn_array *table, const chn_array *ids, do
   if (on != N || od != D) return fail(CHN_ERR_SHAPE, "embed: out must have shape (%lld,%lld)", (long long)N, (long long)D);
   if (V > 0x7fffffff) return fail(CHN_ERR_SHAPE, "embed: a table of %lld rows", (long long)V);
   if (N == 0 || D == 0) return CHN_OK;
-  const dim3 grid = grid_of((N + 3) / 4);
+  const int E = table->dtype == CHN_F32 && out->dtype == CHN_F32 ? 4 : 8;
+  const int64_t upr = (D + E - 1) / E;
+  if (upr > 0x7fffffff) return fail(CHN_ERR_SHAPE, "embed: rows of %lld elements", (long long)D);
+  const dim3 grid = grid_of((N * upr + 256 * kUnits - 1) / (256 * kUnits));
   hipStream_t st = as_stream(stream);
+  // whole lines go past the caches
   const int64_t osz = dtype_size(out->dtype);
   const bool past = D * osz % 128 == 0 && op * osz % 128 == 0 && reinterpret_cast<uintptr_t>(out->data) % 128 == 0;
+#define CHN_LAUNCH(TI, TO, L, P)                                                                                                                     \
+  hipLaunchKernelGGL((embed_scaled_kernel<TI, TO, L, P>), grid, dim3(256), 0, st, static_cast<const TI *>(table->data), tp, V,                       \
+                     static_cast<const L *>(ids->data), is, N, D, (uint32_t)upr, (float)scale, static_cast<TO *>(out->data), op)
 #define CHN_GO(TI, TO)                                                                                                                               \
   do {                                                                                                                                               \
-    if (ids->dtype == CHN_I32)                                                                                                                       \
-      hipLaunchKernelGGL((embed_scaled_kernel<TI, TO, int32_t>), grid, dim3(256), 0, st, static_cast<const TI *>(table->data), tp, V,                \
-                         static_cast<const int32_t *>(ids->data), is, N, D, (float)scale, static_cast<TO *>(out->data), op, past);                   \
-    else                                                                                                                                             \
-      hipLaunchKernelGGL((embed_scaled_kernel<TI, TO, int64_t>), grid, dim3(256), 0, st, static_cast<const TI *>(table->data), tp, V,                \
-                         static_cast<const int64_t *>(ids->data), is, N, D, (float)scale, static_cast<TO *>(out->data), op, past);                   \
+    if (ids->dtype == CHN_I32) { if (past) CHN_LAUNCH(TI, TO, int32_t, true); else CHN_LAUNCH(TI, TO, int32_t, false); }                             \
+    else { if (past) CHN_LAUNCH(TI, TO, int64_t, true); else CHN_LAUNCH(TI, TO, int64_t, false); }                                                   \
   } while (0)
   if (table->dtype == CHN_F32) { if (out->dtype == CHN_F32) CHN_GO(float, float); else CHN_GO(float, bf16_raw); }
   else { if (out->dtype == CHN_F32) CHN_GO(bf16_raw, float); else CHN_GO(bf16_raw, bf16_raw); }
 #undef CHN_GO
+#undef CHN_LAUNCH
   return check_launch("embed_scaled_fwd");
 }
 
@@ -534,8 +609,8 @@ size_t chn_embed_sorted_workspace_bytes(const chn_array *ids, const chn_array *d
   using namespace chn;
   if (!ids || !dtable || ids->ndim != 1 || dtable->ndim != 2) return 0;
   const int64_t N = ids->shape[0], V = dtable->shape[0], D = dtable->shape[1];
-  if (N < 0 || V <= 0 || D <= 0 || N > 0x7fffffff || V > 0x7fffffff) return 0;
-  return Layout(N, V, D).bytes;
+  if (V <= 0 || D <= 0 || N > 0x7fffffff || V > 0x7fffffff) return 0;
+  return N <= kDirect ? 0 : Layout(N, V, D).bytes;
 }
 
 chn_status chn_embed_sorted_bwd(const chn_array *ids, const chn_array *dout, double scale, const chn_array *dtable, int accumulate, void *ws,
@@ -553,9 +628,24 @@ chn_status chn_embed_sorted_bwd(const chn_array *ids, const chn_array *dout, dou
   if (V > 0x7fffffff) return fail(CHN_ERR_SHAPE, "embed: a table of %lld rows", (long long)V);
   CHN_TRY(check_ws(ws, ws_bytes, chn_embed_sorted_workspace_bytes(ids, dtable), "embed_sorted_bwd"));
   if (V == 0 || D == 0) return CHN_OK;
+  const int E = dout->dtype == CHN_F32 ? 4 : 8;
+  SumArgs s = {};
+  s.dout = dout->data; s.dtable = static_cast<float *>(dtable->data);
+  s.dp = dp; s.tp = tp; s.V = V; s.D = D; s.chunks = (D + 64 * E - 1) / (64 * E);
+  s.scale = (float)scale; s.N = (uint32_t)N; s.accumulate = accumulate;
+  const int64_t each = V * s.chunks / 8192;                  // (as many waves as run at once: each waits for its rows' tokens)
+  s.rows = (int)(each < 1 ? 1 : each > 16 ? 16 : each);
+  const int64_t row_jobs = (V + s.rows - 1) / s.rows * s.chunks;
+  hipStream_t st = as_stream(stream);
+  if (N <= kDirect) {
+#define CHN_GO(T, L) hipLaunchKernelGGL((embed_direct_kernel<T, L>), grid_of((row_jobs + 3) / 4), dim3(256), 0, st, s, static_cast<const L *>(ids->data), is)
+    if (ids->dtype == CHN_I32) { if (dout->dtype == CHN_F32) CHN_GO(float, int32_t); else CHN_GO(bf16_raw, int32_t); }
+    else { if (dout->dtype == CHN_F32) CHN_GO(float, int64_t); else CHN_GO(bf16_raw, int64_t); }
+#undef CHN_GO
+    return check_launch("embed_sorted_bwd");
+  }
   const Layout z(N, V, D);
   char *w = static_cast<char *>(ws);
-  hipStream_t st = as_stream(stream);
   auto words = [&](size_t at) { return reinterpret_cast<uint32_t *>(w + at); };
   SortArgs o = {};
   o.ids = ids->data; o.stride = is; o.id64 = ids->dtype == CHN_I64;
@@ -565,12 +655,13 @@ chn_status chn_embed_sorted_bwd(const chn_array *ids, const chn_array *dout, dou
   const bool filled = z.blocks > 1 && !accumulate && N <= V / 2;
   o.dtable = static_cast<float *>(dtable->data); o.tp = tp; o.D = D;
   if (z.blocks == 1) {
-    if (N > 0) hipLaunchKernelGGL(embed_sort_few_kernel, dim3(1), dim3(1024), 0, st, o, z.passes);
+    hipLaunchKernelGGL(embed_sort_few_kernel, dim3(1), dim3(1024), 0, st, o, z.passes);
     CHN_TRY(check_launch("embed_sorted_bwd"));
   } else {
     for (int p = 0; p < z.passes; ++p) {
       const bool last = (z.passes - 1 - p) % 2 == 0;         // the last pass ends in `keys`
       o.first = p == 0;
+      o.only = z.passes == 1;
       o.shift = p * z.bits;
       o.keys = words(last ? z.between : z.keys); o.places = words(last ? z.places_between : z.places);
       o.keys_out = words(last ? z.keys : z.between); o.places_out = words(last ? z.places : z.places_between);
@@ -587,23 +678,17 @@ chn_status chn_embed_sorted_bwd(const chn_array *ids, const chn_array *dout, dou
       }
     }
   }
-  const int E = dout->dtype == CHN_F32 ? 4 : 8;
-  SumArgs s = {};
   s.keys = words(z.keys); s.places = words(z.places); s.starts = words(z.starts); s.ends = words(z.ends);
-  s.dout = dout->data; s.dtable = static_cast<float *>(dtable->data); s.partial = reinterpret_cast<float *>(w + z.partial);
-  s.dp = dp; s.tp = tp; s.pitch = z.pitch; s.V = V; s.D = D; s.chunks = (D + 64 * E - 1) / (64 * E); s.pieces = z.pieces;
-  s.scale = (float)scale; s.N = (uint32_t)N; s.accumulate = accumulate; s.leave = accumulate || filled;
-  if (z.blocks > 1) {
+  s.partial = reinterpret_cast<float *>(w + z.partial); s.pitch = z.pitch; s.pieces = z.pieces;
+  s.leave = accumulate || filled;
+  if (z.blocks > 1 && z.passes > 1) {
     hipLaunchKernelGGL(embed_ranges_kernel, dim3((unsigned)((N + 255) / 256)), dim3(256), 0, st, s);
     CHN_TRY(check_launch("embed_sorted_bwd"));
   }
-  const int64_t each = V * s.chunks / 16384;                 // (fewer waves than that, and the chip is not full)
-  s.rows = (int)(each < 1 ? 1 : each > 16 ? 16 : each);
-  const dim3 grid = grid_of(((z.pieces + (V + s.rows - 1) / s.rows) * s.chunks + 3) / 4);
+  const dim3 grid = grid_of((z.pieces * s.chunks + row_jobs + 3) / 4);
   if (dout->dtype == CHN_F32) hipLaunchKernelGGL((embed_sum_kernel<float>), grid, dim3(256), 0, st, s);
   else hipLaunchKernelGGL((embed_sum_kernel<bf16_raw>), grid, dim3(256), 0, st, s);
   CHN_TRY(check_launch("embed_sorted_bwd"));
-  if (N <= kPiece) return CHN_OK;                            // (no token stands more often)
   if (dout->dtype == CHN_F32) hipLaunchKernelGGL((embed_join_kernel<4>), grid_of((z.pieces + kLooked - 1) / kLooked * s.chunks), dim3(64 * kJoinWaves), 0, st, s);
   else hipLaunchKernelGGL((embed_join_kernel<8>), grid_of((z.pieces + kLooked - 1) / kLooked * s.chunks), dim3(64 * kJoinWaves), 0, st, s);
   return check_launch("embed_sorted_bwd");

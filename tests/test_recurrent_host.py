@@ -57,11 +57,11 @@ def test_scan_asks_for_its_workspace():
     T, Bn, D = 70000, 1, 1024
     gate = d((T, Bn, D))
     need = B.gated_scan_workspace_bytes(gate)
-    if need:
-        for fwd in (True, False):
-            assert scan(fwd, T=T, Bn=Bn, D=D) == -8
-            assert scan(fwd, T=T, Bn=Bn, D=D, ws=4096, nbytes=need - 1) == -8
-            assert scan(fwd, T=T, Bn=Bn, D=D, ws=4096 + 64, nbytes=need) == -8
+    assert need > 0
+    for fwd in (True, False):
+        assert scan(fwd, T=T, Bn=Bn, D=D) == -8
+        assert scan(fwd, T=T, Bn=Bn, D=D, ws=4096, nbytes=need - 1) == -8
+        assert scan(fwd, T=T, Bn=Bn, D=D, ws=4096 + 64, nbytes=need) == -8
     assert B.gated_scan_workspace_bytes(d((1, 128, 650))) == 0
 
 
@@ -83,9 +83,10 @@ def test_embed_refuses():
         assert embed(bwd, table=d((2 ** 31, 4))) == -4
     assert embed(table=d((6, 4), B.BF16)) == -3
     assert embed(table=d((6, 4), strides=[0, 4])) == -5 and embed(False, rows=d((10, 4), strides=[0, 4])) == -5
-    need = B.embed_sorted_workspace_bytes(d((10,), B.I64), d((6, 4)))
-    if need:
-        assert embed() == -8 and embed(ws=4096, nbytes=need - 1) == -8 and embed(ws=4100, nbytes=need) == -8
+    assert B.embed_sorted_workspace_bytes(d((10,), B.I64), d((6, 4))) == 0           # (few ids are not sorted)
+    many = dict(ids=d((5000,), B.I64), rows=d((5000, 4)))
+    need = B.embed_sorted_workspace_bytes(many["ids"], d((6, 4)))
+    assert need > 0 and embed(**many) == -8 and embed(ws=4096, nbytes=need - 1, **many) == -8 and embed(ws=4100, nbytes=need, **many) == -8
     assert embed(V=0) == 0 and embed(D=0) == 0 and embed(False, N=0) == 0
 
 
