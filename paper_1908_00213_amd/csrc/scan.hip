@@ -1,4 +1,24 @@
 // chn_gated_scan_fwd / _bwd: a gated linear recurrence over time and its gradient.
+//
+// A step maps the state affinely, h -> a h + u, and so does any run of steps: its effect is a pair (product of the decays, state from zero), and effects of
+// neighbouring runs join into one, (a, u) then (a', u') being (a' a, a' u + u').  A lane has one column (two of bfloat16 arrays) and walks through 16 steps that lie
+// in its registers; the eight waves of a block take neighbouring sixteens, a piece of 128 steps, and join their effects in LDS.  Then each wave knows its first
+// state and goes through its steps once more, out of registers.  Every element is read once and written once.  Backwards it is the same, from the last step on: the
+// gradient C that flows into a step from the next one goes on as a (dy + C); the states are computed again from one in sixteen that the forward pass keeps (1/16 of
+// 4 bytes an element; kept for every step they would cost 4).
+//
+// Pieces of one tile (64 lanes) are joined in two ways, which give a state its value in a fixed order each:
+//   - from kTiles tiles on a block walks through its tile's pieces, the state staying in its registers;
+//   - otherwise pieces are blocks of their own.  Each makes its effect known in device memory and joins those of the pieces before it in its group of 16 to the state at
+//     the group's start, which the last piece of the group before has made known.  A word is its own sign that it is there (a pattern that no value has, written
+//     before by a small launch), so nothing has to be ordered but a word's own arrival.  Pieces are drawn by tickets, so a block waits only for blocks that already run, and
+//     every wait is bounded: what has not come after kPolls looks counts as NaN.
+//
+// Bound by memory, and in the second way by how long a block holds its registers (a third of which it waits: 1.4 us for the ticket, 3.4 to 4.6 for its loads, 3 to 4 for the others'
+// words, 1.6 for its stores).  2048 x 8 x 4096 bf16 100 us forward, 160 backward (4.0 and 4.2 TB/s), 65536 x 1 x 1024 103 and 144; without the waiting it would be 92 and 78 forward.
+// Of groups of 8, 16, 32 and 64 pieces, pieces of 64, 128 and 256 steps and two or three blocks on a compute unit none was faster than these by more than 3 %, pieces of 64 a quarter
+// slower.  The walk against single pieces, both directions, us: 200 x 128 x 650 fp32 136 / 146, 256 x 64 x 2048 bf16 112 / 120, 512 x 32 x 2048 114 / 121 (512 tiles); with
+// 256 tiles 133 / 124 (1024 x 16 x 2048) and 263 / 243 (2048 x 8 x 4096): one block on a compute unit.  Results past the caches: 255 -> 249 for 2048 x 8 x 4096, 262 -> 249 for 65536 x 1 x 1024.
 #include "rows.h"
 
 #include <initializer_list>
@@ -12,6 +32,7 @@ constexpr int kWaves = 8;                      // waves of a block, at most
 constexpr int kPiece = kSteps * kWaves;        // steps of a block
 constexpr int kEach = 2;                       // pieces before its own that a wave joins
 constexpr int kGroup = kEach * kWaves;         // pieces of a group
+constexpr int kTiles = 512;                    // two blocks for each of 256 compute units
 constexpr int kPolls = 1 << 18;                // (a large part of a second: what is waited for is under way already)
 
 struct ScanArgs {
@@ -26,6 +47,7 @@ struct ScanArgs {
   int64_t len_stride;
   int len64;
   // the launch
+  int chained;                              // whether a block has one piece and hears of the state from the others, or all pieces of its tile
   int64_t subs, pieces, upr, tiles;         // waves' shares of the steps, blocks' shares; units of V columns in a row, blocks next to each other
   unsigned long long *effects;              // (piece, B, D): what a piece does to the state, the product of the decays and the state from zero
   unsigned *starts;                         // (group, B, D): the state before a group of pieces
@@ -91,20 +113,17 @@ template <> struct Few<float, 2> {
 // A wave's rows are addressed from that of its first lane: a pointer for the wave and 32 bits for a lane, whose reach the host has looked at.
 template <int V>
 struct Place {
-  int64_t b, d, end;
+  int b, d, end;                                             // (each below 2^31)
   int b0;                                                    // of the first lane
   bool live, whole;
   __device__ __forceinline__ Place(const ScanArgs &s, int64_t tile) {
-    const int64_t u = tile * 64 + (threadIdx.x & 63);
-    b = u / s.upr;
-    const int64_t j = u - b * s.upr;
-    live = b < s.B && j * V < s.D;
-    b = min(b, s.B - 1);
-    b0 = __builtin_amdgcn_readfirstlane((int)b);
-    d = j * V;
-    whole = d + V <= s.D;
-    d = whole ? d : s.D - V;
-    end = sequence_end(s, b);
+    const int64_t u = tile * 64 + (threadIdx.x & 63), row = u / s.upr, j = u - row * s.upr;
+    live = row < s.B && j * V < s.D;
+    b = (int)min(row, s.B - 1);
+    b0 = __builtin_amdgcn_readfirstlane(b);
+    whole = j * V + V <= s.D;
+    d = (int)(whole ? j * V : s.D - V);
+    end = (int)sequence_end(s, b);
   }
   template <typename T>
   __device__ __forceinline__ unsigned offset(int64_t sb) const { return (unsigned)(((b - b0) * sb + d) * (int64_t)sizeof(T)); }
@@ -128,9 +147,12 @@ __device__ __forceinline__ unsigned long long together(float a, float u) {
   return w == ~0ull ? 0x7fc000007fc00000ull : w;             // (all bits set: not there yet)
 }
 
+// One effect after another.
+__device__ __forceinline__ float2 after(float2 e, float2 f) { return make_float2(f.x * e.x, fmaf(f.x, e.y, f.y)); }
+
 template <int V>
 struct Shared {
-  float2 mine[kWaves][V][64];                                // what each wave does to the state
+  float2 mine[2][kWaves][V][64];                             // what each wave does to the state; pieces take turns, so that one barrier is enough
   float2 theirs[kWaves][V][64];                              // what the pieces before this one do, two at a time
   float start[V][64];
   unsigned ticket;
@@ -140,30 +162,28 @@ struct Shared {
 // An effect is an affine map: state -> a state + u.  `first`: the state that the walk begins with.  Waves, pieces and groups are joined in one fixed
 // order, so results do not depend on which block runs when.  A piece waits for those before it in its group and for the group's start; all
 // of them have drawn their tickets before, so their blocks run already and wait for nothing behind them.
-template <int V>
-__device__ __forceinline__ void begin_with(const ScanArgs &s, Shared<V> &sh, const Place<V> &at, int64_t piece, int waves, Vals<V> a, Vals<V> u, Vals<V> first,
+template <int V, bool CHAINED>
+__device__ __forceinline__ void begin_with(const ScanArgs &s, Shared<V> &sh, const Place<V> &at, int64_t piece, int waves, Vals<V> a, Vals<V> u, Vals<V> &first,
                                            Vals<V> &state) {
+  float2 (*mine)[V][64] = sh.mine[piece & 1];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 #pragma unroll
   for (int v = 0; v < V; ++v) {
     float f = first[v];
     asm volatile("" : "+v"(f));                              // (has been read when the others hear of this piece: its memory may be where the walk's last state goes)
-    sh.mine[wave][v][lane] = make_float2(a[v], u[v]);
+    mine[wave][v][lane] = make_float2(a[v], u[v]);
     state[v] = f;
   }
   __syncthreads();
-  if (s.pieces > 1) {
+  if constexpr (CHAINED) {
     const int64_t group = piece / kGroup;
     const int before = (int)(piece - group * kGroup);
-    const int64_t row = s.B * s.D, column = at.b * s.D + at.d;
+    const int64_t row = s.B * s.D, column = (int64_t)at.b * s.D + at.d;
     if (wave == 0 && before < kGroup - 1 && piece < s.pieces - 1) {
 #pragma unroll
       for (int v = 0; v < V; ++v) {
-        float2 e = sh.mine[0][v][lane];
-        for (int w = 1; w < waves; ++w) {
-          const float2 f = sh.mine[w][v][lane];
-          e = make_float2(f.x * e.x, fmaf(f.x, e.y, f.y));
-        }
+        float2 e = mine[0][v][lane];
+        for (int w = 1; w < waves; ++w) e = after(e, mine[w][v][lane]);
         if (at.owns(v)) __hip_atomic_store(s.effects + piece * row + column + v, together(e.x, e.y), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
       }
     }
@@ -190,229 +210,261 @@ __device__ __forceinline__ void begin_with(const ScanArgs &s, Shared<V> &sh, con
         float2 all = make_float2(1.0f, 0.0f);
 #pragma unroll
         for (int k = 0; k < kEach; ++k)
-          if (k < n) {
-            const float f = __uint_as_float((unsigned)e[k][v]);
-            all = make_float2(f * all.x, fmaf(f, all.y, __uint_as_float((unsigned)(e[k][v] >> 32))));
-          }
+          if (k < n) all = after(all, make_float2(__uint_as_float((unsigned)e[k][v]), __uint_as_float((unsigned)(e[k][v] >> 32))));
         sh.theirs[wave][v][lane] = all;
       }
     }
-    if (wave == kWaves - 1 && group > 0) {
-      const int64_t p = group * row + column;
-      unsigned e[V];
-      bool missing = true;
-      for (int polls = 0; polls < kPolls && missing; ++polls) {
-        missing = false;
-#pragma unroll
-        for (int v = 0; v < V; ++v) e[v] = __hip_atomic_load(s.starts + p + v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-#pragma unroll
-        for (int v = 0; v < V; ++v) missing |= e[v] == ~0u;
-        missing = __any(missing);
-      }
-#pragma unroll
-      for (int v = 0; v < V; ++v) sh.start[v][lane] = __uint_as_float(e[v]);
-    }
-    __syncthreads();
-#pragma unroll
-    for (int v = 0; v < V; ++v) {
-      if (group > 0) state[v] = sh.start[v][lane];
-      for (int w = 0; kEach * w < before; ++w) state[v] = fmaf(sh.theirs[w][v][lane].x, state[v], sh.theirs[w][v][lane].y);
-    }
-    if (wave == kWaves - 1 && before == kGroup - 1 && piece < s.pieces - 1) {
-      const int64_t p = (group + 1) * row + column;
+    if (before > 0) __syncthreads();
+    const bool ends = before == kGroup - 1 && piece < s.pieces - 1;   // the group ends here and another one follows
+    if (wave == kWaves - 1 && (group > 0 || ends)) {
+      // What the pieces before this one do, and this one too, is joined before the group's start is waited for: from group to group it is one
+      // load, one product and one store.
+      float2 until[V], past[V];
 #pragma unroll
       for (int v = 0; v < V; ++v) {
-        float h = state[v];
-        for (int w = 0; w < waves; ++w) h = fmaf(sh.mine[w][v][lane].x, h, sh.mine[w][v][lane].y);
-        const unsigned bits = __float_as_uint(h);
-        if (at.owns(v)) __hip_atomic_store(s.starts + p + v, bits == ~0u ? 0x7fc00000u : bits, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        float2 e = make_float2(1.0f, 0.0f);
+        for (int w = 0; kEach * w < before; ++w) e = after(e, sh.theirs[w][v][lane]);
+        until[v] = e;
+        if (ends)
+          for (int w = 0; w < waves; ++w) e = after(e, mine[w][v][lane]);
+        past[v] = e;
       }
+      unsigned e[V];
+#pragma unroll
+      for (int v = 0; v < V; ++v) e[v] = __float_as_uint(state[v]);
+      if (group > 0) {
+        const int64_t p = group * row + column;
+        bool missing = true;
+        for (int polls = 0; polls < kPolls && missing; ++polls) {
+          missing = false;
+#pragma unroll
+          for (int v = 0; v < V; ++v) e[v] = __hip_atomic_load(s.starts + p + v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+#pragma unroll
+          for (int v = 0; v < V; ++v) missing |= e[v] == ~0u;
+          missing = __any(missing);
+        }
+      }
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        const float start = __uint_as_float(e[v]);
+        const unsigned bits = __float_as_uint(fmaf(past[v].x, start, past[v].y));
+        if (ends && at.owns(v))
+          __hip_atomic_store(s.starts + (group + 1) * row + column + v, bits == ~0u ? 0x7fc00000u : bits, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        sh.start[v][lane] = fmaf(until[v].x, start, until[v].y);
+      }
+    }
+    if (group > 0) {
+      __syncthreads();
+#pragma unroll
+      for (int v = 0; v < V; ++v) state[v] = sh.start[v][lane];
+    } else {
+#pragma unroll
+      for (int v = 0; v < V; ++v)
+        for (int w = 0; kEach * w < before; ++w) state[v] = fmaf(sh.theirs[w][v][lane].x, state[v], sh.theirs[w][v][lane].y);
     }
   }
 #pragma unroll
-  for (int v = 0; v < V; ++v)
-    for (int w = 0; w < wave; ++w) state[v] = fmaf(sh.mine[w][v][lane].x, state[v], sh.mine[w][v][lane].y);
+  for (int v = 0; v < V; ++v) {
+    float h = state[v];
+    for (int w = 0; w < wave; ++w) h = fmaf(mine[w][v][lane].x, h, mine[w][v][lane].y);
+    state[v] = h;
+    if constexpr (!CHAINED) {                                // (what the next piece begins with)
+      for (int w = wave; w < waves; ++w) h = fmaf(mine[w][v][lane].x, h, mine[w][v][lane].y);
+      first[v] = h;
+    }
+  }
 }
 
-// The block's piece and tile, the pieces of all tiles in the order of the walk.
-template <int V>
-__device__ __forceinline__ void next_job(const ScanArgs &s, Shared<V> &sh, int64_t &piece, int64_t &tile) {
+// The block's tile and pieces: one piece, those of all tiles being drawn in the order of the walk, or all of the tile's, one after the other.
+template <int V, bool CHAINED>
+__device__ __forceinline__ void next_job(const ScanArgs &s, Shared<V> &sh, int64_t &piece, int64_t &end, int64_t &tile) {
   int64_t job = block_number();
-  if (s.pieces > 1) {
+  if constexpr (CHAINED) {
     if (threadIdx.x == 0) sh.ticket = __hip_atomic_fetch_add(s.ticket, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     __syncthreads();
     job = __builtin_amdgcn_readfirstlane((int)sh.ticket);    // (fewer than 2^31 jobs and blocks)
   }
   piece = job / s.tiles;
   tile = job - piece * s.tiles;
+  end = CHAINED ? piece + 1 : s.pieces;
 }
 
-template <typename TI, typename TO, int V, bool SIGMOID>
+template <typename TI, typename TO, int V, bool SIGMOID, bool CHAINED>
 __global__ __launch_bounds__(64 * kWaves, 4) void scan_fwd_kernel(ScanArgs s) {
   __shared__ Shared<V> sh;
-  int64_t piece, tile;
-  next_job(s, sh, piece, tile);
-  if (piece >= s.pieces) return;                             // (the grid's last line may be longer than the jobs)
+  int64_t piece, end, tile;
+  next_job<V, CHAINED>(s, sh, piece, end, tile);
+  if (piece >= end || piece >= s.pieces) return;             // (the grid's last line may be longer than the jobs)
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
   const Place<V> at(s, tile);
-  const int64_t sub = piece * kWaves + wave, t0 = sub * kSteps;
   const TI *g = static_cast<const TI *>(s.gate) + at.b0 * s.gb, *x = static_cast<const TI *>(s.x) + at.b0 * s.xb;
   const unsigned go = at.template offset<TI>(s.gb), xo = at.template offset<TI>(s.xb);
-  Few<TI, V> gr[kSteps], xr[kSteps];
-#pragma unroll
-  for (int i = 0; i < kSteps; ++i) {
-    const int64_t t = min(t0 + i, s.T - 1);
-    gr[i].load(moved(g + t * s.gt, go));
-    xr[i].load(moved(x + t * s.xt, xo));
-  }
-  __builtin_amdgcn_sched_barrier(0);                         // (all loads first)
-  const int n = (int)min(max(at.end - t0, (int64_t)0), (int64_t)kSteps), nt = (int)min(s.T - t0, (int64_t)kSteps);
-  Vals<V> h, first, A, U, a[kSteps], u[kSteps];
-#pragma unroll
-  for (int v = 0; v < V; ++v) {
-    first[v] = s.h0 ? s.h0[at.b * s.p0 + at.d + v] : 0.0f;
-    A[v] = 1.0f;
-    U[v] = 0.0f;
-  }
-#pragma unroll
-  for (int i = 0; i < kSteps; ++i) {
-    const bool on = i < n;
-    if (i % 2 == 0) __builtin_amdgcn_sched_barrier(0);       // (two steps at a time: more of them at once take registers that two blocks do not have)
-#pragma unroll
-    for (int v = 0; v < V; ++v) {
-      float av = gr[i].get(v), uv = xr[i].get(v);
-      if constexpr (SIGMOID) {
-        float rest;
-        gate_parts(av, av, rest);
-        uv *= rest;
-      }
-      a[i][v] = on ? av : 1.0f;
-      u[i][v] = on ? uv : 0.0f;
-      A[v] *= a[i][v];
-      U[v] = fmaf(a[i][v], U[v], u[i][v]);
-    }
-  }
-  begin_with<V>(s, sh, at, piece, waves, A, U, first, h);
-  if (t0 >= s.T) return;
-  if (s.states) at.store(s.states + (sub * s.B + at.b) * s.D + at.d, h);
-  TO *y = static_cast<TO *>(s.y) + at.b0 * s.yb + t0 * s.yt;
   const unsigned yo = at.template offset<TO>(s.yb);
+  Vals<V> first;
 #pragma unroll
-  for (int i = 0; i < kSteps; ++i) {
-    if (i >= nt) continue;
-    Vals<V> out;
+  for (int v = 0; v < V; ++v) first[v] = s.h0 ? s.h0[at.b * s.p0 + at.d + v] : 0.0f;
+  do {                                                       // (pieces of the tile, one where they are chained)
+    const int64_t sub = piece * kWaves + wave, t0 = sub * kSteps;
+    Few<TI, V> gr[kSteps], xr[kSteps];
+#pragma unroll
+    for (int i = 0; i < kSteps; ++i) {
+      const int64_t t = min(t0 + i, s.T - 1);
+      gr[i].load(moved(g + t * s.gt, go));
+      xr[i].load(moved(x + t * s.xt, xo));
+    }
+    __builtin_amdgcn_sched_barrier(0);                         // (all loads first)
+    const int n = (int)min(max(at.end - t0, (int64_t)0), (int64_t)kSteps), nt = (int)min(s.T - t0, (int64_t)kSteps);
+    Vals<V> h, A, U, a[kSteps], u[kSteps];
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-      h[v] = fmaf(a[i][v], h[v], u[i][v]);
-      out[v] = i < n ? h[v] : 0.0f;
+      A[v] = 1.0f;
+      U[v] = 0.0f;
     }
-    at.store(moved(y + i * s.yt, yo), out);
-  }
-  if (s.h_last && t0 + kSteps >= s.T) at.store(s.h_last + at.b * s.pl + at.d, h);
+#pragma unroll
+    for (int i = 0; i < kSteps; ++i) {
+      const bool on = i < n;
+      if (i % 2 == 0) __builtin_amdgcn_sched_barrier(0);       // (two steps at a time: more of them at once take registers that two blocks do not have)
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        float av = gr[i].get(v), uv = xr[i].get(v);
+        if constexpr (SIGMOID) {
+          float rest;
+          gate_parts(av, av, rest);
+          uv *= rest;
+        }
+        a[i][v] = on ? av : 1.0f;
+        u[i][v] = on ? uv : 0.0f;
+        A[v] *= a[i][v];
+        U[v] = fmaf(a[i][v], U[v], u[i][v]);
+      }
+    }
+    begin_with<V, CHAINED>(s, sh, at, piece, waves, A, U, first, h);
+    if (t0 >= s.T) return;                                   // (behind the last step, so in the last piece)
+    if (s.states) at.store(s.states + (sub * s.B + at.b) * s.D + at.d, h);
+    TO *y = static_cast<TO *>(s.y) + at.b0 * s.yb + t0 * s.yt;
+#pragma unroll
+    for (int i = 0; i < kSteps; ++i) {
+      if (i >= nt) continue;
+      Vals<V> out;
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        h[v] = fmaf(a[i][v], h[v], u[i][v]);
+        out[v] = i < n ? h[v] : 0.0f;
+      }
+      at.store(moved(y + i * s.yt, yo), out);
+    }
+    if (s.h_last && t0 + kSteps >= s.T) at.store(s.h_last + at.b * s.pl + at.d, h);
+  } while (!CHAINED && ++piece < end);
 }
 
 // Backwards: the wave whose steps are the last ones begins.  The state before each step is computed again from the one that the forward pass kept.  Of a
 // step stay three numbers and dy: the smaller of a and 1 - a (with its sign saying which one it is: the other one is 1 minus it, to half a step),
 // and what dgate has G multiplied with.
-template <typename TI, typename TO, int V, bool SIGMOID>
+template <typename TI, typename TO, int V, bool SIGMOID, bool CHAINED>
 __global__ __launch_bounds__(64 * kWaves, 4) void scan_bwd_kernel(ScanArgs s) {
   __shared__ Shared<V> sh;
-  int64_t piece, tile;
-  next_job(s, sh, piece, tile);
-  if (piece >= s.pieces) return;
+  int64_t piece, end, tile;
+  next_job<V, CHAINED>(s, sh, piece, end, tile);
+  if (piece >= end || piece >= s.pieces) return;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
   const Place<V> at(s, tile);
-  const int64_t walk = piece * kWaves + wave, sub = s.subs - 1 - walk, t0 = max(sub, (int64_t)0) * kSteps;
-  const bool any = sub >= 0;                                 // (the last block's last waves may have no steps)
   const TI *g = static_cast<const TI *>(s.gate) + at.b0 * s.gb, *x = static_cast<const TI *>(s.x) + at.b0 * s.xb;
   const TO *dy = static_cast<const TO *>(s.dy) + at.b0 * s.yb;
   const unsigned go = at.template offset<TI>(s.gb), xo = at.template offset<TI>(s.xb), yo = at.template offset<TO>(s.yb);
-  Few<TI, V> gr[kSteps], xr[kSteps];
-  Few<TO, V> yr[kSteps];
-  Vals<V> h, first, A, U, part[kSteps], coef[kSteps];
+  Vals<V> first;
 #pragma unroll
-  for (int i = 0; i < kSteps; ++i) {
-    const int64_t t = min(t0 + i, s.T - 1);
-    gr[i].load(moved(g + t * s.gt, go));
-    xr[i].load(moved(x + t * s.xt, xo));
-    yr[i].load(moved(dy + t * s.yt, yo));
-  }
-  const int n = any ? (int)min(max(at.end - t0, (int64_t)0), (int64_t)kSteps) : 0, nt = (int)min(s.T - t0, (int64_t)kSteps);
+  for (int v = 0; v < V; ++v) first[v] = s.dh_last ? s.dh_last[at.b * s.pl + at.d + v] : 0.0f;
+  do {                                                       // (pieces of the tile, one where they are chained)
+    const int64_t walk = piece * kWaves + wave, sub = s.subs - 1 - walk, t0 = max(sub, (int64_t)0) * kSteps;
+    const bool any = sub >= 0;                                 // (the last block's last waves may have no steps)
+    Few<TI, V> gr[kSteps], xr[kSteps];
+    Few<TO, V> yr[kSteps];
+    Vals<V> h, A, U, part[kSteps], coef[kSteps];
 #pragma unroll
-  for (int v = 0; v < V; ++v) {
-    first[v] = s.dh_last ? s.dh_last[at.b * s.pl + at.d + v] : 0.0f;
-    h[v] = s.states[((t0 / kSteps) * s.B + at.b) * s.D + at.d + v];
-  }
-  __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-  for (int i = 0; i < kSteps; ++i) {
-    const bool on = i < n;
-    if (i % 2 == 0) __builtin_amdgcn_sched_barrier(0);
+    for (int i = 0; i < kSteps; ++i) {
+      const int64_t t = min(t0 + i, s.T - 1);
+      gr[i].load(moved(g + t * s.gt, go));
+      xr[i].load(moved(x + t * s.xt, xo));
+      yr[i].load(moved(dy + t * s.yt, yo));
+    }
+    const int n = any ? (int)min(max(at.end - t0, (int64_t)0), (int64_t)kSteps) : 0, nt = (int)min(s.T - t0, (int64_t)kSteps);
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-      const float xv = xr[i].get(v);
-      float a = gr[i].get(v);
-      if constexpr (SIGMOID) {
-        float rest;
-        const bool upper = a >= 0.0f;
-        gate_parts(a, a, rest);
-        float c = on ? (h[v] - xv) * (a * rest) : 0.0f;
-        asm volatile("" : "+v"(c));                          // (worked out here: where it is used it would keep four numbers alive until then)
-        coef[i][v] = c;
-        part[i][v] = on ? (upper ? -rest : a) : -0.0f;
-        h[v] = fmaf(a, h[v], rest * xv);
-      } else {
-        coef[i][v] = on ? h[v] : 0.0f;
-        part[i][v] = on ? a : 1.0f;
-        h[v] = fmaf(a, h[v], xv);
+      h[v] = s.states[((t0 / kSteps) * s.B + at.b) * s.D + at.d + v];
+    }
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int i = 0; i < kSteps; ++i) {
+      const bool on = i < n;
+      if (i % 2 == 0) __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        const float xv = xr[i].get(v);
+        float a = gr[i].get(v);
+        if constexpr (SIGMOID) {
+          float rest;
+          const bool upper = a >= 0.0f;
+          gate_parts(a, a, rest);
+          float c = on ? (h[v] - xv) * (a * rest) : 0.0f;
+          asm volatile("" : "+v"(c));                          // (worked out here: where it is used it would keep four numbers alive until then)
+          coef[i][v] = c;
+          part[i][v] = on ? (upper ? -rest : a) : -0.0f;
+          h[v] = fmaf(a, h[v], rest * xv);
+        } else {
+          float c = on ? h[v] : 0.0f, q = on ? a : 1.0f;
+          asm volatile("" : "+v"(c), "+v"(q));
+          coef[i][v] = c;
+          part[i][v] = q;
+          h[v] = fmaf(a, h[v], xv);
+        }
       }
     }
-  }
-  auto decay = [](float q) {
-    return !SIGMOID ? q : __float_as_int(q) < 0 ? 1.0f + q : q;
-  };
-#pragma unroll
-  for (int v = 0; v < V; ++v) {
-    A[v] = 1.0f;
-    U[v] = 0.0f;
-  }
-#pragma unroll
-  for (int i = kSteps - 1; i >= 0; --i) {
-    if (i % 2) __builtin_amdgcn_sched_barrier(0);
+    auto decay = [](float q) {
+      return !SIGMOID ? q : __float_as_int(q) < 0 ? 1.0f + q : q;
+    };
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-      const float a = decay(part[i][v]), d = i < n ? yr[i].get(v) : 0.0f;
-      A[v] *= a;
-      U[v] = a * (U[v] + d);
+      A[v] = 1.0f;
+      U[v] = 0.0f;
     }
-  }
-  __builtin_amdgcn_sched_barrier(0);
-  Vals<V> G;
-  begin_with<V>(s, sh, at, piece, waves, A, U, first, G);
-  if (!any) return;
-  TI *dg = static_cast<TI *>(s.dgate) + at.b0 * s.hb + t0 * s.ht, *dx = static_cast<TI *>(s.dx) + at.b0 * s.ub + t0 * s.ut;
-  const unsigned dgo = at.template offset<TI>(s.hb), dxo = at.template offset<TI>(s.ub);
 #pragma unroll
-  for (int i = kSteps - 1; i >= 0; --i) {
-    if (i >= nt) continue;
-    const bool on = i < n;
-    Vals<V> vg, vx;
-    if constexpr (sizeof(TO) == 2) asm volatile("" : "+v"(yr[i].r));   // (taken apart again, not kept apart)
+    for (int i = kSteps - 1; i >= 0; --i) {
+      if (i % 2) __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-    for (int v = 0; v < V; ++v) {
-      float q = part[i][v];
-      asm volatile("" : "+v"(q));                            // (what is worked out from it is neither kept from above nor begun early, in registers that are not there)
-      const float a = decay(q);
-      if (on) G[v] += yr[i].get(v);
-      vg[v] = on ? coef[i][v] * G[v] : 0.0f;
-      const float rest = !SIGMOID ? 1.0f : __float_as_int(q) < 0 ? -q : 1.0f - q;
-      vx[v] = on ? rest * G[v] : 0.0f;
-      G[v] *= a;
+      for (int v = 0; v < V; ++v) {
+        const float a = decay(part[i][v]), d = i < n ? yr[i].get(v) : 0.0f;
+        A[v] *= a;
+        U[v] = a * (U[v] + d);
+      }
     }
-    at.store(moved(dg + i * s.ht, dgo), vg);
-    at.store(moved(dx + i * s.ut, dxo), vx);
-  }
-  if (s.dh0 && sub == 0) at.store(s.dh0 + at.b * s.p0 + at.d, G);
+    __builtin_amdgcn_sched_barrier(0);
+    Vals<V> G;
+    begin_with<V, CHAINED>(s, sh, at, piece, waves, A, U, first, G);
+    if (!any) return;                                        // (before the first step, so in the last piece)
+    TI *dg = static_cast<TI *>(s.dgate) + at.b0 * s.hb + t0 * s.ht, *dx = static_cast<TI *>(s.dx) + at.b0 * s.ub + t0 * s.ut;
+    const unsigned dgo = at.template offset<TI>(s.hb), dxo = at.template offset<TI>(s.ub);
+#pragma unroll
+    for (int i = kSteps - 1; i >= 0; --i) {
+      if (i >= nt) continue;
+      const bool on = i < n;
+      Vals<V> vg, vx;
+      if constexpr (sizeof(TO) == 2) asm volatile("" : "+v"(yr[i].r));   // (taken apart again, not kept apart)
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        float q = part[i][v];
+        asm volatile("" : "+v"(q));                            // (what is worked out from it is neither kept from above nor begun early, in registers that are not there)
+        const float a = decay(q);
+        if (on) G[v] += yr[i].get(v);
+        vg[v] = on ? coef[i][v] * G[v] : 0.0f;
+        const float rest = !SIGMOID ? 1.0f : __float_as_int(q) < 0 ? -q : 1.0f - q;
+        vx[v] = on ? rest * G[v] : 0.0f;
+        G[v] *= a;
+      }
+      at.store(moved(dg + i * s.ht, dgo), vg);
+      at.store(moved(dx + i * s.ut, dxo), vx);
+    }
+    if (s.dh0 && sub == 0) at.store(s.dh0 + at.b * s.p0 + at.d, G);
+  } while (!CHAINED && ++piece < end);
 }
 
 // Nothing is there yet, no ticket drawn.
@@ -460,9 +512,10 @@ bool far_apart(int64_t B, int64_t D, int V, std::initializer_list<int64_t> strid
 // The launch that both directions share: clears the workspace where pieces wait for each other.
 chn_status lay_out(const Sizes &z, void *ws, hipStream_t st, ScanArgs *s, dim3 *grid, dim3 *block) {
   s->subs = z.subs; s->pieces = z.pieces; s->upr = z.upr; s->tiles = z.tiles;
-  *grid = grid_of(z.jobs);
+  s->chained = z.pieces > 1 && z.tiles < kTiles;
+  *grid = grid_of(s->chained ? z.jobs : z.tiles);
   *block = dim3(64 * (unsigned)(z.subs < kWaves ? z.subs : kWaves));
-  if (z.pieces > 1) {
+  if (s->chained) {
     char *p = static_cast<char *>(ws);
     s->ticket = reinterpret_cast<unsigned *>(p);
     s->effects = reinterpret_cast<unsigned long long *>(p + 256);
@@ -580,8 +633,10 @@ chn_status chn_gated_scan_fwd(int kind, const chn_array *gate, const chn_array *
   CHN_TRY(lay_out(z, ws, st, &s, &grid, &block));
 #define CHN_GO(TI, TO, V_)                                                                                                      \
   do {                                                                                                                          \
-    if (kind == CHN_SCAN_SIGMOID) hipLaunchKernelGGL((scan_fwd_kernel<TI, TO, V_, true>), grid, block, 0, st, s);                 \
-    else hipLaunchKernelGGL((scan_fwd_kernel<TI, TO, V_, false>), grid, block, 0, st, s);                                         \
+    if (kind == CHN_SCAN_SIGMOID && s.chained) hipLaunchKernelGGL((scan_fwd_kernel<TI, TO, V_, true, true>), grid, block, 0, st, s);   \
+    else if (kind == CHN_SCAN_SIGMOID) hipLaunchKernelGGL((scan_fwd_kernel<TI, TO, V_, true, false>), grid, block, 0, st, s);          \
+    else if (s.chained) hipLaunchKernelGGL((scan_fwd_kernel<TI, TO, V_, false, true>), grid, block, 0, st, s);                         \
+    else hipLaunchKernelGGL((scan_fwd_kernel<TI, TO, V_, false, false>), grid, block, 0, st, s);                                       \
   } while (0)
   if (gate->dtype == CHN_F32) { if (y->dtype == CHN_F32) CHN_GO(float, float, 1); else CHN_GO(float, bf16_raw, 1); }
   else if (V == 2) { if (y->dtype == CHN_F32) CHN_GO(bf16_raw, float, 2); else CHN_GO(bf16_raw, bf16_raw, 2); }
@@ -617,8 +672,10 @@ chn_status chn_gated_scan_bwd(int kind, const chn_array *gate, const chn_array *
   CHN_TRY(lay_out(z, ws, st, &s, &grid, &block));
 #define CHN_GO(TI, TO, V_)                                                                                                      \
   do {                                                                                                                          \
-    if (kind == CHN_SCAN_SIGMOID) hipLaunchKernelGGL((scan_bwd_kernel<TI, TO, V_, true>), grid, block, 0, st, s);                 \
-    else hipLaunchKernelGGL((scan_bwd_kernel<TI, TO, V_, false>), grid, block, 0, st, s);                                         \
+    if (kind == CHN_SCAN_SIGMOID && s.chained) hipLaunchKernelGGL((scan_bwd_kernel<TI, TO, V_, true, true>), grid, block, 0, st, s);   \
+    else if (kind == CHN_SCAN_SIGMOID) hipLaunchKernelGGL((scan_bwd_kernel<TI, TO, V_, true, false>), grid, block, 0, st, s);          \
+    else if (s.chained) hipLaunchKernelGGL((scan_bwd_kernel<TI, TO, V_, false, true>), grid, block, 0, st, s);                         \
+    else hipLaunchKernelGGL((scan_bwd_kernel<TI, TO, V_, false, false>), grid, block, 0, st, s);                                       \
   } while (0)
   if (gate->dtype == CHN_F32) { if (dy->dtype == CHN_F32) CHN_GO(float, float, 1); else CHN_GO(float, bf16_raw, 1); }
   else if (V == 2) CHN_GO(bf16_raw, bf16_raw, 2);

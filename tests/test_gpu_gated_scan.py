@@ -122,6 +122,14 @@ def test_scan_of_wide_batches(Bn, D):
     check(20, Bn, D, "decay", "bf16", "bf16", lengths=list(np.arange(Bn) % 22), batch_first=True)
 
 
+def test_scan_of_many_tiles_and_pieces():
+    """More than 512 tiles: a block walks through the pieces of its tile."""
+    Bn, D = 1000, 66
+    check(261, Bn, D, "sigmoid", "f32", "f32", lengths=list(np.arange(Bn) % 270), same=True)
+    check(261, Bn, D, "decay", "bf16", "bf16", batch_first=True, pad=1)
+    check(130, 1100, 65, "sigmoid", "bf16", "f32", same=True)
+
+
 def test_halves_of_one_product_and_repeated_gates():
     T, Bn, D = 200, 3, 50
     gate, x, first, _, _ = inputs(T, Bn, D, "sigmoid", "f32", 5)
