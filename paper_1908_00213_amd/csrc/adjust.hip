@@ -4,6 +4,11 @@
 // often it stands behind the prompt, whether the prompt has it, whether it has a bias), then walks over the piece once: a read and a write for each logit.
 // Whole numbers are counted, so the order in which the list is seen does not show.  The few tokens with biases are left out by that walk: the threads
 // that hold the list's entries write them, each token by the thread with its first entry, which adds up the others in the list's order.
+//
+// Bound by memory where the launch fills the chip: 256 x 131072 fp32 with lists of up to 8192 tokens, 300 biases and masks 67 us (4.1 TB/s), without any of them 40 (a plain copy 37,
+// part of it in the last-level cache).  A block's chain of waits is what costs beside that, so the logits, the masks and the list's first part are fetched before anything is
+// counted, and four blocks of 512 threads with 16 logits each share a compute unit (two with 32 each: 80).  Biases of one id that stands twice were 40 us more while every
+// thread looked through the whole list for its id: they are put in order in LDS first.
 #include "rows.h"
 
 namespace chn {
@@ -303,7 +308,10 @@ chn_status chn_logits_adjust(const chn_array *logits, const chn_array *tokens, c
   }
   if (bias && a.M > 0) { a.bias = static_cast<const float *>(bias->data); a.bias_ids = bias_ids->data; }
   const int E = logits->dtype == CHN_F32 && out->dtype == CHN_F32 ? 4 : 8;
-  const bool large = a.V * N >= 512ll * kThreads * kHeld;
+// From 2^21 logits on in rows of two large pieces and more a thread holds kHeld logits, below one unit (us: 16 x 131072 with lists of 8192 tokens 9.4 / 13.4, 64 x 32768 8.4 / 9.8,
+  // 128 x 65536 18.7 / 25.0, 256 x 32768 22.4 / 37.7; 8 x 131072 7.7 / 6.7, 1 x 131072 7.1 / 5.3, and of rows that leave a large piece mostly empty 256 x 10000 14.3 / 11.1): the
+  // list is looked through once for a piece.
+  const bool large = a.V * N >= 1 << 21 && a.V >= 2 * kThreads * kHeld;
   const int threads = large ? kThreads : 256;
   a.tile = threads * (large ? kHeld : E);
   a.tiles = (a.V + a.tile - 1) / a.tile;

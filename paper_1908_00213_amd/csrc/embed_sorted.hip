@@ -1,4 +1,15 @@
 // chn_embed_scaled_fwd / chn_embed_sorted_bwd: the lookup with its scale, and the table's gradient.
+//
+// The gradient sums rows of dout by token.  The ids are sorted (which keeps a token's places in the order of n), and then
+//   - a wave for a row of the table (several rows of a large table, 64 units of columns) adds up the rows of its token, or writes zeros;
+//   - tokens with more than 64 places are summed by pieces of 64 places of the sorted list, and these sums joined in a launch of its own: a word that is every tenth of a
+//     text would otherwise be one wave's work.
+// Every order is fixed by the ids alone.  Up to 256 ids are not sorted: every wave looks for its rows' tokens among them (1 x 650 into 10000 rows 21 -> 9 us, 128 ids 21 -> 9;
+// 512 ids 18 with the sort, 25 without).
+//
+// Bound by memory for a large table: 65536 x 1024 bf16 into 131072 rows 30 us for the lookup (4.5 TB/s of its output), 158 for the gradient, of which clearing 537 MB takes 100 (5.3 TB/s)
+// while a few blocks sort beside it, and sums 40.  Cleared by the launch that sums, it was 31 us for the sort alone and 146 for the sums.  Stores past the caches: what
+// follows does not wait for their lines to leave (the lookup 41 us and the sums 58 with ordinary stores).  Small cases are launches: 4480 x 650 into 10000 rows 14 (one block sorts), 13 and 5 traced.
 #include "rows.h"
 
 namespace chn {
@@ -633,7 +644,7 @@ chn_status chn_embed_sorted_bwd(const chn_array *ids, const chn_array *dout, dou
   s.dout = dout->data; s.dtable = static_cast<float *>(dtable->data);
   s.dp = dp; s.tp = tp; s.V = V; s.D = D; s.chunks = (D + 64 * E - 1) / (64 * E);
   s.scale = (float)scale; s.N = (uint32_t)N; s.accumulate = accumulate;
-  const int64_t each = V * s.chunks / 8192;                  // (as many waves as run at once: each waits for its rows' tokens)
+  const int64_t each = V * s.chunks / 8192;                  // (about as many waves as run at once: with one row each, 4480 x 650 into 10000 rows 16.5 us, 12.7 like this)
   s.rows = (int)(each < 1 ? 1 : each > 16 ? 16 : each);
   const int64_t row_jobs = (V + s.rows - 1) / s.rows * s.chunks;
   hipStream_t st = as_stream(stream);

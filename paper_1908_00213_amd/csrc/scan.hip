@@ -33,7 +33,7 @@ constexpr int kPiece = kSteps * kWaves;        // steps of a block
 constexpr int kEach = 2;                       // pieces before its own that a wave joins
 constexpr int kGroup = kEach * kWaves;         // pieces of a group
 constexpr int kTiles = 512;                    // two blocks for each of 256 compute units
-constexpr int kPolls = 1 << 18;                // (a large part of a second: what is waited for is under way already)
+constexpr int kPolls = 1 << 20;                // (a second: what is waited for is under way already)
 
 struct ScanArgs {
   const void *gate, *x, *dy;
@@ -608,7 +608,8 @@ size_t chn_gated_scan_workspace_bytes(const chn_array *gate) {
   if (!gate || gate->ndim != 3 || !is_float(gate->dtype)) return 0;
   for (int k = 0; k < 3; ++k)
     if (gate->shape[k] <= 0 || gate->shape[k] > 0x7fffffff) return 0;
-  return Sizes(gate->shape[0], gate->shape[1], gate->shape[2], 1, false).bytes;
+  const Sizes z(gate->shape[0], gate->shape[1], gate->shape[2], columns(gate->dtype, CHN_BF16, gate->shape[2]), false);
+  return z.tiles < kTiles ? z.bytes : 0;                     // (fewer columns for a lane, or rows apart, make more tiles)
 }
 
 chn_status chn_gated_scan_fwd(int kind, const chn_array *gate, const chn_array *x, const chn_array *h0, const chn_array *lengths, const chn_array *y,

@@ -38,7 +38,7 @@ def gradient(ids, dout, v, scale, accumulate=False, pad=0, shift=0, stride=1, dt
 
 
 SIZES = [(1, 1, 1), (1, 5, 3), (3, 4, 1), (63, 8, 7), (64, 1, 64), (65, 2, 65), (100, 33, 257), (257, 16, 255), (1000, 650, 100), (4096, 12, 513), (5000, 9, 3), (9001, 66, 1000),
-         (70000, 5, 70000), (33000, 130, 300), (20000, 3, 200000)]
+         (70000, 5, 70000), (33000, 130, 300), (20000, 3, 200000), (9001, 2, 300000), (5000, 2, 300000)]
 
 
 @pytest.mark.parametrize("kind", ["words", "all equal", "outside", "none", "even"])

@@ -193,6 +193,33 @@ def test_nan_and_infinity_stay_in_their_column_and_sequence():
     assert np.isfinite(got).all()
 
 
+@pytest.mark.parametrize("D", [2, 3])
+def test_sequences_further_apart_than_32_bits(D):
+    """66 sequences, 2^25 elements and more from one to the next, everything interleaved in one block of memory."""
+    T, Bn, apart = 150, 66, (1 << 25) + 24
+    buf = torch.empty(Bn * apart, device="cuda", dtype=torch.bfloat16)
+    view = lambda k: buf.as_strided((T, Bn, D), (20, apart, 1), k * D)
+    gate, x, first, dy, dlast = inputs(T, Bn, D, "sigmoid", "bf16", 4)
+    dy = rounded(dy, "bf16")
+    g, xx, dyd, y, dg, dx = (view(k) for k in range(6))
+    for v, a in ((g, gate), (xx, x), (dyd, dy)):
+        v.copy_(torch.from_numpy(a).cuda())
+    ws = workspace(g)
+    st, hl, d0 = torch.empty(B.gated_scan_states_shape(T, Bn, D), device="cuda"), torch.empty(Bn, D, device="cuda"), torch.empty(Bn, D, device="cuda")
+    B.gated_scan_fwd(g, xx, y, h0=dev(first), h_last=hl, states=st, ws=ws)
+    B.gated_scan_bwd(g, xx, st, dyd, dg, dx, dh_last=dev(dlast), dh0=d0, ws=ws)
+    got = [values(v) for v in (y, hl, dg, dx, d0)]
+    near = lambda a: torch.from_numpy(a).cuda().bfloat16()
+    g, xx, dyd = near(gate), near(x), near(dy)
+    y, dg, dx, hl, d0 = (torch.empty_like(v) for v in (g, g, g, hl, d0))
+    B.gated_scan_fwd(g, xx, y, h0=dev(first), h_last=hl, states=st, ws=ws)
+    B.gated_scan_bwd(g, xx, st, dyd, dg, dx, dh_last=dev(dlast), dh0=d0, ws=ws)
+    for a, b in zip(got, (y, hl, dg, dx, d0)):
+        assert np.array_equal(a, values(b))
+    want, _, bound = R.gated_scan(gate, x, first, "sigmoid")
+    close(got[0], want, bound[1:] + HALF["bf16"] * (np.abs(want) + bound[1:]))
+
+
 def test_no_steps_no_columns():
     h0 = torch.randn(3, 5, device="cuda")
     e = torch.empty(0, 3, 5, device="cuda")
