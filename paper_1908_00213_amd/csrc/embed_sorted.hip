@@ -220,6 +220,7 @@ __global__ __launch_bounds__(1024) void embed_sort_kernel(SortArgs s) {
 __global__ __launch_bounds__(1024) void embed_sort_few_kernel(SortArgs s, int passes) {
   __shared__ SortShared sh;
   __shared__ uint2 pairs[kFew];
+  static_assert(kFew % 1024 == 0, "pairs of a thread");
   constexpr int M = kFew / 1024;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const uint32_t mask = (1u << s.bits) - 1, part = ((s.N + kSortWaves - 1) / kSortWaves + 63) / 64 * 64;
@@ -548,7 +549,7 @@ struct Layout {
     while (whole < 32 && (V >> whole)) ++whole;              // keys are 0 .. V
     passes = (whole + kMaxBits - 1) / kMaxBits;
     bits = (whole + passes - 1) / passes;
-    blocks = (int)(N <= kFew ? 1 : N / 2048 < 64 ? N / 2048 : 64);
+    blocks = (int)(N <= kFew ? 1 : N < 2 * 2048 ? 2 : N / 2048 < 64 ? N / 2048 : 64);   // (one block: its kernel takes no more than kFew)
     share = (uint32_t)((N + blocks - 1) / blocks);
     pieces = (N + kPiece - 1) / kPiece;
     pitch = (D + 7) / 8 * 8;
