@@ -270,6 +270,31 @@ def test_another_stream_and_a_captured_graph():
         assert all(torch.equal(a, b) for a, b in zip(got, want)), k
 
 
+def test_two_streams_at_once():
+    """Two recurrences whose pieces wait for each other, and products beside them: more blocks than run at once."""
+    T, Bn, D = 6000, 4, 1024
+    gate, x, first, _, _ = inputs(T, Bn, D, "sigmoid", "bf16", 7)
+    g, xx, f = steps(gate, "bf16"), steps(x, "bf16"), dev(first)
+    want, ws = torch.empty_like(g), workspace(g)
+    B.gated_scan_fwd(g, xx, want, h0=f, ws=ws)
+    streams = [torch.cuda.Stream() for _ in range(3)]
+    outs, spaces = [torch.empty_like(g) for _ in range(2)], [workspace(g) for _ in range(2)]
+    m = torch.randn(2048, 2048, device="cuda")
+    for k in range(5):
+        torch.cuda.synchronize()
+        for o in outs:
+            o.zero_()
+        torch.cuda.synchronize()
+        for _ in range(3):
+            for s, o, w in zip(streams, outs, spaces):
+                with torch.cuda.stream(s):
+                    B.gated_scan_fwd(g, xx, o, h0=f, ws=w)
+            with torch.cuda.stream(streams[2]):
+                torch.mm(m, m)
+        torch.cuda.synchronize()
+        assert all(torch.equal(o, want) for o in outs), k
+
+
 def test_gradients_against_differences():
     """Differences of the fp32 results: a step of 2^-6 is off by its square times third derivatives below 1, and by 2 roundings of the sum over its size."""
     T, Bn, D = 40, 2, 3
