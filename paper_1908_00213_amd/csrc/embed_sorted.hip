@@ -127,13 +127,15 @@ struct SortShared {
 
 // The lanes whose digit is this lane's.
 __device__ __forceinline__ unsigned long long equals(bool on, uint32_t digit, int bits) {
-  unsigned long long same = __ballot(on);
+  const unsigned long long all = __ballot(on);
+  uint32_t low = (uint32_t)all, high = (uint32_t)(all >> 32);
   for (int b = 0; b < bits; ++b) {
-    const bool bit = digit >> b & 1;
+    const int bit = (int)(digit << (31 - b)) >> 31;          // all ones where it is set
     const unsigned long long m = __ballot(bit);
-    same &= bit ? m : ~m;
+    low &= ~((uint32_t)m ^ bit);
+    high &= ~((uint32_t)(m >> 32) ^ bit);
   }
-  return same;
+  return (unsigned long long)high << 32 | low;
 }
 
 // What the wave's lanes have written to LDS is what its lanes read from here on.
