@@ -17,7 +17,7 @@
 // Bound by memory, and in the second way by how long a block holds its registers (a third of which it waits: 1.4 us for the ticket, 3.4 to 4.6 for its loads, 3 to 4 for the others'
 // words, 1.6 for its stores).  2048 x 8 x 4096 bf16 100 us forward, 160 backward (4.0 and 4.2 TB/s), 65536 x 1 x 1024 103 and 144; without the waiting it would be 92 and 78 forward.
 // Of groups of 8, 16, 32 and 64 pieces, pieces of 64, 128 and 256 steps and two or three blocks on a compute unit none was faster than these by more than 3 %, pieces of 64 a quarter
-// slower.  The walk against single pieces, both directions, us: 200 x 128 x 650 fp32 136 / 146, 256 x 64 x 2048 bf16 112 / 120, 512 x 32 x 2048 114 / 121 (512 tiles); with
+// slower; tiles dealt out over the XCDs, with tickets for each: 777 x 5 x 1001 43.5 -> 40.8, 65536 x 1 x 1024 245 -> 284 (a stripe of every row for an XCD, few channels of its L2).  The walk against single pieces, both directions, us: 200 x 128 x 650 fp32 136 / 146, 256 x 64 x 2048 bf16 112 / 120, 512 x 32 x 2048 114 / 121 (512 tiles); with
 // 256 tiles 133 / 124 (1024 x 16 x 2048) and 263 / 243 (2048 x 8 x 4096): one block on a compute unit.  Results past the caches: 255 -> 249 for 2048 x 8 x 4096, 262 -> 249 for 65536 x 1 x 1024.
 #include "rows.h"
 
