@@ -148,6 +148,29 @@ def test_halves_of_one_product_and_repeated_gates():
         close(values(y), want, bound[1:] + R.U * np.abs(want))
 
 
+@pytest.mark.parametrize("T", [1, 40, 700])
+def test_states_inside_wider_rows(T):
+    """First and last states as columns of a wider array, the last one in the first one's place; the columns beside them stay."""
+    Bn, D = 3, 37
+    gate, x, first, dy, dlast = inputs(T, Bn, D, "sigmoid", "f32", 11)
+    dy = np.float32(dy)
+    want, states, bound = R.gated_scan(gate, x, first, "sigmoid")
+    (_, _, w0), (_, _, b0) = R.gated_scan_bwd(gate, x, first, dy, dlast, "sigmoid")
+    wide = torch.full((Bn, D + 6), 7.0, device="cuda")
+    h = wide[:, 2:D + 2]
+    h.copy_(dev(first))
+    g, xx = dev(gate), dev(x)
+    y, st = torch.empty_like(g), torch.empty(B.gated_scan_states_shape(T, Bn, D), device="cuda")
+    ws = workspace(g)
+    B.gated_scan_fwd(g, xx, y, h0=h, h_last=h, states=st, ws=ws)
+    close(values(y), want, bound[1:] + R.U * np.abs(want))
+    close(values(h), states[T], bound[T] + 1e-36)
+    h.copy_(dev(dlast))
+    B.gated_scan_bwd(g, xx, st, dev(dy), torch.empty_like(g), torch.empty_like(g), dh_last=h, dh0=h, ws=ws)
+    close(values(h), w0, b0 + 1e-36)
+    assert (wide[:, :2] == 7).all() and (wide[:, D + 2:] == 7).all()
+
+
 def test_gates_at_the_ends_of_the_range():
     big = np.float32(3e38)
     g = np.array([0, 1e-30, 20, -20, 88, -88, 104, -104, 1000, -1000, big, -big, np.inf, -np.inf], np.float32)
