@@ -275,26 +275,31 @@ __device__ __forceinline__ void begin_with(const ScanArgs &s, Shared<V> &sh, con
   }
 }
 
-// The block's tile and pieces: one piece, those of all tiles being drawn in the order of the walk, or all of the tile's, one after the other.
+// The block's tile and pieces: one piece, those of all tiles being drawn in the order of the walk, or all of the tile's, one after the other.  False for the
+// blocks that the grid's last line has beyond the jobs.
 template <int V, bool CHAINED>
-__device__ __forceinline__ void next_job(const ScanArgs &s, Shared<V> &sh, int64_t &piece, int64_t &end, int64_t &tile) {
-  int64_t job = block_number();
+__device__ __forceinline__ bool next_job(const ScanArgs &s, Shared<V> &sh, int64_t &piece, int64_t &end, int64_t &tile) {
   if constexpr (CHAINED) {
     if (threadIdx.x == 0) sh.ticket = __hip_atomic_fetch_add(s.ticket, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     __syncthreads();
-    job = __builtin_amdgcn_readfirstlane((int)sh.ticket);    // (fewer than 2^31 jobs and blocks)
+    const int64_t job = __builtin_amdgcn_readfirstlane((int)sh.ticket);   // (fewer than 2^31 jobs and blocks)
+    piece = job / s.tiles;
+    tile = job - piece * s.tiles;
+    end = piece + 1;
+    return piece < s.pieces;
+  } else {
+    piece = 0;
+    tile = block_number();
+    end = s.pieces;
+    return tile < s.tiles;
   }
-  piece = job / s.tiles;
-  tile = job - piece * s.tiles;
-  end = CHAINED ? piece + 1 : s.pieces;
 }
 
 template <typename TI, typename TO, int V, bool SIGMOID, bool CHAINED>
 __global__ __launch_bounds__(64 * kWaves, 4) void scan_fwd_kernel(ScanArgs s) {
   __shared__ Shared<V> sh;
   int64_t piece, end, tile;
-  next_job<V, CHAINED>(s, sh, piece, end, tile);
-  if (piece >= end || piece >= s.pieces) return;             // (the grid's last line may be longer than the jobs)
+  if (!next_job<V, CHAINED>(s, sh, piece, end, tile)) return;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
   const Place<V> at(s, tile);
   const TI *g = static_cast<const TI *>(s.gate) + at.b0 * s.gb, *x = static_cast<const TI *>(s.x) + at.b0 * s.xb;
@@ -364,8 +369,7 @@ template <typename TI, typename TO, int V, bool SIGMOID, bool CHAINED>
 __global__ __launch_bounds__(64 * kWaves, 4) void scan_bwd_kernel(ScanArgs s) {
   __shared__ Shared<V> sh;
   int64_t piece, end, tile;
-  next_job<V, CHAINED>(s, sh, piece, end, tile);
-  if (piece >= end || piece >= s.pieces) return;
+  if (!next_job<V, CHAINED>(s, sh, piece, end, tile)) return;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
   const Place<V> at(s, tile);
   const TI *g = static_cast<const TI *>(s.gate) + at.b0 * s.gb, *x = static_cast<const TI *>(s.x) + at.b0 * s.xb;
