@@ -529,9 +529,10 @@ chn_status chn_logits_adjust(const chn_array *logits, const chn_array *tokens, c
  *   CHN_SCAN_DECAY    dx_t = G_t             dgate_t = h_{t-1} G_t
  *   dh0 = a_1 G_1, (B,D) F32 or NULL
  * dy: F32 or BF16; dgate, dx: the type of gate; behind a sequence's end they are 0.
- * States and gradients are fp32, results the same bits from run to run.  Sequences of more than 16 steps are cut in stretches, whose effect is
- * (the product of the decays, the state from zero): where the product over up to 2048 steps leaves fp32's range (decays above 1), so does the result, and an infinite state may
- * turn into NaN.  A NaN or an infinity stays in its column of its sequence.
+ * States and gradients are fp32, results the same bits from run to run.  Sequences of more than 16 steps are cut in stretches of that many, whose effect is
+ * (the product of the decays, the state from zero): where the product over 16 steps leaves fp32's range (decays above 256), so does the result, NaN where the state was 0, and an
+ * infinite state may turn into NaN.  A product over up to 2048 steps that falls below the normal range is off by 2^-149, so what is left of a state may be by that part of it.
+ * A NaN or an infinity stays in its column of its sequence.
  * An output may be the very array of an input (h_last of h0, y of x, dgate of gate, dx of x or dy).
  * T = 0 copies the state.  T and B below 2^31, D below 2^30, B * D up to 2^40 (CHN_ERR_SHAPE).
  * ws: chn_gated_scan_workspace_bytes(gate) bytes, 256-byte aligned, the library's until the work on `stream` is done; the backward pass may use the same. */

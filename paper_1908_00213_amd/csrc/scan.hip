@@ -142,13 +142,22 @@ __device__ __forceinline__ T *moved(T *p, unsigned bytes) {
   return reinterpret_cast<T *>(reinterpret_cast<char *>(const_cast<std::remove_const_t<T> *>(p)) + (uint64_t)bytes);
 }
 
-__device__ __forceinline__ unsigned long long together(float a, float u) {
-  const unsigned long long w = (unsigned long long)__float_as_uint(u) << 32 | __float_as_uint(a);
-  return w == ~0ull ? 0x7fc000007fc00000ull : w;             // (all bits set: not there yet)
-}
+// (never all bits set, which is the sign of a word that is not there yet: a is finite or kBehind)
+__device__ __forceinline__ unsigned long long together(unsigned a, float u) { return (unsigned long long)__float_as_uint(u) << 32 | a; }
 
 // One effect after another.
 __device__ __forceinline__ float2 after(float2 e, float2 f) { return make_float2(f.x * e.x, fmaf(f.x, e.y, f.y)); }
+
+// Whether an effect says what it does to every state: a product of decays beyond fp32's range does not, not even to a state of zero.  Effects and states joined to
+// such a one are infinite or NaN too, so it is enough to look at the last.
+__device__ __forceinline__ bool says(float2 e) { return __builtin_isfinite(e.x + e.y); }
+
+// In the place of a product (a NaN that no other effect is given): the word's other half is the state behind the piece, known once the state before it was.
+constexpr unsigned kBehind = 0x7fc00001u;
+__device__ __forceinline__ float through(unsigned long long word, float h) {
+  const float u = __uint_as_float((unsigned)(word >> 32));
+  return (unsigned)word == kBehind ? u : fmaf(__uint_as_float((unsigned)word), h, u);
+}
 
 template <int V>
 struct Shared {
@@ -162,6 +171,8 @@ struct Shared {
 // An effect is an affine map: state -> a state + u.  `first`: the state that the walk begins with.  Waves, pieces and groups are joined in one fixed
 // order, so results do not depend on which block runs when.  A piece waits for those before it in its group and for the group's start; all
 // of them have drawn their tickets before, so their blocks run already and wait for nothing behind them.
+// Joined effects hold products of up to 2048 decays, a walk from wave to wave none of more than 16.  Where such a product leaves fp32's range, pieces are gone through one
+// after the other here too: one whose own effect says nothing makes known the state behind it as soon as it knows the one before it.  (Asking whether that is so is 1 % of 65536 x 1 x 1024.)
 template <int V, bool CHAINED>
 __device__ __forceinline__ void begin_with(const ScanArgs &s, Shared<V> &sh, const Place<V> &at, int64_t piece, int waves, Vals<V> a, Vals<V> u, Vals<V> &first,
                                            Vals<V> &state) {
@@ -179,13 +190,29 @@ __device__ __forceinline__ void begin_with(const ScanArgs &s, Shared<V> &sh, con
     const int64_t group = piece / kGroup;
     const int before = (int)(piece - group * kGroup);
     const int64_t row = s.B * s.D, column = (int64_t)at.b * s.D + at.d;
+    bool late = false;                                       // whether one of the wave's effects says nothing
+    auto effect = [&](int v) {                               // of this piece
+      float2 e = mine[0][v][lane];
+      for (int w = 1; w < waves; ++w) e = after(e, mine[w][v][lane]);
+      return e;
+    };
+    auto one_by_one = [&](int v, float h) {                  // the state behind the pieces before this one in its group
+      const unsigned long long *p = s.effects + group * kGroup * row + column + v;
+      for (int k = 0; k < before; ++k) h = through(__hip_atomic_load(p + k * row, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT), h);
+      return h;
+    };
+    auto own_waves = [&](int v, float h) {                   // and then behind this one
+      for (int w = 0; w < waves; ++w) h = fmaf(mine[w][v][lane].x, h, mine[w][v][lane].y);
+      return h;
+    };
     if (wave == 0 && before < kGroup - 1 && piece < s.pieces - 1) {
 #pragma unroll
       for (int v = 0; v < V; ++v) {
-        float2 e = mine[0][v][lane];
-        for (int w = 1; w < waves; ++w) e = after(e, mine[w][v][lane]);
-        if (at.owns(v)) __hip_atomic_store(s.effects + piece * row + column + v, together(e.x, e.y), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        const float2 e = effect(v);
+        late |= !says(e);
+        if (at.owns(v) && says(e)) __hip_atomic_store(s.effects + piece * row + column + v, together(__float_as_uint(e.x), e.y), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
       }
+      late = __any(late);
     }
     if (kEach * wave < before) {
       const int n = min(before - kEach * wave, kEach);
@@ -229,6 +256,10 @@ __device__ __forceinline__ void begin_with(const ScanArgs &s, Shared<V> &sh, con
           for (int w = 0; w < waves; ++w) e = after(e, mine[w][v][lane]);
         past[v] = e;
       }
+      bool mute = false;
+#pragma unroll
+      for (int v = 0; v < V; ++v) mute |= !says(past[v]);
+      mute = __any(mute);
       unsigned e[V];
 #pragma unroll
       for (int v = 0; v < V; ++v) e[v] = __float_as_uint(state[v]);
@@ -247,10 +278,15 @@ __device__ __forceinline__ void begin_with(const ScanArgs &s, Shared<V> &sh, con
 #pragma unroll
       for (int v = 0; v < V; ++v) {
         const float start = __uint_as_float(e[v]);
-        const unsigned bits = __float_as_uint(fmaf(past[v].x, start, past[v].y));
+        float next = fmaf(past[v].x, start, past[v].y), here = fmaf(until[v].x, start, until[v].y);
+        if (mute) {
+          here = one_by_one(v, start);
+          next = own_waves(v, here);
+        }
+        const unsigned bits = __float_as_uint(next);
         if (ends && at.owns(v))
           __hip_atomic_store(s.starts + (group + 1) * row + column + v, bits == ~0u ? 0x7fc00000u : bits, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        sh.start[v][lane] = fmaf(until[v].x, start, until[v].y);
+        sh.start[v][lane] = here;
       }
     }
     if (group > 0) {
@@ -259,8 +295,20 @@ __device__ __forceinline__ void begin_with(const ScanArgs &s, Shared<V> &sh, con
       for (int v = 0; v < V; ++v) state[v] = sh.start[v][lane];
     } else {
 #pragma unroll
+      for (int v = 0; v < V; ++v) {
+        float h = state[v];
+        for (int w = 0; kEach * w < before; ++w) {
+          const float2 e = sh.theirs[w][v][lane];
+          h = fmaf(e.x, h, e.y);
+        }
+        state[v] = __any(!__builtin_isfinite(h)) ? one_by_one(v, state[v]) : h;
+      }
+    }
+    if (late) {
+#pragma unroll
       for (int v = 0; v < V; ++v)
-        for (int w = 0; kEach * w < before; ++w) state[v] = fmaf(sh.theirs[w][v][lane].x, state[v], sh.theirs[w][v][lane].y);
+        if (at.owns(v) && !says(effect(v)))
+          __hip_atomic_store(s.effects + piece * row + column + v, together(kBehind, own_waves(v, state[v])), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     }
   }
 #pragma unroll
