@@ -507,7 +507,7 @@ chn_status chn_sample(const chn_array *logits, const chn_array *u, const chn_arr
  *   and no prompt), the first prompt[n] of them being the prompt.  With c the number of times i stands behind the prompt:
  *     repetition (N,) F32: z / repetition where z > 0, else z * repetition, if i is anywhere in the text;
  *     frequency (N,) F32:  then z - frequency * c;      presence (N,) F32: then z - presence, if c > 0;
- *   bias_ids (N,M) I32 or I64 and bias (N,M) F32: then z + the biases whose id is i, added up in the order of the list;
+ *   bias_ids (N,M) I32 or I64, the type of tokens where both are given (CHN_ERR_DTYPE), and bias (N,M) F32: then z + the biases whose id is i, added up in the order of the list;
  *   allowed (N, ceil(V/32)) I32: then -inf unless bit i % 32 of word i / 32 is set.  A mask may leave nothing.
  * Every parameter NULL where it is not used (no tokens: empty lists; biases without ids are CHN_ERR_NULL); stride 0: one row for all.  lengths and prompt are cut to 0 .. L,
  * ids outside [0, V) are passed over.  out: (N,V) F32 or BF16, which may be the array of logits.  fp32 arithmetic in a fixed order, rounded once at the

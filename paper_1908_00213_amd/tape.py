@@ -2120,8 +2120,10 @@ class _Generates:
         filters = (row(temperature, np.float32), row(top_k, np.int64), row(top_p, np.float32), row(min_p, np.float32))
 
         def rows(v, dt):
-            if v is None or (hasattr(v, "shape") and not isinstance(v, np.ndarray)):
+            if v is None:
                 return v
+            if hasattr(v, "shape") and not isinstance(v, np.ndarray):
+                return v.expand(Bn, v.shape[0]) if len(v.shape) == 1 else v      # (one row for all, without a copy)
             v = np.asarray(v, dtype=dt)
             return F.from_numpy(np.array(np.broadcast_to(v, (Bn, v.shape[-1]))))
         penalties = {"repetition": row(repetition, np.float32), "frequency": row(frequency, np.float32), "presence": row(presence, np.float32)}
@@ -2130,6 +2132,8 @@ class _Generates:
         if any(p is not None for p in penalties.values()):
             text = F.text(ids, n_steps, u.shape[0])
             adjusts.update(penalties, prompt=F.from_numpy(np.full(Bn, n_steps, dtype=np.int64)))
+            if adjusts["bias_ids"] is not None:                                   # (both lists of tokens are of one type, the text's)
+                adjusts["bias_ids"] = F.text(adjusts["bias_ids"].reshape(-1), Bn, 0)
             out = text[n_steps:]
         else:
             out = F.empty(tuple(u.shape), "i64")
