@@ -551,8 +551,9 @@ chn_status chn_gated_scan_bwd(int kind, const chn_array *gate, const chn_array *
  * One product in fp32 and one rounding.
  * Backward: dtable[v] = (dtable[v] +) scale * (the sum of the rows n of dout with ids[n] = v); dout (N,D) F32 or BF16, dtable (V,D) F32.  Unlike
  * chn_embed_bwd, which looks through all ids for every few rows of the table, it sorts the ids first: work grows with N + V, not with their product.
- * Sums are fp32 in a fixed order (the same bits from run to run): the rows of a token one after the other, of a token that stands often in pieces of 64 in
- * the order of n, then the pieces.  N and V below 2^31 (CHN_ERR_SHAPE).
+ * Sums are fp32 in a fixed order (the same bits from run to run): the rows of a token one after the other, in the order of n.  Where there are more than 256 ids, those of a token
+ * with more than 64 rows are added up by the pieces of 64 places that the sorted list is cut in (of which its first and its last one hold other tokens too), and these sums one
+ * after the other in eight shares of neighbouring pieces, then the shares.  N and V below 2^31 (CHN_ERR_SHAPE).
  * ws: chn_embed_sorted_workspace_bytes(ids, dtable) bytes, 256-byte aligned, the library's until the work on `stream` is done. */
 chn_status chn_embed_scaled_fwd(const chn_array *table, const chn_array *ids, double scale, const chn_array *out, chn_stream stream);
 size_t chn_embed_sorted_workspace_bytes(const chn_array *ids, const chn_array *dtable);

@@ -75,14 +75,15 @@ def embed_scaled(table, ids, scale):
 
 
 def embed_scaled_bwd(ids, dout, rows, scale):
-    """The table's gradient and its bound: rows one after the other in pieces of 64 at most, then the pieces (in 16 shares), then the scale."""
+    """The table's gradient and its bound: up to 256 ids a token's rows one after the other; above, rows one after the other in pieces of 64 at most, then the pieces (in 8
+    shares, each of which is no longer than all of them); then the scale.  A sum is off by a rounding of the sum of magnitudes for each addition on a row's way."""
     ids, dout = np.asarray(ids), np.asarray(dout, np.float64)
     ok = (ids >= 0) & (ids < rows)
     g, s, n = np.zeros((rows, dout.shape[1])), np.zeros((rows, dout.shape[1])), np.zeros(rows)
     np.add.at(g, ids[ok], dout[ok])
     np.add.at(s, ids[ok], np.abs(dout[ok]))
     np.add.at(n, ids[ok], 1)
-    depth = np.minimum(n, 64) + np.ceil(n / 64) + 20
+    depth = (n if len(ids) <= 256 else np.minimum(n, 64) + np.ceil(n / 64)) + 20
     return g * scale, s * abs(scale) * (depth * U)[:, None]
 
 

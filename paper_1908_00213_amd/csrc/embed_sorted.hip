@@ -319,29 +319,16 @@ __device__ __forceinline__ void add_rows(F row, int i, int n, int64_t at, float 
     }
 }
 
-// The sum of n rows, 64 of them at most, in a lane's columns, in the order in which the lanes hold their numbers.
+// Adds n rows, 64 of them at most, to a lane's columns, in the order in which the lanes hold their numbers.  A lane behind the last whole unit of a row adds the row's last
+// E columns; `own_columns` moves the sums to where the lane's own ones begin.
 template <typename T, int E>
-__device__ __forceinline__ void sum_places(const SumArgs &s, uint32_t place, int n, int64_t d, float (&sum)[E]) {
+__device__ __forceinline__ void add_places(const SumArgs &s, uint32_t place, int n, int64_t d, float (&sum)[E]) {
   auto row = [&](int i) { return static_cast<const T *>(s.dout) + (int64_t)(uint32_t)__builtin_amdgcn_readlane((int)place, i) * s.dp; };
-#pragma unroll
-  for (int e = 0; e < E; ++e) sum[e] = 0.0f;
   if (s.D >= E) {
-    const int64_t at = min(d, s.D - E);                      // (behind the last whole unit: the row's last E columns)
+    const int64_t at = min(d, s.D - E);
     int i = 0;
     for (; n - i > kTogether / 2; i += kTogether) add_rows<T, E, kTogether>(row, i, n, at, sum);
     for (; i < n; i += kTogether / 4) add_rows<T, E, kTogether / 4>(row, i, n, at, sum);
-    const int off = (int)min(d - at, (int64_t)E);
-    if (__any(off > 0)) {
-      float moved[E];
-#pragma unroll
-      for (int e = 0; e < E; ++e) {
-        moved[e] = 0.0f;
-#pragma unroll
-        for (int f = e; f < E; ++f) moved[e] = f == e + off ? sum[f] : moved[e];
-      }
-#pragma unroll
-      for (int e = 0; e < E; ++e) sum[e] = moved[e];
-    }
   } else {
     for (int i = 0; i < n; ++i) {
       const T *r = row(i);
@@ -350,12 +337,30 @@ __device__ __forceinline__ void sum_places(const SumArgs &s, uint32_t place, int
     }
   }
 }
+template <int E>
+__device__ __forceinline__ void own_columns(const SumArgs &s, int64_t d, float (&sum)[E]) {
+  const int off = s.D >= E ? (int)min(d - min(d, s.D - E), (int64_t)E) : 0;
+  if (__any(off > 0)) {
+    float moved[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      moved[e] = 0.0f;
+#pragma unroll
+      for (int f = e; f < E; ++f) moved[e] = f == e + off ? sum[f] : moved[e];
+    }
+#pragma unroll
+    for (int e = 0; e < E; ++e) sum[e] = moved[e];
+  }
+}
 
-// The same for places [lo, hi) of the sorted list: each lane fetches one, and from there on only rows are waited for.
+// The sum of the rows at places [lo, hi) of the sorted list, 64 at most: each lane fetches one, and from there on only rows are waited for.
 template <typename T, int E>
 __device__ __forceinline__ void sum_rows(const SumArgs &s, uint32_t lo, uint32_t hi, int64_t d, float (&sum)[E]) {
   const int n = __builtin_amdgcn_readfirstlane((int)(hi - lo));
-  sum_places<T, E>(s, s.places[min(lo + (threadIdx.x & 63), hi - 1)], n, d, sum);
+#pragma unroll
+  for (int e = 0; e < E; ++e) sum[e] = 0.0f;
+  add_places<T, E>(s, s.places[min(lo + (threadIdx.x & 63), hi - 1)], n, d, sum);
+  own_columns<E>(s, d, sum);
 }
 
 template <int E>
@@ -440,7 +445,7 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(SumArgs s) {
   }
 }
 
-// Few ids: nothing is sorted.  A wave looks through them for its rows' tokens, 64 at a time, and adds up the rows that it finds there, then these sums.
+// Few ids: nothing is sorted.  A wave looks through them for its rows' tokens, 64 at a time, and adds the rows that it finds there to the sum.
 constexpr int kDirect = 256;
 
 template <typename T, typename L>
@@ -462,30 +467,30 @@ __global__ __launch_bounds__(256) void embed_direct_kernel(SumArgs s, const L *i
     }
   }
   for (int r = 0; r < n; ++r) {
-    float total[E];
-    bool any = false;
-#pragma unroll
-    for (int e = 0; e < E; ++e) total[e] = 0.0f;
+    unsigned long long found[M], any = 0;                    // the places of the row's token
 #pragma unroll
     for (int m = 0; m < M; ++m) {
-      if (m * 64 >= N) break;
-      unsigned long long found = __ballot(id[m] == (uint32_t)(v0 + r));
-      if (!found) continue;
-      any = true;
-      // the found places in their order, one to a lane
-      const int count = __popcll(found);
-      int place = 0;
-      for (int k = 0; k < count; ++k, found &= found - 1) place = lane == k ? m * 64 + (int)__builtin_ctzll(found) : place;
-      float sum[E];
-      sum_places<T, E>(s, (uint32_t)place, count, d, sum);
+      found[m] = __ballot(id[m] == (uint32_t)(v0 + r));
+      any |= found[m];
+    }
+    if (!any) {
+      if (!s.accumulate) zero_row<E>(s, v0 + r, d - lane * E);
+      continue;
+    }
+    float sum[E];
 #pragma unroll
-      for (int e = 0; e < E; ++e) total[e] += sum[e];
+    for (int e = 0; e < E; ++e) sum[e] = 0.0f;
+#pragma unroll
+    for (int m = 0; m < M; ++m) {
+      if (!found[m]) continue;
+      // in their order, one to a lane
+      const int count = __popcll(found[m]);
+      int place = 0;
+      for (int k = 0; k < count; ++k, found[m] &= found[m] - 1) place = lane == k ? m * 64 + (int)__builtin_ctzll(found[m]) : place;
+      add_places<T, E>(s, (uint32_t)place, count, d, sum);
     }
-    if (any) {
-      if (d < s.D) write_row<E>(s, v0 + r, d, total);
-    } else if (!s.accumulate) {
-      zero_row<E>(s, v0 + r, d - lane * E);
-    }
+    own_columns<E>(s, d, sum);
+    if (d < s.D) write_row<E>(s, v0 + r, d, sum);
   }
 }
 
