@@ -37,13 +37,13 @@ __device__ __forceinline__ int cut(const void *p, int is64, int64_t at, int L) {
 }
 
 struct Penalties {
-  float repetition, inverse, frequency, presence;
+  float repetition, up, divisor, inverse, frequency, presence;   // divisor: up times the repetition, so that its reciprocal is in fp32's range
   bool rep;
   // (without frequency or presence: zeros, which change nothing but the sign of a zero)
   __device__ __forceinline__ float apply(float z, uint32_t word) const {
     const uint32_t c = word & kCount;
     if (rep) {
-      const float q = z * inverse, d = fmaf(fmaf(-q, repetition, z), inverse, q);   // z / repetition, its rounding made good
+      const float y = z * up, q = y * inverse, d = fmaf(fmaf(-q, divisor, y), inverse, q);   // z / repetition, its rounding made good
       const float less = z > 0.0f ? (d == d ? d : q) : z * repetition;
       z = word & (kSeen | kCount) ? less : z;
     }
@@ -103,7 +103,9 @@ __global__ __launch_bounds__(kThreads, 8) void adjust_kernel(AdjustArgs a) {
   Penalties p;
   p.rep = a.repetition != nullptr;
   p.repetition = p.rep ? a.repetition[n * a.sr] : 1.0f;
-  p.inverse = 1.0f / p.repetition;
+  p.up = fabsf(p.repetition) < 0x1p-100f ? 0x1p40f : 1.0f;   // (a logit that this takes out of the range has an infinite quotient)
+  p.divisor = p.repetition * p.up;
+  p.inverse = 1.0f / p.divisor;
   p.frequency = a.frequency ? a.frequency[n * a.sf] : 0.0f;
   p.presence = a.presence ? a.presence[n * a.ss] : 0.0f;
   const ID *tokens = static_cast<const ID *>(a.tokens) + n * a.pt, *named = static_cast<const ID *>(a.bias_ids) + n * a.pi;
