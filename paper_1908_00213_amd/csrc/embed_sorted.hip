@@ -671,9 +671,14 @@ chn_status chn_embed_sorted_bwd(const chn_array *ids, const chn_array *dout, dou
   o.V = V; o.N = (uint32_t)N; o.share = z.share; o.bits = z.bits; o.blocks = z.blocks;
   o.counts = words(z.counts); o.starts = words(z.starts); o.ends = words(z.ends);
   o.keys_out = words(z.keys); o.places_out = words(z.places);
-  // (us, cleared beside the sort / by the sums: 16384 x 1024 bf16 into 131072 rows 133 / 143, 32768 x 1024 into 65536 87 / 99, into 32768 71 / 65, 65536 x 1024 into 65536 121 / 113,
-  // 65536 x 512 fp32 into 131072 94 / 90)
-  const bool filled = z.blocks > 1 && !accumulate && N <= V / 2;
+  // Clearing beside the sort against clearing by the sums, us with tokens as frequent as words are (and evenly drawn), in graphs of ten calls.
+  // bfloat16 dout, N <= V / 2: 16384 x 1024 into 131072 130 / 141 (132 / 150), 32768 x 1024 into 65536 87 / 97 (97 / 105), 65536 x 1024 into 131072 155 / 164 (181 / 184), 65536 x 512 into
+  // 131072 87 / 101 (96 / 106), 65536 x 4096 into 131072 590 / 611 (710 / 593); at N = V 32768 x 1024 66 / 67 (71 / 66), 65536 x 1024 102 / 107 (121 / 114).
+  // fp32 dout, whose sums write zeros in narrower pieces: 10000 x 650 into 100000 98 / 114 (98 / 110), 8500 x 1024 into 68000 82 / 86 (82 / 84), 16384 x 512 into 131072 75 / 80 (77 / 78); beyond each
+  // of its three limits 32768 x 512 into 131072 81 / 83 (85 / 80) and 65536 x 512 into 131072 96 / 91 (101 / 84), 65536 x 128 into 524288 99 / 89 (101 / 88), 16384 x 1024 into 131072 138 / 131 (143 / 130)
+  // and 65536 x 1024 into 200000 246 / 217 (269 / 191).
+  const bool mostly_zeros = dout->dtype == CHN_BF16 ? N <= V / 2 : N <= V / 8 && N <= 1 << 15 && V * D < 1 << 27;
+  const bool filled = z.blocks > 1 && !accumulate && mostly_zeros;
   o.dtable = static_cast<float *>(dtable->data); o.tp = tp; o.D = D;
   if (z.blocks == 1) {
     hipLaunchKernelGGL(embed_sort_few_kernel, dim3(1), dim3(1024), 0, st, o, z.passes);
