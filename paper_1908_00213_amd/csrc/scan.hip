@@ -280,8 +280,11 @@ __device__ __forceinline__ void begin_with(const ScanArgs &s, Shared<V> &sh, con
         const float start = __uint_as_float(e[v]);
         float next = fmaf(past[v].x, start, past[v].y), here = fmaf(until[v].x, start, until[v].y);
         if (mute) {
-          here = one_by_one(v, start);
-          next = own_waves(v, here);
+          const float there = one_by_one(v, start), behind = own_waves(v, there);
+          if (!says(past[v])) {                              // (every column by itself, whatever its neighbours hold)
+            here = there;
+            next = behind;
+          }
         }
         const unsigned bits = __float_as_uint(next);
         if (ends && at.owns(v))
@@ -297,11 +300,13 @@ __device__ __forceinline__ void begin_with(const ScanArgs &s, Shared<V> &sh, con
 #pragma unroll
       for (int v = 0; v < V; ++v) {
         float h = state[v];
-        for (int w = 0; kEach * w < before; ++w) {
-          const float2 e = sh.theirs[w][v][lane];
-          h = fmaf(e.x, h, e.y);
+        for (int w = 0; kEach * w < before; ++w) h = fmaf(sh.theirs[w][v][lane].x, h, sh.theirs[w][v][lane].y);
+        const bool mute = !__builtin_isfinite(h);
+        if (__any(mute)) {
+          const float there = one_by_one(v, state[v]);
+          h = mute ? there : h;
         }
-        state[v] = __any(!__builtin_isfinite(h)) ? one_by_one(v, state[v]) : h;
+        state[v] = h;
       }
     }
     if (late) {
