@@ -5,7 +5,7 @@
 // Whole numbers are counted, so the order in which the list is seen does not show.  The few tokens with biases are left out by that walk: the threads
 // that hold the list's entries write them, each token by the thread with its first entry, which adds up the others in the list's order.
 //
-// Bound by memory where the launch fills the chip: 256 x 131072 fp32 with lists of up to 8192 tokens, 300 biases and masks 67 us (4.1 TB/s), without any of them 40 (a plain copy 37,
+// Bound by memory where the launch fills the chip: 256 x 131072 fp32 with lists of up to 8192 tokens, 300 biases and masks 68 us (4.1 TB/s), without any of them 40 (a plain copy 37,
 // part of it in the last-level cache).  A block's chain of waits is what costs beside that, so the logits, the masks and the list's first part are fetched before anything is
 // counted, and four blocks of 512 threads with 16 logits each share a compute unit (two with 32 each: 80).  Biases of one id that stands twice were 40 us more while every
 // thread looked through the whole list for its id: they are put in order in LDS first.

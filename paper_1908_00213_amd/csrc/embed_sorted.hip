@@ -7,9 +7,9 @@
 // Every order is fixed by the ids alone.  Up to 256 ids are not sorted: every wave looks for its rows' tokens among them (1 x 650 into 10000 rows 21 -> 9 us, 128 ids 21 -> 9;
 // 512 ids 18 with the sort, 25 without).
 //
-// Bound by memory for a large table: 65536 x 1024 bf16 into 131072 rows 30 us for the lookup (4.5 TB/s of its output), 158 for the gradient, of which clearing 537 MB takes 100 (5.3 TB/s)
+// Bound by memory for a large table: 65536 x 1024 bf16 into 131072 rows 30 us for the lookup (4.5 TB/s of its output), 155 for the gradient, of which clearing 537 MB takes 104 (5.2 TB/s)
 // while a few blocks sort beside it, and sums 40.  Cleared by the launch that sums, it was 31 us for the sort alone and 146 for the sums.  Stores past the caches: what
-// follows does not wait for their lines to leave (the lookup 41 us and the sums 58 with ordinary stores).  Small cases are launches: 4480 x 650 into 10000 rows 14 (one block sorts), 13 and 5 traced.
+// follows does not wait for their lines to leave (the lookup 41 us and the sums 58 with ordinary stores).  Small cases are launches: 4480 x 650 into 10000 rows 13 (one block sorts), 13 and 5 traced.
 #include "rows.h"
 
 namespace chn {

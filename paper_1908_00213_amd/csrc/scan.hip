@@ -15,10 +15,10 @@
 //     every wait is bounded: what has not come after kPolls looks counts as NaN.
 //
 // Bound by memory, and in the second way by how long a block holds its registers (a third of which it waits: 1.4 us for the ticket, 3.4 to 4.6 for its loads, 3 to 4 for the others'
-// words, 1.6 for its stores).  2048 x 8 x 4096 bf16 100 us forward, 160 backward (4.0 and 4.2 TB/s), 65536 x 1 x 1024 103 and 144; without the waiting it would be 92 and 78 forward.
+// words, 1.6 for its stores).  2048 x 8 x 4096 bf16 100 us forward, 157 backward (4.0 and 4.3 TB/s), 65536 x 1 x 1024 105 and 144; without the waiting it would be 92 and 78 forward.
 // Of groups of 8, 16, 32 and 64 pieces, pieces of 64, 128 and 256 steps and two or three blocks on a compute unit none was faster than these by more than 3 %, pieces of 64 a quarter
-// slower; tiles dealt out over the XCDs, with tickets for each: 777 x 5 x 1001 43.5 -> 40.8, 65536 x 1 x 1024 245 -> 284 (a stripe of every row for an XCD, few channels of its L2).  The walk against single pieces, both directions, us: 200 x 128 x 650 fp32 136 / 146, 256 x 64 x 2048 bf16 112 / 120, 512 x 32 x 2048 114 / 121 (512 tiles); with
-// 256 tiles 133 / 124 (1024 x 16 x 2048) and 263 / 243 (2048 x 8 x 4096): one block on a compute unit.  Results past the caches: 255 -> 249 for 2048 x 8 x 4096, 262 -> 249 for 65536 x 1 x 1024.
+// slower; tiles dealt out over the XCDs, with tickets for each: 777 x 5 x 1001 43.5 -> 40.8, 65536 x 1 x 1024 245 -> 284 (a stripe of every row for an XCD, few channels of its L2).  The walk against single pieces, both directions, us: 200 x 128 x 650 fp32 136 / 147, 256 x 64 x 2048 bf16 113 / 119, 512 x 32 x 2048 112 / 122 (512 tiles); with
+// 256 tiles 132 / 125 (1024 x 16 x 2048) and 262 / 248 (2048 x 8 x 4096): one block on a compute unit.  Results past the caches: 255 -> 249 for 2048 x 8 x 4096, 262 -> 249 for 65536 x 1 x 1024.
 #include "rows.h"
 
 #include <initializer_list>
@@ -416,7 +416,7 @@ __global__ __launch_bounds__(64 * kWaves, 4) void scan_fwd_kernel(ScanArgs s) {
 }
 
 // Backwards: the wave whose steps are the last ones begins.  The state before each step is computed again from the one that the forward pass kept.  Of a
-// step stay three numbers and dy: the smaller of a and 1 - a (with its sign saying which one it is: the other one is 1 minus it, to half a step),
+// step stay two numbers and dy: the smaller of a and 1 - a (with its sign saying which one it is: the other one is 1 minus it, to half a step),
 // and what dgate has G multiplied with.
 template <typename TI, typename TO, int V, bool SIGMOID, bool CHAINED>
 __global__ __launch_bounds__(64 * kWaves, 4) void scan_bwd_kernel(ScanArgs s) {
