@@ -2132,8 +2132,9 @@ class _Generates:
         if any(p is not None for p in penalties.values()):
             text = F.text(ids, n_steps, u.shape[0])
             adjusts.update(penalties, prompt=F.from_numpy(np.full(Bn, n_steps, dtype=np.int64)))
-            if adjusts["bias_ids"] is not None:                                   # (both lists of tokens are of one type, the text's)
-                adjusts["bias_ids"] = F.text(adjusts["bias_ids"].reshape(-1), Bn, 0)
+            named = adjusts["bias_ids"]                                           # (both lists of tokens are of one type, the text's)
+            if named is not None and len(named.shape) == 2 and named.shape[0] == Bn:
+                adjusts["bias_ids"] = F.text(named.reshape(-1), Bn, 0)
             out = text[n_steps:]
         else:
             out = F.empty(tuple(u.shape), "i64")

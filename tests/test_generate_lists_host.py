@@ -35,3 +35,22 @@ def test_arrays_of_the_backend(ranks, ids_type, penalty):
         device = {k: torch.from_numpy(v if r == 1 else np.tile(v, (Bn, 1))).to(types[k]) for (k, v), r in zip(lists.items(), ranks)}
         got, _ = model.generate(ids, n, u, **device, **penalty)
         assert np.array_equal(got, want) and (got != 5).all()
+
+
+@pytest.mark.parametrize("penalty", [{}, {"repetition": 1.3}])
+def test_lists_of_other_shapes_reach_the_entry_point_as_they_are(penalty):
+    """Which refuses them: ids of (2 B, M) are not those of (B, 2 M)."""
+    rng = np.random.default_rng(4)
+    n, Bn, V = 4, 2, 11
+    seen = []
+
+    class Backend(RecurrentBackend):
+        def logits_adjust(self, logits, out, **k):
+            seen.append(tuple(k["bias_ids"].shape))
+            raise ValueError("refused")
+    for shape in ((4, 3), (1, 4), (2, 3, 1)):
+        with T.using_backend(Backend()):
+            model = T.GatedLanguageModel(gated_params(rng))
+            with pytest.raises(ValueError, match="refused"):
+                model.generate(rng.integers(0, V, n * Bn), n, rng.random((1, Bn)), bias_ids=torch.zeros(shape, dtype=torch.int64), bias=torch.zeros(2, 6), **penalty)
+        assert seen.pop() == shape
